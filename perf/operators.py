@@ -4,8 +4,8 @@ A case is a dict of plain values; `op` names the public entry point:
 
   add_norm   amd.add_norm_fp8: residual add, RMS norm and gain, e4m3 with a scale per row and block of 128 columns
   quant      amd.quant_fp8: the same rounding of rows that no norm precedes (inputs of the O and down projections)
-  gemm       amd.gemm_fp8: product of such rows with e4m3 weights that have a scale per block of 128 x 128; epilogue 0 stores,
-             1 adds to a residual stream, 2 is SiLU * mul of a gate and an up matrix
+  gemm       amd.gemm_fp8: product of such rows with e4m3 weights that have a scale per block of 128 x 128; epilogue 0 stores
+             (fp32 or bf16), 2 is SiLU * mul of a gate and an up matrix
   sample     amd.sample_rows: temperature, top-k, top-p and min-p, the distribution and a draw by a given uniform
 
 Widths are those of synth.config's pairs.  The plain forms are elementary torch operations; `exact` is the definition in
@@ -40,13 +40,13 @@ def listed():
         # what the 7B down projection reads in a 2048-token prompt
         {"name": "quant_11008_m2047", "op": "quant", "m": 2047, "k": 11008, "x": "bf16"},
         # the output projection of a 1B-shape draft model: the smallest matrix of a decode step, one token
-        {"name": "gemm_2048x2048_m1", "op": "gemm", "m": 1, "n": 2048, "k": 2048, "epilogue": 0},
-        # the down projection of the 70B shape over a verify window of 7, added to the residual stream
-        {"name": "gemm_8192x28672_m7", "op": "gemm", "m": 7, "n": 8192, "k": 28672, "epilogue": 1},
+        {"name": "gemm_2048x2048_m1", "op": "gemm", "m": 1, "n": 2048, "k": 2048, "epilogue": 0, "out": "fp32"},
+        # the down projection of the 70B shape over a verify window of 7, for the residual add that follows
+        {"name": "gemm_8192x28672_m7", "op": "gemm", "m": 7, "n": 8192, "k": 28672, "epilogue": 0, "out": "bf16"},
         # QKV of the 7B shape for a short prompt or a chunk of one: between the two regimes
-        {"name": "gemm_12288x4096_m100", "op": "gemm", "m": 100, "n": 12288, "k": 4096, "epilogue": 0},
+        {"name": "gemm_12288x4096_m100", "op": "gemm", "m": 100, "n": 12288, "k": 4096, "epilogue": 0, "out": "bf16"},
         # gate/up of the 70B shape for its 4096-token prompt: the largest single call there is
-        {"name": "gemm_57344x8192_m4095", "op": "gemm", "m": 4095, "n": 57344, "k": 8192, "epilogue": 2},
+        {"name": "gemm_57344x8192_m4095", "op": "gemm", "m": 4095, "n": 57344, "k": 8192, "epilogue": 2, "out": "bf16"},
         # a draft step's draw at the pairs' vocabulary with everyday settings
         {"name": "sample_32000_m1", "op": "sample", "rows": 1, "v": 32000, "temperature": 0.75, "top_k": 50, "top_p": 0.9375,
          "min_p": 0.0, "coarse": False},
@@ -75,10 +75,10 @@ def draw(rng):
     if op == "quant":
         return {"op": op, "m": _log_int(rng, 1, 4096), "k": _sixteens(rng, 256, 28672), "x": rng.choice(["bf16", "bf16", "fp32"])}
     if op == "gemm":
-        epilogue = rng.choice([0, 0, 1, 2])
+        epilogue, out = rng.choice([(0, "fp32"), (0, "bf16"), (0, "bf16"), (2, "bf16")])
         m = rng.choice([_log_int(rng, 1, 32), _log_int(rng, 1, 4096)])
         n = _sixteens(rng, 256, 57344, 32 if epilogue == 2 else 16)
-        return {"op": op, "m": m, "n": n, "k": _sixteens(rng, 256, 8192 if n > 16384 else 28672), "epilogue": epilogue}
+        return {"op": op, "m": m, "n": n, "k": _sixteens(rng, 256, 8192 if n > 16384 else 28672), "epilogue": epilogue, "out": out}
     return {"op": op, "rows": _log_int(rng, 1, 48), "v": _log_int(rng, 1000, 160000), "temperature": rng.choice([0.5, 0.75, 1.0, 1.5]),
             "top_k": rng.choice([0, 0, _log_int(rng, 1, 2000)]), "top_p": rng.choice([1.0, rng.randint(16, 63) / 64]),
             "min_p": rng.choice([0.0, 0.0, rng.randint(1, 16) / 128]), "coarse": rng.choice([False, True])}
@@ -125,13 +125,13 @@ def _inputs(case, seed):
     elif op == "gemm":
         m, n, k, epilogue = case["m"], case["n"], case["k"], case["epilogue"]
         q, scale = _quantize(_activations(g, m, k))
-        s = {"x": q, "x_scale": scale, "y": 2 * _normal(g, m, n) if epilogue == 1 else None}
+        s = {"x": q, "x_scale": scale}
         s["weights"] = [_weight(g, n // 2, k), _weight(g, n // 2, k)] if epilogue == 2 else [_weight(g, n, k)]
     else:
         rows, v = case["rows"], case["v"]
         logits = 2.5 * _normal(g, rows, v)                  # a tail of small ids, and a few that stand out
-        top = torch.randint(v, (rows, 24), generator=g, device="cuda")
-        logits.scatter_add_(1, top, 6 + 2 * _normal(g, rows, 24))
+        top = (torch.randint(v, (rows, 1), generator=g, device="cuda") + torch.arange(24, device="cuda") * (v // 24)) % v
+        logits.scatter_(1, top, 6 + 3 * _normal(g, rows, 24))
         s = {"logits": logits.to(torch.bfloat16).float() if case["coarse"] else logits,
              "u": torch.rand(rows, generator=g, device="cuda")}
     return s
@@ -163,7 +163,7 @@ def run(state):
             q, scale = amd.quant_fp8(state["x"])
             return {"q": q, "scale": scale}
         if op == "gemm":
-            return amd.gemm_fp8(state["x"], state["x_scale"], state["packed"], case["epilogue"], state["y"])
+            return amd.gemm_fp8(state["x"], state["x_scale"], state["packed"], case["epilogue"], TYPES[case["out"]])
         tokens, q = amd.sample_rows(state["logits"], state["u"], case["temperature"], 1.0, case["top_k"], case["top_p"],
                                     case["min_p"])
         return {"tokens": tokens, "q": q}
@@ -173,7 +173,7 @@ def run(state):
         q, scale = _quantize(state["x"].float())
         return {"q": q, "scale": scale}
     if op == "gemm":
-        return _plain_gemm(state, case["epilogue"])
+        return _plain_gemm(state, case["epilogue"], TYPES[case["out"]])
     return _plain_sample(state, case)
 
 
@@ -201,15 +201,13 @@ def _spread(scale, n, k):
     return scale.repeat_interleave(BLOCK, 0)[:n].repeat_interleave(BLOCK, 1)[:, :k]
 
 
-def _plain_gemm(s, epilogue):
+def _plain_gemm(s, epilogue, out):
     m, k = s["x"].shape
     x = s["x"].float() * s["x_scale"].t().repeat_interleave(BLOCK, 1)[:, :k]
     y = [x @ (q.float() * _spread(scale, q.shape[0], k)).t() for q, scale in s["weights"]]
     if epilogue == 2:
-        return (y[0] / (1 + torch.exp(-y[0])) * y[1]).to(torch.bfloat16)
-    if epilogue == 1:
-        return s["y"].add_(y[0])
-    return y[0]
+        return (y[0] / (1 + torch.exp(-y[0])) * y[1]).to(out)
+    return y[0].to(out)
 
 
 def _plain_sample(s, case):
@@ -246,7 +244,7 @@ def work(case):
     if op == "gemm":
         m, n, k = case["m"], case["n"], case["k"]
         kb = -(-k // BLOCK)
-        out = m * n * (4, 8, 1)[case["epilogue"]]
+        out = m * n * size[case["out"]] // (2 if case["epilogue"] == 2 else 1)
         return {"bytes": n * k + 4 * -(-n // BLOCK) * kb + m * k + 4 * m * kb + out, "flops": 2 * m * n * k}
     return {"bytes": case["rows"] * (8 * case["v"] + 8), "flops": 20 * case["rows"] * case["v"]}
 
@@ -297,7 +295,7 @@ def exact(case, seed):
             y.append(out)
         if case["epilogue"] == 2:
             return y[0] * torch.sigmoid(y[0]) * y[1]
-        return y[0] + s["y"].double() if case["epilogue"] == 1 else y[0]
+        return y[0]
     tokens, q = [], []
     for row, u in zip(s["logits"].cpu().numpy().astype(np.float64), s["u"].cpu().numpy().astype(np.float64)):
         w = np.exp((row - row.max()) / case["temperature"])
