@@ -259,6 +259,43 @@ int spec_gemm_partials(const void* x_dev, const void* w_packed_dev, int M, int N
 int spec_dense_gemm(float* y_dev, void* z_dev, const void* x_dev, const void* w_packed_dev, int M, int N, int K,
                     int epilogue, void* stream);
 
+/* ---- 8-bit operands ------------------------------------------------------------------------
+ * e4m3 is the OCP 8-bit type with 4 exponent bits (largest value 448), rounded to nearest even.  Rows x[M][K] have one fp32
+ * scale per row and block of 128 columns (the last one may be short), stored block by block: scale[ceil(K/128)][M]; the value
+ * of an element is e4m3 * scale.  Weights have one per block of 128 x 128: scale[ceil(N/128)][ceil(K/128)].  A scale is
+ * (largest magnitude of the block) / 448; blocks below 2^-100 take 2^-100 / 448.  A NaN stays a NaN of its own, an infinite
+ * value makes its block NaN.  K (d) is a multiple of 16, N of 16; both at most SPEC_FP8_K_MAX, rows of the first two calls
+ * at most SPEC_FP8_ROW_MAX.  All are asynchronous on `stream`, allocate nothing and can be captured. */
+enum { SPEC_F32 = 0, SPEC_BF16 = 1 };
+#define SPEC_FP8_ROW_MAX 32768
+#define SPEC_FP8_K_MAX 1048576
+
+/* Residual add, RMS norm and gain, rounded to e4m3: h[m] += delta[m] (delta may be NULL), in place and rounded to the type of
+ * h; then y = h / sqrt(mean(h^2) + eps) * gain of what is stored, and its e4m3 values q[M][d] and scales.  h, delta: device,
+ * SPEC_F32 or SPEC_BF16, row strides ldh, ldd >= d (elements; ldd also 0: one row for all); gain bf16 [d]; sums in fp32.  A
+ * row's results do not depend on M.  q starts at a multiple of 8, the others at multiples of their elements. */
+int spec_add_norm_quant(void* h_dev, int h_type, long long ldh, const void* delta_dev, int delta_type, long long ldd,
+                      const void* gain_dev, float eps, int M, int d, void* q_dev, float* scale_dev, void* stream);
+/* The e4m3 values q[M][K] and scales of rows as they are: what a projection reads that no norm precedes. */
+int spec_quant_rows(const void* x_dev, int x_type, long long ldx, int M, int K, void* q_dev, float* scale_dev, void* stream);
+/* The same of a weight matrix W[N][K] (bf16 row-major, device), with its scales per block of 128 x 128. */
+int spec_quant_weight(const void* w_dev, int N, int K, void* q_dev, float* scale_dev, void* stream);
+/* Repack e4m3 W[N][K] and its scales into the panels that spec_gemm_quant streams: panel j (16 rows) goes to panel
+ * panel_start + j * panel_step of dst (2 KiB per 128 columns, zeros behind K), with its own row of scales in
+ * dst_scale[panels][ceil(K/128)], so that matrices can be concatenated, or gate and up interleaved, as with spec_pack_weight.
+ * dst starts at a 16-byte address. */
+int spec_pack_quant(void* dst_dev, float* dst_scale_dev, const void* src_dev, const float* src_scale_dev, int N, int K,
+                         int panel_start, int panel_step, void* stream);
+size_t spec_packed_quant_bytes(int N, int K);
+/* y = x W^T of e4m3 rows and packed e4m3 weights, any M >= 1; sums in fp32.  epilogue 0: out[M][N] of out_type, SPEC_F32 or
+ * SPEC_BF16; 2: out[M][N/2], SPEC_BF16, = silu(gate) * up of interleaved panels (N % 32 == 0).  (There is no epilogue 1:
+ * spec_add_norm_quant adds what follows to the residual stream.)  fp32 results are sums of exact products; from 33 rows on
+ * bf16 ones come from 8-bit matrix instructions, which cost them 1.5e-5 before the rounding and take half the time.
+ * x and the packed weights start at 16-byte addresses, out at one of 16 (SPEC_F32) or 8.  Up to 32 rows, a row's results do
+ * not depend on M. */
+int spec_gemm_quant(void* out_dev, int out_type, const void* x_dev, const float* x_scale_dev, const void* w_packed_dev,
+                    const float* w_scale_dev, int M, int N, int K, int epilogue, void* stream);
+
 /* Streaming-read probe: sums `bytes` bytes of device memory with 16-byte loads; used to
  * measure the achievable HBM read ceiling next to the nominal peak.  out_dev: 4 bytes. */
 int spec_read_probe(const void* src_dev, size_t bytes, void* out_dev, void* stream);

@@ -29,6 +29,8 @@ SPEC_OPT_FUSE_SINGLE = 5
 SPEC_OPT_GUESS_TOKENS = 6
 SPEC_OPT_TARGET_TAIL_LAYERS = 7
 EPI_STORE, EPI_RESID, EPI_SWIGLU = 0, 1, 2
+SPEC_F32, SPEC_BF16 = 0, 1
+FP8_BLOCK = 128                                    # columns (and weight rows) that share a scale
 
 
 class ModelDesc(C.Structure):
@@ -85,6 +87,13 @@ SIGNATURES = {
     "spec_gemm_uses_work": (C.c_int, [_P, _P, C.c_int, C.c_int, C.c_int]),
     "spec_gemm_partials": (C.c_int, [_P, _P, C.c_int, C.c_int, C.c_int, _P, _P]),
     "spec_dense_gemm": (C.c_int, [_P, _P, _P, _P, C.c_int, C.c_int, C.c_int, C.c_int, _P]),
+    "spec_add_norm_quant": (C.c_int, [_P, C.c_int, C.c_longlong, _P, C.c_int, C.c_longlong, _P, C.c_float, C.c_int, C.c_int, _P,
+                                    _P, _P]),
+    "spec_quant_rows": (C.c_int, [_P, C.c_int, C.c_longlong, C.c_int, C.c_int, _P, _P, _P]),
+    "spec_quant_weight": (C.c_int, [_P, C.c_int, C.c_int, _P, _P, _P]),
+    "spec_pack_quant": (C.c_int, [_P, _P, _P, _P, C.c_int, C.c_int, C.c_int, C.c_int, _P]),
+    "spec_packed_quant_bytes": (C.c_size_t, [C.c_int, C.c_int]),
+    "spec_gemm_quant": (C.c_int, [_P, C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_int, C.c_int, _P]),
     "spec_read_probe": (C.c_int, [_P, C.c_size_t, _P, _P]),
     "spec_sample_row": (C.c_int, [_P, C.c_int, C.c_float, C.c_float, C.c_float, _P, _P, _P]),
     "spec_accept_rows": (C.c_int, [_P, C.c_int, _P, _P, C.c_int, C.c_int, C.c_float, C.c_float, _PF, C.c_float,
@@ -129,3 +138,4 @@ def check(rc: int) -> int:
 
 
 from .binding import SpecContext, pack_model, gemm, dense_gemm, sample_row, accept_rows, accept_rows_static, read_probe  # noqa: E402,F401
+from .fp8 import Fp8Weight, add_norm_fp8, gemm_fp8, pack_weights_fp8, quant_fp8, quant_weight_fp8  # noqa: E402,F401

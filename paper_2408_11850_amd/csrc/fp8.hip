@@ -1,0 +1,590 @@
+// 8-bit operands for gfx950: residual add + RMS norm to e4m3, rows to e4m3, weights to e4m3 and into operand order, and the
+// products of the two.
+//
+// e4m3 is the OCP type (largest value 448).  A row has one fp32 scale per 128 columns, a weight matrix one per 128 x 128
+// block, so a product is  y[m][n] = sum_b sx[b][m] sw[n / 128][b] sum_{k in block b} x[m][k] w[n][k]:  the inner sum is one
+// v_mfma_f32_16x16x128_f8f6f4 (K = 128, fp32 sums of exact products), the outer one an fp32 multiply-add per result.
+#include <type_traits>
+
+#include "spec_internal.h"
+
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4a;
+typedef __attribute__((ext_vector_type(8), aligned(2))) unsigned short bf16x8a;
+
+#define E4M3_MAX 448.0f
+#define FP8_LEAST 0x1p-100f       // blocks whose largest magnitude is below take this one's scale: no scale is 0 or denormal
+
+// ---- rows -----------------------------------------------------------------------------------------------------------
+// A lane takes 8 neighbouring columns, so that 16 lanes share a block of 128 and its largest magnitude is four rotations
+// inside a row of lanes.
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_ror(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, dpp_ror<0x128>(v));
+  v = fmaxf(v, dpp_ror<0x124>(v));
+  v = fmaxf(v, dpp_ror<0x122>(v));
+  return fmaxf(v, dpp_ror<0x121>(v));
+}
+// every step adds the same two numbers in both lanes of a pair: all lanes hold the same bits
+__device__ __forceinline__ float wave64_sum(float v) {
+  v += dpp_ror<0x128>(v);
+  v += dpp_ror<0x124>(v);
+  v += dpp_ror<0x122>(v);
+  v += dpp_ror<0x121>(v);
+  return groups_sum(v);
+}
+
+template <int T>
+__device__ __forceinline__ void load8(const void* p, size_t at, float (&v)[8]) {
+  if (T == SPEC_F32) {
+    const f32x4a* s = reinterpret_cast<const f32x4a*>(reinterpret_cast<const float*>(p) + at);
+    const f32x4a a = s[0], b = s[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  } else {
+    const bf16x8a a = *reinterpret_cast<const bf16x8a*>(reinterpret_cast<const unsigned short*>(p) + at);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float((unsigned)a[i] << 16);
+  }
+}
+// v becomes what is stored
+template <int T>
+__device__ __forceinline__ void store8(void* p, size_t at, float (&v)[8]) {
+  if (T == SPEC_F32) {
+    f32x4a* s = reinterpret_cast<f32x4a*>(reinterpret_cast<float*>(p) + at);
+    s[0] = f32x4a{v[0], v[1], v[2], v[3]};
+    s[1] = f32x4a{v[4], v[5], v[6], v[7]};
+  } else {
+    bf16x8a a;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bf16 b = __float2bfloat16(v[i]);
+      a[i] = *reinterpret_cast<const unsigned short*>(&b);
+      v[i] = __uint_as_float((unsigned)a[i] << 16);
+    }
+    *reinterpret_cast<bf16x8a*>(reinterpret_cast<unsigned short*>(p) + at) = a;
+  }
+}
+
+// 8 columns of a block of 128 to e4m3; the 16 lanes of the block share its scale.  A NaN is none of the magnitudes and stays
+// NaN; an infinite one makes the scale infinite, and the block NaN.
+__device__ __forceinline__ float block_scale(const float (&v)[8]) {
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(v[i]));
+  return fmaxf(row16_max(a), FP8_LEAST) * (1.0f / E4M3_MAX);
+}
+__device__ __forceinline__ uint2 to_e4m3(const float (&v)[8], float scale) {
+  const float inv = 1.0f / scale;                  // |v * inv| <= 448 up to two roundings, which round to 448
+  int lo = 0, hi = 0;
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inv, v[5] * inv, hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, hi, true);
+  return make_uint2((unsigned)lo, (unsigned)hi);
+}
+
+// XT: type of the rows; DT: of what is added first, -1 none; NORM: RMS norm and gain, else the rows as they are.
+// A row belongs to `wpr` waves of a workgroup; a chunk is the 512 columns a wave takes at a time, at most G per wave.  The sum of
+// squares is formed per chunk and over the chunks in ascending order, so a row's bits do not depend on how it is dealt out.
+#define ROWS_CHUNK 512
+#define ROWS_WAVES_MAX 16
+template <int XT, int DT, bool NORM, int G>
+__global__ __launch_bounds__(ROWS_WAVES_MAX * 64) void rows_fp8_kernel(void* x, size_t ldx, const void* delta, size_t ldd,
+                                                                      const bf16* gain, float eps, int M, int d, int wpr,
+                                                                      uint8_t* __restrict__ q, float* __restrict__ scale) {
+  __shared__ float sums[ROWS_WAVES_MAX * G];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int rpw = (blockDim.x >> 6) / wpr;          // rows of a workgroup
+  const int rw = w / wpr, wr = w % wpr, row = blockIdx.x * rpw + rw;
+  const bool live = row < M;
+  const int chunks = (d + ROWS_CHUNK - 1) / ROWS_CHUNK;
+  float v[G][8];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int col = (g * wpr + wr) * ROWS_CHUNK + lane * 8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[g][i] = 0.f;
+    if (live && col < d) load8<XT>(x, row * ldx + col, v[g]);
+  }
+  if (DT >= 0) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int col = (g * wpr + wr) * ROWS_CHUNK + lane * 8;
+      if (live && col < d) {
+        float a[8];
+        load8<DT>(delta, row * ldd + col, a);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[g][i] += a[i];
+        store8<XT>(x, row * ldx + col, v[g]);
+      }
+    }
+  }
+  if (NORM) {
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int chunk = g * wpr + wr;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[g][i] * v[g][i];
+      s = wave64_sum(s);
+      if (chunk < chunks && lane == 0) sums[rw * chunks + chunk] = s;
+    }
+    __syncthreads();
+    float tot = 0.f;
+    for (int c = 0; c < chunks; ++c) tot += sums[rw * chunks + c];
+    const float inv = 1.0f / sqrtf(tot / (float)d + eps);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int col = (g * wpr + wr) * ROWS_CHUNK + lane * 8;
+      if (col < d) {
+        float b[8];
+        load8<SPEC_BF16>(gain, col, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[g][i] = v[g][i] * inv * b[i];
+      }
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const int col = (g * wpr + wr) * ROWS_CHUNK + lane * 8;
+    const float s = block_scale(v[g]);
+    if (live && col < d) {
+      *reinterpret_cast<uint2*>(q + (size_t)row * d + col) = to_e4m3(v[g], s);
+      if ((lane & 15) == 0) scale[(size_t)(col >> 7) * M + row] = s;
+    }
+  }
+}
+
+template <int XT, int DT, bool NORM>
+static hipError_t launch_rows(void* x, size_t ldx, const void* delta, size_t ldd, const bf16* gain, float eps, int M, int d,
+                              uint8_t* q, float* scale, hipStream_t st) {
+  const int chunks = (d + ROWS_CHUNK - 1) / ROWS_CHUNK;
+  const int G = chunks <= ROWS_WAVES_MAX ? 1 : 4;
+  const int wpr = (chunks + G - 1) / G;
+  const int rpw = wpr >= 4 ? 1 : 4 / wpr;
+  const dim3 grid((M + rpw - 1) / rpw), block(rpw * wpr * 64);
+  if (G == 1) rows_fp8_kernel<XT, DT, NORM, 1><<<grid, block, 0, st>>>(x, ldx, delta, ldd, gain, eps, M, d, wpr, q, scale);
+  else rows_fp8_kernel<XT, DT, NORM, 4><<<grid, block, 0, st>>>(x, ldx, delta, ldd, gain, eps, M, d, wpr, q, scale);
+  return hipGetLastError();
+}
+
+hipError_t launch_add_norm_fp8(void* h, int h_type, size_t ldh, const void* delta, int delta_type, size_t ldd, const bf16* gain,
+                               float eps, int M, int d, uint8_t* q, float* scale, hipStream_t st) {
+#define NORM_CASE(XT, DT) return launch_rows<XT, DT, true>(h, ldh, delta, ldd, gain, eps, M, d, q, scale, st)
+  if (h_type == SPEC_F32) {
+    if (!delta) NORM_CASE(SPEC_F32, -1);
+    if (delta_type == SPEC_F32) NORM_CASE(SPEC_F32, SPEC_F32);
+    NORM_CASE(SPEC_F32, SPEC_BF16);
+  }
+  if (!delta) NORM_CASE(SPEC_BF16, -1);
+  if (delta_type == SPEC_F32) NORM_CASE(SPEC_BF16, SPEC_F32);
+  NORM_CASE(SPEC_BF16, SPEC_BF16);
+#undef NORM_CASE
+}
+hipError_t launch_quant_fp8(const void* x, int x_type, size_t ldx, int M, int K, uint8_t* q, float* scale, hipStream_t st) {
+  void* p = const_cast<void*>(x);                   // only read without a delta
+  if (x_type == SPEC_F32) return launch_rows<SPEC_F32, -1, false>(p, ldx, nullptr, 0, nullptr, 0.f, M, K, q, scale, st);
+  return launch_rows<SPEC_BF16, -1, false>(p, ldx, nullptr, 0, nullptr, 0.f, M, K, q, scale, st);
+}
+
+// ---- weights --------------------------------------------------------------------------------------------------------
+// One workgroup of 256 threads per block of 128 x 128: 16 lanes a row of it, 16 rows at a time.
+__global__ __launch_bounds__(256) void quant_weight_kernel(const bf16* __restrict__ w, int N, int K, uint8_t* __restrict__ q,
+                                                           float* __restrict__ scale) {
+  __shared__ float top[16];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, col = blockIdx.x * 128 + c * 8;
+  float v[8][8], a = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int n = blockIdx.y * 128 + j * 16 + r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
+    if (n < N && col < K) load8<SPEC_BF16>(w, (size_t)n * K + col, v[j]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(v[j][i]));
+  }
+  a = row16_max(a);
+  if (c == 0) top[r] = a;
+  __syncthreads();
+  a = row16_max(top[c]);
+  const float s = fmaxf(a, FP8_LEAST) * (1.0f / E4M3_MAX);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int n = blockIdx.y * 128 + j * 16 + r;
+    if (n < N && col < K) *reinterpret_cast<uint2*>(q + (size_t)n * K + col) = to_e4m3(v[j], s);
+  }
+  if (threadIdx.x == 0) scale[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
+}
+hipError_t launch_quant_weight_fp8(const bf16* w, int N, int K, uint8_t* q, float* scale, hipStream_t st) {
+  quant_weight_kernel<<<dim3((K + 127) / 128, (N + 127) / 128), 256, 0, st>>>(w, N, K, q, scale);
+  return hipGetLastError();
+}
+
+// Packed order: panel p (16 weight rows), block b of 128 columns: 2 KiB, row r at 128 r, its 16-byte piece i at place
+// i ^ (r % 8), zeros behind K.  Copied as it is to LDS, the 16 rows x 4 pieces of half an operand meet no bank twice.  The
+// scales come along per panel, [panel][block], so that matrices can be concatenated and interleaved by panels.
+__global__ __launch_bounds__(128) void pack_weight_fp8_kernel(const uint8_t* __restrict__ src, const float* __restrict__ src_scale,
+                                                              int N, int K, int panel_start, int panel_step,
+                                                              uint8_t* __restrict__ dst, float* __restrict__ dst_scale) {
+  const int b = blockIdx.x, panel = blockIdx.y, KB = gridDim.x;
+  const int r = threadIdx.x >> 3, i = threadIdx.x & 7, k = b * 128 + i * 16;
+  const size_t to = (size_t)(panel_start + panel * panel_step) * KB + b;
+  u32x4 v = {0, 0, 0, 0};
+  typedef __attribute__((ext_vector_type(4), aligned(1))) unsigned u32x4b;
+  if (k < K) v = *reinterpret_cast<const u32x4b*>(src + (size_t)(panel * 16 + r) * K + k);
+  *reinterpret_cast<u32x4*>(dst + to * 2048 + r * 128 + (i ^ (r & 7)) * 16) = v;
+  if (threadIdx.x == 0) dst_scale[to] = src_scale[(size_t)(panel / 8) * KB + b];
+}
+hipError_t launch_pack_weight_fp8(void* dst, float* dst_scale, const void* src, const float* src_scale, int N, int K,
+                                  int panel_start, int panel_step, hipStream_t st) {
+  pack_weight_fp8_kernel<<<dim3((K + 127) / 128, N / 16), 128, 0, st>>>((const uint8_t*)src, src_scale, N, K, panel_start,
+                                                                        panel_step, (uint8_t*)dst, dst_scale);
+  return hipGetLastError();
+}
+
+// ---- products -------------------------------------------------------------------------------------------------------
+// Operand order: lane (c, g) = (lane % 16, lane / 16) holds 32 bytes of row c; which 32 of the block's 128 does not matter as
+// long as both operands agree: the 16-byte pieces g and g + 4.  A result's lane (c, g) holds column c (a token), rows 4 g ..
+// 4 g + 3 (outputs): the scale of a token is one value per lane, that of a panel one per wave.
+//
+// Two ways to the inner sum of a block.  v_mfma_f32_16x16x128_f8f6f4 takes e4m3 as it is, at twice the rate of bf16; but inside
+// each group of 8 products it drops what lies about 2^-14 below the largest of them: 1.5e-5 of the result (2-norm, normal
+// operands), nothing beside a rounding to bf16 (2e-3), too much for an fp32 result.  So fp32 results, and decode-time ones of
+// either type (which wait for the weights anyway), turn e4m3 into bf16 (exact) and use v_mfma_f32_16x16x32_bf16 (1e-8 there).
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+enum { FP8_STORE = 0, FP8_STORE16 = 1, FP8_SWIGLU = 2 };
+
+struct Operand { u32x4 lo, hi; };
+__device__ __forceinline__ f32x4 block_product(const Operand& w, const Operand& x) {
+  const i32x8 a = {(int)w.lo[0], (int)w.lo[1], (int)w.lo[2], (int)w.lo[3], (int)w.hi[0], (int)w.hi[1], (int)w.hi[2], (int)w.hi[3]};
+  const i32x8 b = {(int)x.lo[0], (int)x.lo[1], (int)x.lo[2], (int)x.lo[3], (int)x.hi[0], (int)x.hi[1], (int)x.hi[2], (int)x.hi[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+}
+struct Operand16 { bf16x8 part[4]; };
+__device__ __forceinline__ bf16x8 to_bf16(unsigned a, unsigned b) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
+  return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
+}
+__device__ __forceinline__ Operand16 to_bf16(const Operand& o) {
+  return Operand16{{to_bf16(o.lo[0], o.lo[1]), to_bf16(o.lo[2], o.lo[3]), to_bf16(o.hi[0], o.hi[1]), to_bf16(o.hi[2], o.hi[3])}};
+}
+__device__ __forceinline__ f32x4 block_product(const Operand16& w, const Operand16& x) {
+  f32x4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.part[i], x.part[i], d, 0, 0, 0);
+  return d;
+}
+__device__ __forceinline__ f32x4 scaled_add(f32x4 d, float s, f32x4 acc) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) acc[r] = fmaf(d[r], s, acc[r]);
+  return acc;
+}
+
+template <typename T> __device__ __forceinline__ T as_operand(const Operand& o);
+template <> __device__ __forceinline__ Operand as_operand<Operand>(const Operand& o) { return o; }
+template <> __device__ __forceinline__ Operand16 as_operand<Operand16>(const Operand& o) { return to_bf16(o); }
+
+struct Fp8Args {
+  const uint8_t* x;      // [M][K]
+  const float* xs;       // [KB][M]
+  const uint8_t* w;      // packed
+  const float* ws;       // [NT][KB]
+  void* out;             // STORE: fp32 [M][N];  STORE16: bf16 [M][N];  SWIGLU: bf16 [M][N / 2]
+  int M, N, K, KB, NT;
+};
+
+// outputs 4 g .. 4 g + 3 of a panel (SWIGLU: v, up = the gate and the up panel) for one token
+template <int EPI>
+__device__ __forceinline__ void fp8_store(const Fp8Args& a, int m, int panel, int g, f32x4 v, f32x4 up) {
+  if (EPI == FP8_STORE) {
+    *reinterpret_cast<f32x4*>((float*)a.out + (size_t)m * a.N + panel * 16 + g * 4) = v;
+    return;
+  }
+  bf16 o[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o[r] = __float2bfloat16(EPI == FP8_SWIGLU ? v[r] / (1.0f + __expf(-v[r])) * up[r] : v[r]);
+  const size_t at = EPI == FP8_SWIGLU ? (size_t)m * (a.N / 2) + (panel >> 1) * 16 : (size_t)m * a.N + panel * 16;
+  *reinterpret_cast<uint2*>((bf16*)a.out + at + g * 4) = *reinterpret_cast<const uint2*>(o);
+}
+
+// Up to 32 tokens: bound by the stream of the weights.  A workgroup of 8 waves owns a contiguous range of units (RP panels, SWIGLU:
+// a gate and an up panel); wave w takes its eighth of a unit's blocks of 128, through a ring of D register stages of one block
+// that runs on from unit to unit.  All ring loads are buffer loads whose range check turns "past the end" (blocks, rows, columns)
+// into zeros without traffic: unconditional, so that a stage waits for its own loads only.  The 8 waves' sums are added through
+// LDS in a fixed order: they depend on K alone.
+#define SK_WAVES 8
+#define SK_SKIP 0x7f000000u            // beyond every buffer
+template <int MT, int EPI, int RP, int D>
+__global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny_kernel(Fp8Args a, int per, int rem) {
+  __shared__ f32x4 red[2][SK_WAVES][RP][MT][64];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  const int b = blockIdx.x, u0 = b * per + min(b, rem), u1 = u0 + per + (b < rem ? 1 : 0);
+  const int s0 = w * a.KB / SK_WAVES, ns = (w + 1) * a.KB / SK_WAVES - s0;
+  const int rounds = ns > D ? (ns + D - 1) / D : 1;
+  const unsigned pbytes = (unsigned)a.KB * 2048u;
+  const __amdgpu_buffer_rsrc_t xr =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x), 0, (unsigned)a.M * (unsigned)a.K, 0x00020000);
+  const __amdgpu_buffer_rsrc_t sr =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.xs), 0, (unsigned)a.KB * (unsigned)a.M * 4u, 0x00020000);
+  const unsigned wlo = c * 128 + (g ^ (c & 7)) * 16, whi = wlo ^ 64;
+  unsigned xoff[MT], soff[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int m = t * 16 + c;
+    xoff[t] = m < a.M ? (unsigned)m * (unsigned)a.K + g * 16 : SK_SKIP;
+    soff[t] = m < a.M ? m * 4u : SK_SKIP;
+  }
+  Operand wq[D][RP], xq[D][MT];
+  float xs[D][MT], ws[D][RP];
+  typedef const __attribute__((address_space(4))) float* scalar_floats;
+  // stage s: block r * D + s of the wave's share of unit u.  What is not there is skipped by the lanes' offsets; the scalar ones
+  // stay inside the buffers (a range check subtracts them from the size).
+  auto load = [&](int s, int u, int r) {
+    const int i = r * D + s, blk = min(s0 + i, a.KB - 1);
+    const bool on = i < ns && u < u1;
+#pragma unroll
+    for (int p = 0; p < RP; ++p) {
+      const int panel = min(u * RP + p, a.NT - 1);
+      const unsigned skip = on && u * RP + p < a.NT ? 0u : SK_SKIP;
+      const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint8_t*>(a.w) + (size_t)panel * pbytes, 0, pbytes, 0x00020000);
+      wq[s][p].lo = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, skip | wlo, blk * 2048, 2));
+      wq[s][p].hi = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, skip | whi, blk * 2048, 2));
+      ws[s][p] = ((scalar_floats)a.ws)[(size_t)panel * a.KB + blk];
+    }
+    const unsigned skip = on ? 0u : SK_SKIP;
+    const int left = a.K - blk * 128 - g * 16;       // columns behind this lane's first one
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const unsigned at = skip | xoff[t];
+      xq[s][t].lo = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, left > 0 ? at : SK_SKIP, blk * 128, 0));
+      xq[s][t].hi = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, left > 64 ? at + 64 : SK_SKIP, blk * 128, 0));
+      xs[s][t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, skip | soff[t], blk * a.M * 4, 0));
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < D; ++s) load(s, u0, 0);
+  f32x4 acc[RP][MT];
+#pragma unroll
+  for (int p = 0; p < RP; ++p)
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int buf = 0;
+#pragma unroll 1
+  for (int u = u0, r = 0; u < u1;) {
+    const bool last = r + 1 == rounds;
+    const int nu = last ? u + 1 : u, nr = last ? 0 : r + 1;
+#pragma unroll
+    for (int s = 0; s < D; ++s) {
+      Operand16 x16[MT];
+#pragma unroll
+      for (int t = 0; t < MT; ++t) x16[t] = to_bf16(xq[s][t]);
+#pragma unroll
+      for (int p = 0; p < RP; ++p) {
+        const Operand16 w16 = to_bf16(wq[s][p]);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[p][t] = scaled_add(block_product(w16, x16[t]), xs[s][t] * ws[s][p], acc[p][t]);
+      }
+      load(s, nu, nr);
+      __builtin_amdgcn_sched_barrier(0);              // stage by stage: the ring holds most registers
+    }
+    if (last) {
+#pragma unroll
+      for (int p = 0; p < RP; ++p)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          red[buf][w][p][t][lane] = acc[p][t];
+          acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      // two buffers: nobody writes this one again before everybody has passed the next unit's barrier
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      constexpr int JOBS = EPI == FP8_SWIGLU ? MT : RP * MT;       // a wave adds and stores one tile (SWIGLU: a pair)
+      const int job = (w + u) & (SK_WAVES - 1);
+      if (job < JOBS) {
+        const int t = job % MT, p0 = EPI == FP8_SWIGLU ? 0 : job / MT, m = t * 16 + c;
+        f32x4 sum[2];
+#pragma unroll
+        for (int q = 0; q < (EPI == FP8_SWIGLU ? 2 : 1); ++q) {
+          f32x4 e[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] = red[buf][2 * i][p0 + q][t][lane] + red[buf][2 * i + 1][p0 + q][t][lane];
+          sum[q] = (e[0] + e[1]) + (e[2] + e[3]);
+        }
+        if (m < a.M && u * RP + p0 < a.NT) fp8_store<EPI>(a, m, u * RP + p0, g, sum[0], sum[EPI == FP8_SWIGLU ? 1 : 0]);
+      }
+      buf ^= 1;
+    }
+    u = nu, r = nr;
+  }
+}
+
+// From 33 tokens on: BMT token tiles x BNP panels per workgroup of WM x WN waves, a block of 128 columns per stage, ST stages.
+// Both operands, and their scales, go global -> LDS without a stop in registers: rows of x as 128 bytes, piece i of row r at
+// place i ^ (r % 8), as the weights are packed.  The loads are inline asm (they write no register), so that the compiler, which
+// would wait for all of them before any LDS read, leaves the waiting to the explicit counts; everything else is ordinary code.
+// Buffer range checks turn rows behind M, panels behind NT and columns behind K into zeros.
+#define DMA_SKIP 0x7f000000u          // beyond every buffer
+__device__ __forceinline__ u32x4 dma_rsrc(const void* base, unsigned bytes) {
+  const uint64_t p = (uint64_t)base;
+  return u32x4{(unsigned)p, (unsigned)(p >> 32) & 0xffffu, bytes, 0x00020000u};
+}
+__device__ __forceinline__ void dma16(unsigned lds, u32x4 rsrc, unsigned voff, unsigned soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               ::"s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+}
+__device__ __forceinline__ void dma4(unsigned lds, u32x4 rsrc, unsigned voff, unsigned soff) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               ::"s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+}
+
+template <int BMT, int BNP, int WM, int WN, int ST>
+struct DenseShape {
+  static constexpr int WAVES = WM * WN, MT = BMT / WM, NP = BNP / WN;
+  static constexpr int XB = BMT * 2048, WB = BNP * 2048, SB = 2048;   // a stage: rows, panels, scales (of tokens, then of panels)
+  static constexpr int STAGE = XB + WB + SB, BYTES = ST * STAGE;
+  static constexpr int JOBS = (BMT + BNP) * 2 / WAVES + 1;            // loads of a wave per stage: operands, one of scales
+  static_assert((BMT + BNP) * 2 % WAVES == 0 && BMT * 2 % WAVES == 0, "even shares");
+  static_assert(BMT / 4 + 1 <= WAVES && BMT * 64 + BNP * 4 <= SB && BNP <= 64, "a load of scales per wave");
+};
+
+template <int EPI, int BMT, int BNP, int WM, int WN, int ST>
+__global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int TM, int TN, int chunk, int slice) {
+  typedef DenseShape<BMT, BNP, WM, WN, ST> S;
+  extern __shared__ u32x4 fp8_lds[];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  // XCD x (workgroups are dealt round-robin) takes the tiles [x chunk, (x + 1) chunk), row-major in groups of 4 columns
+  const int j = blockIdx.x >> 3, tile = (blockIdx.x & 7) * chunk + j;
+  if (j >= chunk || tile >= TM * TN) return;
+  const int grp = tile / (TM * 4), idx = tile % (TM * 4), gw = min(4, TN - grp * 4);
+  const int tm = idx / gw, tn = grp * 4 + idx % gw;
+  const int b0 = blockIdx.y * slice, nb = min(slice, a.KB - b0);
+  const int m0 = tm * BMT * 16, p0 = tn * BNP;
+  const int rows = min(BMT * 16, a.M - m0), panels = min(BNP, a.NT - p0);
+  const u32x4 xr = dma_rsrc(a.x + (size_t)m0 * a.K, (unsigned)rows * (unsigned)a.K);
+  const u32x4 wr = dma_rsrc(a.w + (size_t)p0 * a.KB * 2048, (unsigned)panels * (unsigned)a.KB * 2048u);
+  const u32x4 sxr = dma_rsrc(a.xs + m0, (unsigned)((a.KB - 1) * (size_t)a.M + rows) * 4u);
+  const u32x4 swr = dma_rsrc(a.ws + (size_t)p0 * a.KB, (unsigned)panels * (unsigned)a.KB * 4u);
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) u32x4*)fp8_lds;
+  constexpr int XJ = BMT * 2 / S::WAVES, WJ = BNP * 2 / S::WAVES;
+  // x: job i covers rows 8 i .. 8 i + 7, lane l row l / 8, place l % 8
+  unsigned xoff[XJ], woff[WJ], soff;
+  const int xpiece = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+  for (int i = 0; i < XJ; ++i) {
+    const int r = (w * XJ + i) * 8 + (lane >> 3);
+    xoff[i] = r < rows ? (unsigned)r * (unsigned)a.K + xpiece * 16 : DMA_SKIP;
+  }
+#pragma unroll
+  for (int i = 0; i < WJ; ++i) {
+    const int job = w * WJ + i;
+    woff[i] = (unsigned)(job >> 1) * (unsigned)a.KB * 2048u + (job & 1) * 1024 + lane * 16;
+  }
+  const bool tokens = w < BMT / 4;              // this wave's load of scales: of 64 tokens, or of the panels
+  soff = tokens ? (w * 64 + lane < rows ? (w * 64 + lane) * 4u : DMA_SKIP)
+                : (lane < panels ? (unsigned)lane * (unsigned)a.KB * 4u : DMA_SKIP);
+  const bool tail = (a.K & 127) != 0;
+  auto issue = [&](int i, int slot) {           // block b0 + i
+    const unsigned b = b0 + i, base = lds0 + slot * S::STAGE;
+    const bool cut = tail && (int)b == a.KB - 1 && (int)(b * 128) + xpiece * 16 >= a.K;
+#pragma unroll
+    for (int q = 0; q < XJ; ++q) dma16(base + (w * XJ + q) * 1024, xr, cut ? DMA_SKIP : xoff[q], b * 128);
+#pragma unroll
+    for (int q = 0; q < WJ; ++q) dma16(base + S::XB + (w * WJ + q) * 1024, wr, woff[q], b * 2048);
+    if (tokens) dma4(base + S::XB + S::WB + w * 256, sxr, soff, b * (unsigned)a.M * 4u);
+    else dma4(base + S::XB + S::WB + BMT * 64, swr, soff, b * 4);
+  };
+  const int wm = w / WN, wn = w % WN;
+  f32x4 acc[S::NP][S::MT];
+#pragma unroll
+  for (int p = 0; p < S::NP; ++p)
+#pragma unroll
+    for (int t = 0; t < S::MT; ++t) acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < ST - 1; ++s)
+    if (s < nb) issue(s, s);
+  int slot = 0, next = ST - 1;
+  for (int i = 0; i < nb; ++i) {
+    // this wave's loads of block i have landed, then everybody's; everybody is past reading the slot that is filled next
+    if (i + ST - 1 <= nb) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 2) * S::JOBS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    if (i + ST - 1 < nb) issue(i + ST - 1, next);
+    const u32x4* xl = fp8_lds + slot * (S::STAGE / 16) + wm * S::MT * 128 + c * 8;
+    const u32x4* wl = fp8_lds + slot * (S::STAGE / 16) + S::XB / 16 + wn * S::NP * 128 + c * 8;
+    const float* sl = reinterpret_cast<const float*>(fp8_lds + slot * (S::STAGE / 16) + (S::XB + S::WB) / 16);
+    const int lo = g ^ (c & 7), hi = lo ^ 4;
+    typedef typename std::conditional<EPI == FP8_STORE, Operand16, Operand>::type Op;
+    Op xf[S::MT];
+    float xs[S::MT];
+#pragma unroll
+    for (int t = 0; t < S::MT; ++t) {
+      xf[t] = as_operand<Op>(Operand{xl[t * 128 + lo], xl[t * 128 + hi]});
+      xs[t] = sl[(wm * S::MT + t) * 16 + c];
+    }
+#pragma unroll
+    for (int p = 0; p < S::NP; ++p) {
+      const Op wf = as_operand<Op>(Operand{wl[p * 128 + lo], wl[p * 128 + hi]});
+      const float ws = sl[BMT * 16 + wn * S::NP + p];
+#pragma unroll
+      for (int t = 0; t < S::MT; ++t) acc[p][t] = scaled_add(block_product(wf, xf[t]), xs[t] * ws, acc[p][t]);
+    }
+    // its LDS reads are done before this wave meets the next barrier
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    slot = slot + 1 == ST ? 0 : slot + 1;
+    next = next + 1 == ST ? 0 : next + 1;
+  }
+#pragma unroll
+  for (int t = 0; t < S::MT; ++t) {
+    const int m = m0 + (wm * S::MT + t) * 16 + c;
+    if (m >= a.M) continue;
+#pragma unroll
+    for (int p = 0; p < S::NP; p += 2) {
+      const int panel = p0 + wn * S::NP + p;
+      if (EPI == FP8_SWIGLU) {
+        if (panel + 1 < a.NT) fp8_store<EPI>(a, m, panel, g, acc[p][t], acc[p + 1][t]);
+      } else {
+        if (panel < a.NT) fp8_store<EPI>(a, m, panel, g, acc[p][t], acc[p][t]);
+        if (panel + 1 < a.NT) fp8_store<EPI>(a, m, panel + 1, g, acc[p + 1][t], acc[p + 1][t]);
+      }
+    }
+  }
+}
+
+template <int EPI, int BMT, int BNP, int WM, int WN, int ST>
+static hipError_t launch_dense(const Fp8Args& a, int slices, hipStream_t st) {
+  typedef DenseShape<BMT, BNP, WM, WN, ST> S;
+  const int TM = (a.M + BMT * 16 - 1) / (BMT * 16), TN = (a.NT + BNP - 1) / BNP, chunk = (TM * TN + 7) / 8;
+  const int slice = (a.KB + slices - 1) / slices;
+  auto kernel = fp8_dense_kernel<EPI, BMT, BNP, WM, WN, ST>;
+  static const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
+  if (attr != hipSuccess) return attr;
+  kernel<<<dim3(chunk * 8, slices), S::WAVES * 64, S::BYTES, st>>>(a, TM, TN, chunk, slice);
+  return hipGetLastError();
+}
+
+template <int EPI>
+static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
+  constexpr int RP = EPI == FP8_SWIGLU ? 2 : 1;
+  const int units = (a.NT + RP - 1) / RP, G = min(units, 2 * spec_num_cu()), per = units / G, rem = units % G;
+  if (a.M <= 16) fp8_skinny_kernel<1, EPI, RP, RP == 2 ? 2 : 4><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
+  else fp8_skinny_kernel<2, EPI, RP, 2><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
+  return hipGetLastError();
+}
+template <int EPI>
+static hipError_t launch_fp8(const Fp8Args& a, hipStream_t st) {
+  if (a.M <= 32) return launch_skinny<EPI>(a, st);
+  if (a.M <= 512 || EPI == FP8_STORE) return launch_dense<EPI, 8, 8, 4, 2, 3>(a, 1, st);
+  return launch_dense<EPI, 16, 16, 4, 2, 2>(a, 1, st);
+}
+hipError_t launch_gemm_fp8(const uint8_t* x, const float* xs, const void* w, const float* ws, int M, int N, int K, int swiglu,
+                           void* out, int out_type, hipStream_t st) {
+  const Fp8Args a = {x, xs, (const uint8_t*)w, ws, out, M, N, K, (K + 127) / 128, N / 16};
+  if (swiglu) return launch_fp8<FP8_SWIGLU>(a, st);
+  if (out_type == SPEC_F32) return launch_fp8<FP8_STORE>(a, st);
+  return launch_fp8<FP8_STORE16>(a, st);
+}

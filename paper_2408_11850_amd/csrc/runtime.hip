@@ -1435,6 +1435,82 @@ extern "C" int spec_dense_gemm(float* y, void* z, const void* x, const void* w, 
   return SPEC_OK;
 }
 
+// ---- 8-bit operands
+static bool fp8_type(int t) { return t == SPEC_F32 || t == SPEC_BF16; }
+static bool off_by(const void* p, size_t bytes) { return (uintptr_t)p % bytes != 0; }
+static bool off_element(const void* p, int type) { return off_by(p, type == SPEC_F32 ? 4 : 2); }
+
+static int check_fp8_rows(int M, int d) {
+  if (M < 1 || d < 16 || d % 16 || d > SPEC_FP8_ROW_MAX)
+    FAIL(SPEC_E_INVAL, "need M >= 1 and rows of 16 to %d columns, a multiple of 16", SPEC_FP8_ROW_MAX);
+  return SPEC_OK;
+}
+extern "C" int spec_add_norm_quant(void* h, int h_type, long long ldh, const void* delta, int delta_type, long long ldd,
+                                 const void* gain, float eps, int M, int d, void* q, float* scale, void* stream) {
+  if (!h || !gain || !q || !scale) FAIL(SPEC_E_INVAL, "null pointer");
+  if (!fp8_type(h_type) || (delta && !fp8_type(delta_type))) FAIL(SPEC_E_INVAL, "types are SPEC_F32 and SPEC_BF16");
+  int rc = check_fp8_rows(M, d);
+  if (rc) return rc;
+  if (ldh < d || (delta && ldd != 0 && ldd < d)) FAIL(SPEC_E_INVAL, "row stride below the row");
+  if (!(eps > 0.0f) || eps == INFINITY) FAIL(SPEC_E_INVAL, "eps must be positive");
+  if (off_element(h, h_type) || (delta && off_element(delta, delta_type)) || off_by(gain, 2) || off_by(q, 8) || off_by(scale, 4))
+    FAIL(SPEC_E_INVAL, "misaligned operand");
+  HIPCHK(launch_add_norm_fp8(h, h_type, (size_t)ldh, delta, delta_type, (size_t)ldd, (const bf16*)gain, eps, M, d, (uint8_t*)q,
+                             scale, (hipStream_t)stream));
+  return SPEC_OK;
+}
+extern "C" int spec_quant_rows(const void* x, int x_type, long long ldx, int M, int K, void* q, float* scale, void* stream) {
+  if (!x || !q || !scale) FAIL(SPEC_E_INVAL, "null pointer");
+  if (!fp8_type(x_type)) FAIL(SPEC_E_INVAL, "types are SPEC_F32 and SPEC_BF16");
+  int rc = check_fp8_rows(M, K);
+  if (rc) return rc;
+  if (ldx != 0 && ldx < K) FAIL(SPEC_E_INVAL, "row stride below the row");
+  if (off_element(x, x_type) || off_by(q, 8) || off_by(scale, 4)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  HIPCHK(launch_quant_fp8(x, x_type, (size_t)ldx, M, K, (uint8_t*)q, scale, (hipStream_t)stream));
+  return SPEC_OK;
+}
+static int check_fp8_matrix(int N, int K) {
+  if (N < 16 || N % 16 || N > SPEC_FP8_K_MAX || K < 16 || K % 16 || K > SPEC_FP8_K_MAX)
+    FAIL(SPEC_E_INVAL, "need N %% 16 == 0 and K %% 16 == 0, both at most %d", SPEC_FP8_K_MAX);
+  return SPEC_OK;
+}
+extern "C" int spec_quant_weight(const void* w, int N, int K, void* q, float* scale, void* stream) {
+  if (!w || !q || !scale) FAIL(SPEC_E_INVAL, "null pointer");
+  int rc = check_fp8_matrix(N, K);
+  if (rc) return rc;
+  if (off_by(w, 2) || off_by(q, 8) || off_by(scale, 4)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  HIPCHK(launch_quant_weight_fp8((const bf16*)w, N, K, (uint8_t*)q, scale, (hipStream_t)stream));
+  return SPEC_OK;
+}
+extern "C" size_t spec_packed_quant_bytes(int N, int K) {
+  return check_fp8_matrix(N, K) ? 0 : (size_t)(N / 16) * ((K + 127) / 128) * 2048;
+}
+extern "C" int spec_pack_quant(void* dst, float* dst_scale, const void* src, const float* src_scale, int N, int K,
+                                    int panel_start, int panel_step, void* stream) {
+  if (!dst || !dst_scale || !src || !src_scale) FAIL(SPEC_E_INVAL, "null pointer");
+  int rc = check_fp8_matrix(N, K);
+  if (rc) return rc;
+  if (panel_start < 0 || panel_step < 1) FAIL(SPEC_E_INVAL, "bad panel range");
+  if (off_by(dst, 16) || off_by(dst_scale, 4) || off_by(src_scale, 4)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  HIPCHK(launch_pack_weight_fp8(dst, dst_scale, src, src_scale, N, K, panel_start, panel_step, (hipStream_t)stream));
+  return SPEC_OK;
+}
+extern "C" int spec_gemm_quant(void* out, int out_type, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                               int M, int N, int K, int epilogue, void* stream) {
+  if (!out || !x || !x_scale || !w || !w_scale) FAIL(SPEC_E_INVAL, "null pointer");
+  if (epilogue != 0 && epilogue != 2) FAIL(SPEC_E_INVAL, "epilogue must be 0 or 2");
+  if (!fp8_type(out_type) || (epilogue == 2 && out_type != SPEC_BF16))
+    FAIL(SPEC_E_INVAL, "results are SPEC_F32 or SPEC_BF16, of epilogue 2 SPEC_BF16");
+  int rc = check_fp8_matrix(N, K);
+  if (rc) return rc;
+  if (epilogue == 2 && N % 32) FAIL(SPEC_E_INVAL, "epilogue 2 needs N %% 32 == 0");
+  if (M < 1 || (size_t)M * ((K + 127) / 128) > (1u << 28)) FAIL(SPEC_E_INVAL, "need 1 <= M and at most 2^28 scales of x");
+  if (off_by(x, 16) || off_by(w, 16) || off_by(x_scale, 4) || off_by(w_scale, 4) || off_by(out, out_type == SPEC_F32 ? 16 : 8))
+    FAIL(SPEC_E_INVAL, "misaligned operand");
+  HIPCHK(launch_gemm_fp8((const uint8_t*)x, x_scale, w, w_scale, M, N, K, epilogue == 2, out, out_type, (hipStream_t)stream));
+  return SPEC_OK;
+}
+
 extern "C" int spec_read_probe(const void* src, size_t bytes, void* out, void* stream) {
   if (!src || !out || bytes < 16) FAIL(SPEC_E_INVAL, "bad argument");
   HIPCHK(launch_read_probe(src, bytes, out, (hipStream_t)stream));

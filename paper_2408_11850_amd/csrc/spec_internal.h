@@ -193,6 +193,16 @@ hipError_t launch_dense_qkv_rope(const bf16* x, const void* wp, int M, int K, bf
 hipError_t launch_prefill_attention(const bf16* q, const bf16* pool, const int* block_table, const int* len_ptr,
                                     KvGeom g, int layer, int M, int Hq, bf16* out, hipStream_t st);
 
+// 8-bit operands (fp8.hip); types are SPEC_F32 / SPEC_BF16, scales as in spec.h
+hipError_t launch_add_norm_fp8(void* h, int h_type, size_t ldh, const void* delta, int delta_type, size_t ldd, const bf16* gain,
+                               float eps, int M, int d, uint8_t* q, float* scale, hipStream_t st);
+hipError_t launch_quant_fp8(const void* x, int x_type, size_t ldx, int M, int K, uint8_t* q, float* scale, hipStream_t st);
+hipError_t launch_quant_weight_fp8(const bf16* w, int N, int K, uint8_t* q, float* scale, hipStream_t st);
+hipError_t launch_pack_weight_fp8(void* dst, float* dst_scale, const void* src, const float* src_scale, int N, int K,
+                                  int panel_start, int panel_step, hipStream_t st);
+hipError_t launch_gemm_fp8(const uint8_t* x, const float* xs, const void* w, const float* ws, int M, int N, int K, int swiglu,
+                           void* out, int out_type, hipStream_t st);
+
 // sampling / acceptance
 struct AcceptArgs {
   int kind;                 // SPEC_ACCEPT_*

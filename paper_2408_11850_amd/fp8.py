@@ -1,0 +1,155 @@
+"""8-bit operands: rows and weights in e4m3 with a scale per block of 128, and their products (see include/spec.h).
+
+Argument marshalling only.  Every call runs on the current stream of the tensors' device; the results are that device's.
+"""
+from __future__ import annotations
+
+from typing import List, Optional, Tuple
+
+import torch
+
+from . import EPI_STORE, EPI_SWIGLU, FP8_BLOCK, SPEC_BF16, SPEC_F32, check, load_library
+
+_TYPES = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16}
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+E4M3 = torch.float8_e4m3fn
+
+
+class _On:
+    """The device of a call's tensors as the current one, and its stream.  Entering a device that is current costs a query."""
+
+    __slots__ = ("index", "before")
+
+    def __init__(self, index: int):
+        self.index = index
+
+    def __enter__(self) -> int:
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+        return _raw_stream(self.index) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def _blocks(k: int) -> int:
+    return -(-k // FP8_BLOCK)
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows(x: torch.Tensor, name: str) -> int:
+    """Row stride of a matrix of rows in fp32 or bf16."""
+    _need(x.is_cuda and x.dim() == 2 and x.dtype in _TYPES, f"{name}: rows in float32 or bfloat16 on a GPU are wanted")
+    _need(x.shape[1] == 1 or x.stride(1) == 1, f"{name}: the elements of a row must be neighbours")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def add_norm_fp8(h: torch.Tensor, delta: Optional[torch.Tensor], gain: torch.Tensor,
+                 eps: float) -> Tuple[torch.Tensor, torch.Tensor]:
+    """h += delta in place (None: nothing is added), then (q, scale) of the RMS norm of h times gain.
+
+    h [M][d] and delta [M][d] fp32 or bf16, rows at any stride (delta's may be 0: the same row for all); gain bf16 [d].
+    q e4m3 [M][d], scale fp32 [ceil(d / 128)][M]."""
+    ldh = _rows(h, "h")
+    M, d = h.shape
+    _need(gain.dtype == torch.bfloat16 and gain.device == h.device and tuple(gain.shape) == (d,) and gain.is_contiguous(),
+          "gain: bfloat16 [d] on the device of h is wanted")
+    ldd = 0
+    if delta is not None:
+        ldd = _rows(delta, "delta")
+        _need(delta.device == h.device and delta.shape == h.shape, "delta: the shape and device of h are wanted")
+    lib = load_library()
+    q = torch.empty((M, d), dtype=E4M3, device=h.device)
+    scale = torch.empty((_blocks(d), M), dtype=torch.float32, device=h.device)
+    with _On(h.device.index) as st:
+        check(lib.spec_add_norm_quant(h.data_ptr(), _TYPES[h.dtype], ldh, delta.data_ptr() if delta is not None else None,
+                                    _TYPES[delta.dtype] if delta is not None else 0, ldd, gain.data_ptr(), eps, M, d,
+                                    q.data_ptr(), scale.data_ptr(), st))
+    return q, scale
+
+
+def quant_fp8(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(q, scale) of rows x [M][K] in fp32 or bf16 at any row stride: q e4m3 [M][K], scale fp32 [ceil(K / 128)][M]."""
+    ldx = _rows(x, "x")
+    M, K = x.shape
+    lib = load_library()
+    q = torch.empty((M, K), dtype=E4M3, device=x.device)
+    scale = torch.empty((_blocks(K), M), dtype=torch.float32, device=x.device)
+    with _On(x.device.index) as st:
+        check(lib.spec_quant_rows(x.data_ptr(), _TYPES[x.dtype], ldx, M, K, q.data_ptr(), scale.data_ptr(), st))
+    return q, scale
+
+
+def quant_weight_fp8(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(q, scale) of a bf16 matrix [N][K]: q e4m3 [N][K], scale fp32 [ceil(N / 128)][ceil(K / 128)]."""
+    _need(w.is_cuda and w.dim() == 2 and w.dtype == torch.bfloat16 and w.is_contiguous(),
+          "w: a contiguous bfloat16 matrix on a GPU is wanted")
+    N, K = w.shape
+    lib = load_library()
+    q = torch.empty((N, K), dtype=E4M3, device=w.device)
+    scale = torch.empty((_blocks(N), _blocks(K)), dtype=torch.float32, device=w.device)
+    with _On(w.device.index) as st:
+        check(lib.spec_quant_weight(w.data_ptr(), N, K, q.data_ptr(), scale.data_ptr(), st))
+    return q, scale
+
+
+class Fp8Weight:
+    """Packed e4m3 weights [N][K] and the scales of their panels."""
+
+    __slots__ = ("data", "scale", "N", "K", "interleaved")
+
+    def __init__(self, data: torch.Tensor, scale: torch.Tensor, N: int, K: int, interleaved: bool):
+        self.data, self.scale, self.N, self.K, self.interleaved = data, scale, N, K, interleaved
+
+
+def pack_weights_fp8(mats: List[Tuple[torch.Tensor, torch.Tensor]], interleave: bool = False) -> Fp8Weight:
+    """Packs e4m3 matrices [N_i][K] with scales [ceil(N_i / 128)][ceil(K / 128)] one behind the other, or (gate and up) with
+    their panels of 16 rows interleaved."""
+    _need(len(mats) > 0, "no matrices")
+    K, device = mats[0][0].shape[1], mats[0][0].device
+    for q, s in mats:
+        _need(q.is_cuda and q.dim() == 2 and q.dtype == E4M3 and q.is_contiguous() and q.shape[1] == K and q.device == device,
+              "e4m3 matrices of one width on one GPU are wanted")
+        _need(s.dtype == torch.float32 and s.is_contiguous() and s.device == device and
+              tuple(s.shape) == (_blocks(q.shape[0]), _blocks(K)), "scales: float32 [ceil(N / 128)][ceil(K / 128)] are wanted")
+        _need(not interleave or q.shape == mats[0][0].shape, "only matrices of one shape can be interleaved")
+    lib = load_library()
+    N = sum(q.shape[0] for q, _ in mats)
+    _need(all(lib.spec_packed_quant_bytes(q.shape[0], K) > 0 for q, _ in mats), "need N % 16 == 0 and K % 16 == 0")
+    data = torch.empty(sum(lib.spec_packed_quant_bytes(q.shape[0], K) for q, _ in mats), dtype=torch.uint8, device=device)
+    scale = torch.empty((N // 16, _blocks(K)), dtype=torch.float32, device=device)
+    with _On(device.index) as st:
+        start = 0
+        for i, (q, s) in enumerate(mats):
+            check(lib.spec_pack_quant(data.data_ptr(), scale.data_ptr(), q.data_ptr(), s.data_ptr(), q.shape[0], K,
+                                           i if interleave else start, len(mats) if interleave else 1, st))
+            start += q.shape[0] // 16
+    return Fp8Weight(data, scale, N, K, interleave and len(mats) == 2)
+
+
+def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: Fp8Weight, epilogue: int = EPI_STORE,
+             dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """x W^T of e4m3 rows [M][K] with scales [ceil(K / 128)][M].
+
+    epilogue 0: returns y [M][N] in bfloat16 or float32; 2: z [M][N / 2] bf16 = silu(gate) * up of weights packed with
+    interleave=True."""
+    M, K = x.shape
+    dev, N = x.device, w.N
+    _need(x.is_cuda and x.dtype == E4M3 and x.is_contiguous() and K == w.K and w.data.device == dev,
+          "x: contiguous e4m3 rows of the weights' width on their device are wanted")
+    _need(x_scale.dtype == torch.float32 and x_scale.is_contiguous() and x_scale.device == dev and
+          tuple(x_scale.shape) == (_blocks(K), M), "x_scale: float32 [ceil(K / 128)][M] is wanted")
+    _need(dtype in _TYPES, "results in bfloat16 or float32")
+    _need(epilogue != EPI_SWIGLU or w.interleaved, "epilogue 2 wants a gate and an up matrix packed with interleave=True")
+    lib = load_library()
+    out = torch.empty((M, N // 2 if epilogue == EPI_SWIGLU else N), dtype=dtype, device=dev)
+    with _On(dev.index) as st:
+        check(lib.spec_gemm_quant(out.data_ptr(), _TYPES[dtype], x.data_ptr(), x_scale.data_ptr(), w.data.data_ptr(),
+                                  w.scale.data_ptr(), M, N, K, epilogue, st))
+    return out
