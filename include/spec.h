@@ -305,6 +305,32 @@ int spec_read_probe(const void* src_dev, size_t bytes, void* out_dev, void* stre
 int spec_sample_row(const float* logits_dev, int vocab, float temperature, float logit_scale, float u,
                     float* q_out_dev, int32_t* tok_out_dev, void* stream);
 
+/* Draws under temperature, top-k, top-p and min-p, for n_rows rows of fp32 logits (device, row stride ld >= vocab).  With
+ * z = logit * logit_scale / temperature and w = exp(z - max z), ids in the order of falling logits (equal ones by rising id): of
+ * the first top_k (0, or vocab and more: all) the shortest prefix that holds at least top_p of their mass (1: all; at least
+ * one id), and of that the ids with w >= min_p (0: all) are kept.  temperature 0: the lowest id of the largest logit.
+ *   q_out[n_rows][vocab]       w / (sum of w) over what is kept, else 0: rows for spec_accept_rows
+ *   masked_out[n_rows][vocab]  the logit of a kept id, else -inf: what spec_accept_rows takes as p_logits, with the same
+ *                              temperature and logit_scale, for the target to be truncated as the draft model is
+ *   tok_out[n_rows]            the first id at which the sum of q passes u_dev[row] (below 0 and NaN as 0, from 1 on the last id)
+ * each of them may be NULL, but not all; u_dev only matters for tok_out at a temperature.  q_out or masked_out may be the
+ * logits (ld == vocab).  A row without a finite logit, or with a NaN or +inf, has no distribution: NaN and token -1 (at
+ * temperature 0 a NaN counts as none, and a row without any logit above -inf gives id 0).  Borders and draws are decided in 64
+ * bits, the results do not depend on the order in which anything runs.  temperature >= 0, logit_scale > 0, both finite,
+ * top_k >= 0, top_p and min_p in [0, 1], n_rows <= 65535, vocab <= SPEC_SAMPLE_VOCAB_MAX.  work_dev: 16-byte aligned device
+ * memory of spec_sample_rows_workspace_bytes(n_rows, vocab), for this call alone until it has run; nothing in it need be set.
+ * Allocates nothing, can be captured; asynchronous on `stream`. */
+typedef struct {
+  float temperature, logit_scale;
+  int top_k;
+  float top_p, min_p;
+} spec_sampling;
+#define SPEC_SAMPLE_VOCAB_MAX 1048576
+int spec_sample_rows(const float* logits_dev, long long ld, int n_rows, int vocab, const spec_sampling* sampling,
+                     const float* u_dev, float* q_out_dev, float* masked_out_dev, int32_t* tok_out_dev, void* work_dev,
+                     void* stream);
+size_t spec_sample_rows_workspace_bytes(int n_rows, int vocab);
+
 /* Acceptance on caller-provided rows (device): p_logits [n_rows][vocab] fp32 logits of the
  * target, q_rows [n_test][vocab] distributions, x_dev[n_test] draft tokens, r_host[n_test].
  * If n_rows == n_test + 1 and all are accepted a bonus token is drawn from the last row.

@@ -52,6 +52,11 @@ class Config(C.Structure):
                 ("stream_target", C.c_void_p), ("stream_draft", C.c_void_p)]
 
 
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("logit_scale", C.c_float), ("top_k", C.c_int), ("top_p", C.c_float),
+                ("min_p", C.c_float)]
+
+
 # name -> (restype, argtypes); every symbol include/spec.h declares
 _P = C.c_void_p
 _PI = C.POINTER(C.c_int)
@@ -96,6 +101,8 @@ SIGNATURES = {
     "spec_gemm_quant": (C.c_int, [_P, C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_int, C.c_int, _P]),
     "spec_read_probe": (C.c_int, [_P, C.c_size_t, _P, _P]),
     "spec_sample_row": (C.c_int, [_P, C.c_int, C.c_float, C.c_float, C.c_float, _P, _P, _P]),
+    "spec_sample_rows": (C.c_int, [_P, C.c_longlong, C.c_int, C.c_int, C.POINTER(Sampling), _P, _P, _P, _P, _P, _P]),
+    "spec_sample_rows_workspace_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "spec_accept_rows": (C.c_int, [_P, C.c_int, _P, _P, C.c_int, C.c_int, C.c_float, C.c_float, _PF, C.c_float,
                                    _PI32, _P]),
     "spec_accept_rows_static": (C.c_int, [_P, C.c_int, _P, _P, C.c_int, C.c_int, C.c_float, C.c_float, _PF, C.c_float,
@@ -138,4 +145,5 @@ def check(rc: int) -> int:
 
 
 from .binding import SpecContext, pack_model, gemm, dense_gemm, sample_row, accept_rows, accept_rows_static, read_probe  # noqa: E402,F401
+from .draws import filter_rows, sample_rows  # noqa: E402,F401
 from .fp8 import Fp8Weight, add_norm_fp8, gemm_fp8, pack_weights_fp8, quant_fp8, quant_weight_fp8  # noqa: E402,F401

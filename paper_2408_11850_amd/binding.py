@@ -31,6 +31,31 @@ def _current_stream_ptr() -> int:
     return _raw_stream(torch.cuda.current_device()) if _raw_stream else _stream_ptr(torch.cuda.current_stream())
 
 
+class on_device:
+    """A tensor's device as the current one for a call, and its current stream's handle.  Where it is current already that costs
+    one query."""
+
+    __slots__ = ("index", "before")
+
+    def __init__(self, index: int):
+        self.index = index
+
+    def __enter__(self) -> int:
+        self.before = torch.cuda.current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+        return _raw_stream(self.index) if _raw_stream else _stream_ptr(torch.cuda.current_stream())
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
+def need(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
 class PackedModel:
     """Device weights of one decoder in the library's layouts (projections panel-packed)."""
 

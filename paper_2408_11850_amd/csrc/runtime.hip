@@ -1527,6 +1527,33 @@ extern "C" int spec_sample_row(const float* logits, int vocab, float temperature
   return SPEC_OK;
 }
 
+static int check_sample_rows(int n_rows, int vocab) {
+  if (n_rows < 1 || n_rows > 65535 || vocab < 1 || vocab > SPEC_SAMPLE_VOCAB_MAX)
+    FAIL(SPEC_E_INVAL, "need 1 to 65535 rows of 1 to %d ids", SPEC_SAMPLE_VOCAB_MAX);
+  return SPEC_OK;
+}
+extern "C" size_t spec_sample_rows_workspace_bytes(int n_rows, int vocab) {
+  return check_sample_rows(n_rows, vocab) ? 0 : filter_work_bytes(n_rows, vocab);
+}
+extern "C" int spec_sample_rows(const float* logits, long long ld, int n_rows, int vocab, const spec_sampling* s, const float* u,
+                                float* q_out, float* masked_out, int32_t* tok_out, void* work, void* stream) {
+  if (!logits || !s || !work || (!q_out && !masked_out && !tok_out)) FAIL(SPEC_E_INVAL, "null pointer");
+  int rc = check_sample_rows(n_rows, vocab);
+  if (rc) return rc;
+  if (ld < vocab) FAIL(SPEC_E_INVAL, "row stride below the row");
+  if (!(s->temperature >= 0.0f) || s->temperature == INFINITY || !(s->logit_scale > 0.0f) || s->logit_scale == INFINITY)
+    FAIL(SPEC_E_INVAL, "temperature and logit_scale must be finite, >= 0 and > 0");
+  if (s->top_k < 0 || !(s->top_p >= 0.0f && s->top_p <= 1.0f) || !(s->min_p >= 0.0f && s->min_p <= 1.0f))
+    FAIL(SPEC_E_INVAL, "need top_k >= 0, top_p and min_p in [0, 1]");
+  if (tok_out && s->temperature > 0.0f && !u) FAIL(SPEC_E_INVAL, "a draw needs its uniforms");
+  if (q_out && q_out == masked_out) FAIL(SPEC_E_INVAL, "two results in one place");
+  if ((q_out == logits || masked_out == logits) && ld != vocab) FAIL(SPEC_E_INVAL, "results in place need ld == vocab");
+  if (off_by(logits, 4) || off_by(u, 4) || off_by(q_out, 4) || off_by(masked_out, 4) || off_by(tok_out, 4) || off_by(work, 16))
+    FAIL(SPEC_E_INVAL, "misaligned operand");
+  HIPCHK(launch_sample_rows(logits, (size_t)ld, n_rows, vocab, *s, u, q_out, masked_out, tok_out, work, (hipStream_t)stream));
+  return SPEC_OK;
+}
+
 extern "C" int spec_accept_rows(const float* p_logits, int n_rows, const float* q_rows, const int32_t* x, int n_test,
                                 int vocab, float temperature, float logit_scale, const float* r, float u_resample,
                                 int32_t* result, void* stream) {

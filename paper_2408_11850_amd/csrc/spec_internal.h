@@ -224,6 +224,10 @@ struct AcceptResult {       // device -> pinned host
 };
 hipError_t launch_sample_row(const float* logits, int V, float mult, int greedy, float u, float* q_out, int* tok_out,
                              hipStream_t st);
+// truncated draws (filter.hip)
+size_t filter_work_bytes(int rows, int V);
+hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, const spec_sampling& s, const float* u, float* q,
+                              float* masked, int* tok, void* work, hipStream_t st);
 size_t accept_scratch_floats(int V);   // scratch of one acceptance (rows <= SPEC_MAX_TOKENS)
 hipError_t launch_accept(const float* logits, int V, float mult, int greedy, const float* qcache, const int* ring,
                          const int* x_direct, AcceptArgs a, float* scratch, AcceptResult* result_dev,

@@ -1,0 +1,54 @@
+"""Draws under temperature, top-k, top-p and min-p, and rows truncated the same way (see spec_sample_rows in include/spec.h).
+
+Argument marshalling only.  Every call runs on the current stream of the logits' device.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from . import Sampling, check, load_library
+from .binding import need, on_device
+
+
+def _call(logits: torch.Tensor, u, sampling, want_q: bool, masked, want_tokens: bool):
+    need(logits.is_cuda and logits.dim() == 2 and logits.dtype == torch.float32 and
+         (logits.shape[1] == 1 or logits.stride(1) == 1), "logits: rows in float32 on a GPU are wanted")
+    n, V = logits.shape
+    dev = logits.device
+    lib = load_library()
+    size = lib.spec_sample_rows_workspace_bytes(n, V)
+    work = torch.empty(max(size, 16), dtype=torch.uint8, device=dev)
+    q = torch.empty((n, V), dtype=torch.float32, device=dev) if want_q else None
+    tokens = torch.empty(n, dtype=torch.int32, device=dev) if want_tokens else None
+    with on_device(dev.index) as st:
+        check(lib.spec_sample_rows(logits.data_ptr(), logits.stride(0) if n > 1 else V, n, V, C.byref(sampling),
+                                   u.data_ptr() if u is not None else None, q.data_ptr() if want_q else None,
+                                   masked.data_ptr() if masked is not None else None,
+                                   tokens.data_ptr() if want_tokens else None, work.data_ptr(), st))
+    return tokens, q
+
+
+def sample_rows(logits: torch.Tensor, u: Optional[torch.Tensor], temperature: float = 1.0, logit_scale: float = 1.0,
+                top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+                want_q: bool = True) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """A token per row of fp32 logits [n][vocab] (any row stride) by the uniforms u [n] (fp32, on the GPU; None at temperature
+    0): (tokens int32 [n], the distributions they were drawn from [n][vocab], or None if not wanted)."""
+    if u is not None:
+        need(u.dtype == torch.float32 and u.is_contiguous() and u.device == logits.device and u.numel() == logits.shape[0],
+             "u: float32 [n] on the device of the logits is wanted")
+    return _call(logits, u, Sampling(temperature, logit_scale, top_k, top_p, min_p), want_q, None, True)
+
+
+def filter_rows(logits: torch.Tensor, temperature: float = 1.0, logit_scale: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                min_p: float = 0.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The logits with -inf where sample_rows would keep no id: p_logits for accept_rows with the same temperature and
+    logit_scale.  out: contiguous [n][vocab], may be the logits."""
+    if out is None:
+        out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
+    need(out.dtype == torch.float32 and out.is_contiguous() and out.device == logits.device and out.shape == logits.shape,
+         "out: contiguous float32 of the logits' shape is wanted")
+    _call(logits, None, Sampling(temperature, logit_scale, top_k, top_p, min_p), False, out, False)
+    return out

@@ -9,38 +9,14 @@ from typing import List, Optional, Tuple
 import torch
 
 from . import EPI_STORE, EPI_SWIGLU, FP8_BLOCK, SPEC_BF16, SPEC_F32, check, load_library
+from .binding import need as _need, on_device as _On
 
 _TYPES = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16}
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 E4M3 = torch.float8_e4m3fn
-
-
-class _On:
-    """The device of a call's tensors as the current one, and its stream.  Entering a device that is current costs a query."""
-
-    __slots__ = ("index", "before")
-
-    def __init__(self, index: int):
-        self.index = index
-
-    def __enter__(self) -> int:
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return _raw_stream(self.index) if _raw_stream else torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
 
 
 def _blocks(k: int) -> int:
     return -(-k // FP8_BLOCK)
-
-
-def _need(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
 
 
 def _rows(x: torch.Tensor, name: str) -> int:
