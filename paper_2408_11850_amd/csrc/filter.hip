@@ -4,19 +4,22 @@
 // id): of the first k ids the shortest prefix that holds at least top_p of their mass, and of that the ids with w >= min_p.
 // What is kept is renormalised; a draw is the first id, ascending, at which the running sum passes u times the total.
 //
-// Which id is the last one is decided at a border, and a draw next to one, so z and w are 64-bit and sums of w are integers, in
-// units of 2^-43 (a sum of 2^20 of them fits 64 bits): exact, whatever order atomics come in.
+// Which id is the last one is decided at a border, and a draw next to one, so z and w are 64-bit.  Where atomics add weights up
+// they are integers, in units of 2^-43 (2^20 of them fit 64 bits): the same sum in whatever order; all other sums have a fixed
+// order.
 //
-// A row is cut into chunks of 8192 ids, so that one row uses many compute units.  Passes, each a launch over (chunk, row) unless
-// said otherwise:
-//   top      the chunk's largest logit
-//   bins     counts and masses of 256 classes of z's distance from the row's largest (1/16 up to 12, then 1/4)
-//   collect  every workgroup adds the chunks' classes up and finds those that hold the two borders; ids above them are in, those of
-//            the border classes go to the row's list of candidates
-//   resolve  one workgroup per row: the borders among the candidates by radix selection on (logit, id), masses of what is kept,
-//            and the draw: the chunk, then the id inside it
-//   write    the distribution, or the logits with -inf where an id is not kept
-// Without top-k and top-p nothing has to be sorted: `bins` sums what min-p keeps and `resolve` follows.
+// A row is cut into chunks of 8192 ids (a workgroup each), so that few rows use many compute units.  By what is asked for:
+//   greedy, or temperature alone   top (a chunk's largest logit, sum of weights), finish
+//   min-p alone                    top, mass (what a chunk keeps), finish
+//   top-k up to 1024 ids           groups (largest logit of every 16 ids), few.  The k-th largest group is no more than the k-th
+//                                  largest logit, so whatever counts lies in the groups that reach it: one workgroup per row
+//                                  reads those, resolves the borders among them, draws, and writes q over a row that `groups`
+//                                  has cleared.
+//   else                           bins, collect, resolve, finish.  Borders are first narrowed down by classes of z, 1/8 wide on a
+//                                  fixed grid: `bins` has a chunk's masses and counts by class; in `collect` every workgroup adds
+//                                  the chunks up, ids above the border classes are in, those inside are listed; `resolve`, a
+//                                  workgroup per row, finds the border among them.
+// `finish` writes the distribution or the truncated logits and draws inside the chunk that the draw falls into.
 #include "spec_internal.h"
 
 #define FL_THREADS 512
@@ -25,32 +28,46 @@
 #define FL_QUADS (FL_CHUNK / FL_THREADS / 4)
 #define FL_CHUNKS_MAX (SPEC_SAMPLE_VOCAB_MAX / FL_CHUNK)
 #define FL_BINS 256
-#define FL_LIST 4096                      // candidates that are kept as a list; beyond, the row is read again
-#define FL_ONE 0x1p43                     // a weight of 1
+#define FL_GRID 8.0                       // classes per unit of z
+#define FL_LIST 8192                      // candidates that are kept as a list; beyond, the row is read again
+#define FL_GROUP 16
+#define FL_FEW 1024                       // largest top-k that goes by groups
+#define FL_ONE 0x1p43                     // units of a weight of 1
 typedef unsigned long long u64;
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 static_assert(SPEC_SAMPLE_VOCAB_MAX <= 1 << 20, "sums of weights fit 64 bits");
+static_assert(FL_CHUNKS_MAX <= 128, "two chunks per lane");
 
-struct FilterTop { float v; int id, bad, pad; };              // largest logit of a chunk, its lowest id, NaN or +inf seen
-struct FilterInfo {                                           // borders of a row by classes
-  int kbin, plo, phi, n_before;                               // class of the k-th id; classes that top-p may end in; ids before kbin
-  u64 m_before_k, m_before_p, mass;                           // mass before kbin, before plo, of all
+struct FilterTop {               // of a chunk
+  float v;                       // largest logit ...
+  int id;                        // ... its lowest id
+  int bad, pad;                  // NaN or +inf seen
+  double x;                      // sum of exp(z - this chunk's largest z), or the grid line below its largest z
 };
-struct FilterEnd { u64 last, total; int bad, tok; };         // (logit, id) of the last kept id, mass of what is kept
-struct FilterWork {                                           // arrays over the rows of a call
-  FilterTop* top;      // [row][C]
-  u64* mass;           // [row][C][FL_BINS]
-  unsigned* count;     // [row][C][FL_BINS]
-  u64* sure;           // [row][C]: mass that is kept whatever the candidates
-  u64* list;           // [row][FL_LIST]
-  FilterInfo* info;    // [row]
-  FilterEnd* end;      // [row]
-  unsigned* listed;    // [row]
+struct FilterInfo {              // of a row: borders by classes, masses relative to its largest weight
+  int kbin, plo, phi, n_before;  // class of the k-th id; classes that top-p may end in; ids before kbin
+  double m_before_k, m_before_p, mass;
+};
+struct FilterEnd {
+  u64 last;                      // order of the last kept id
+  double total;                  // units kept
+  int bad, tok;
+};
+struct FilterWork {              // arrays over the rows of a call
+  FilterTop* top;                // [row][C]
+  double* kept;                  // [row][C]: units kept
+  u64* mass;                     // [row][C][FL_BINS]
+  unsigned* count;               // [row][C][FL_BINS]
+  u64* list;                     // [row][FL_LIST]
+  FilterInfo* info;              // [row]
+  FilterEnd* end;                // [row]
+  unsigned* listed;              // [row]
+  float* group;                  // [row][G]: +inf for one with a NaN
 };
 struct FilterArgs {
   const float* logits;
   size_t ld;
-  int V, C, greedy, top_k;       // top_k 0: off
+  int V, C, G, greedy, top_k;    // top_k 0: off
   double mult, top_p, min_p;     // top_p 1: off
   const float* u;
   float *q, *masked;
@@ -60,51 +77,73 @@ struct FilterArgs {
 
 // ---- one id ---------------------------------------------------------------------------------------------------------
 // 64 bits that rise as an id falls in the order: logits by falling value, then ids
-__device__ __forceinline__ u64 order_of(float x, int id) {
+__device__ __forceinline__ unsigned key_of(float x) {
   const unsigned b = __float_as_uint(x + 0.0f);               // -0 counts as 0
-  const unsigned key = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return (u64)~key << 32 | (unsigned)id;
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ u64 order_of(float x, int id) { return (u64)~key_of(x) << 32 | (unsigned)id; }
 __device__ __forceinline__ float logit_of(u64 order) {
   const unsigned key = ~(unsigned)(order >> 32);
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
+// exp(-d), d >= 0: 2^-n times the Taylor series of 2^f, |f| <= 1/2, to the 12th power (6e-15 of the value)
+__device__ __forceinline__ double weight(double d) {
+  const double y = fmin(d, 1000.0) * 1.4426950408889634074, n = rint(y), t = (n - y) * 0.69314718055994530942;
+  double p = 1.0 / 479001600.0;
+  p = fma(p, t, 1.0 / 39916800.0);
+  p = fma(p, t, 1.0 / 3628800.0);
+  p = fma(p, t, 1.0 / 362880.0);
+  p = fma(p, t, 1.0 / 40320.0);
+  p = fma(p, t, 1.0 / 5040.0);
+  p = fma(p, t, 1.0 / 720.0);
+  p = fma(p, t, 1.0 / 120.0);
+  p = fma(p, t, 1.0 / 24.0);
+  p = fma(p, t, 1.0 / 6.0);
+  p = fma(p, t, 0.5);
+  p = fma(p, t, 1.0);
+  p = fma(p, t, 1.0);
+  return ldexp(p, -(int)n);
+}
 __device__ __forceinline__ double distance(float top, float x, double mult) { return ((double)top - (double)x) * mult; }
-__device__ __forceinline__ double weight(double dist) { return exp(-dist); }
-__device__ __forceinline__ u64 units(double w) { return (u64)(w * FL_ONE + 0.5); }
-__device__ __forceinline__ int bin_of(double dist) {
-  const double b = dist < 12.0 ? dist * 16.0 : 192.0 + (dist - 12.0) * 4.0;
+// w <= 1: added to 2^52, the units are the low bits of the sum
+__device__ __forceinline__ u64 units(double w) { return (u64)__double_as_longlong(fma(w, FL_ONE, 0x1p52)) & 0xfffffffffffffull; }
+__device__ __forceinline__ double line_of(float x, double mult) { return floor((double)x * mult * FL_GRID); }
+__device__ __forceinline__ int class_of(double line, float x, double mult) {
+  const double b = line - line_of(x, mult);
   return b < FL_BINS - 1 ? (int)b : FL_BINS - 1;
 }
 
 // ---- a workgroup ----------------------------------------------------------------------------------------------------
-__device__ __forceinline__ u64 wave_sum_u(u64 v) {
+template <typename T>
+__device__ __forceinline__ T wave_sum_t(T v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-__device__ __forceinline__ u64 wave_scan_u(u64 v) {           // inclusive
+template <typename T>
+__device__ __forceinline__ T wave_scan_t(T v) {               // inclusive
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const u64 t = __shfl_up(v, o);
+    const T t = __shfl_up(v, o);
     if (lane >= o) v += t;
   }
   return v;
 }
-__device__ __forceinline__ u64 block_sum_u(u64 v, u64* sh) {  // to every thread
-  v = wave_sum_u(v);
+template <typename T>
+__device__ __forceinline__ T block_sum_t(T v, T* sh) {        // to every thread
+  v = wave_sum_t(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
-  u64 t = 0;
+  T t = 0;
 #pragma unroll
   for (int i = 0; i < FL_WAVES; ++i) t += sh[i];
   return t;
 }
 __device__ __forceinline__ u64 block_scan_u(u64 v, u64* sh, u64* total) {   // exclusive
   const int w = threadIdx.x >> 6;
-  const u64 s = wave_scan_u(v);
+  const u64 s = wave_scan_t(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 63) sh[w] = s;
   __syncthreads();
@@ -135,8 +174,18 @@ __device__ __forceinline__ void load_chunk(const FilterArgs& a, int row, int chu
   }
 }
 __device__ __forceinline__ int id_of(int chunk, int j, int i) { return chunk * FL_CHUNK + j * FL_THREADS * 4 + threadIdx.x * 4 + i; }
+// four results from the id of i = 0 on
+__device__ __forceinline__ void put4(float* out, const FilterArgs& a, int row, int id, const float (&v)[4]) {
+  float* p = out + (size_t)row * a.V + id;
+  if (id + 4 <= a.V) {
+    *reinterpret_cast<f32x4u*>(p) = f32x4u{v[0], v[1], v[2], v[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (id + i < a.V) p[i] = v[i];
+  }
+}
 
-struct RowTop { float v; int id; bool none; };                // none: no distribution
 __device__ __forceinline__ FilterTop better(FilterTop a, FilterTop b) {
   const bool take = b.v > a.v || (b.v == a.v && b.id < a.id);
   a.v = take ? b.v : a.v;
@@ -155,20 +204,9 @@ __device__ __forceinline__ FilterTop wave_better(FilterTop t) {
   }
   return t;
 }
-__device__ __forceinline__ RowTop row_top(const FilterArgs& a, int row) {    // by every wave for itself
-  FilterTop t = {-INFINITY, 0, 0, 0};
-  for (int c = threadIdx.x & 63; c < a.C; c += 64) t = better(t, a.w.top[(size_t)row * a.C + c]);
-  t = wave_better(t);
-  return RowTop{t.v, t.id, t.bad || t.v == -INFINITY};
-}
-
-// ---- the passes -----------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(FL_THREADS) void filter_top_kernel(FilterArgs a) {
-  __shared__ FilterTop sh[FL_WAVES];
-  const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
-  load_chunk(a, row, chunk, x);
-  FilterTop t = {-INFINITY, 0x7fffffff, 0, 0};
+// of the chunk, to every thread; id 0 where nothing is above -inf
+__device__ __forceinline__ FilterTop chunk_top(const FilterArgs& a, int chunk, const float (&x)[FL_QUADS][4], FilterTop* sh) {
+  FilterTop t = {-INFINITY, 0x7fffffff, 0, 0, 0.0};
 #pragma unroll
   for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
@@ -179,130 +217,188 @@ __global__ __launch_bounds__(FL_THREADS) void filter_top_kernel(FilterArgs a) {
   t = wave_better(t);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = t;
   __syncthreads();
-  if (threadIdx.x == 0) {
+  t = sh[0];
 #pragma unroll
-    for (int i = 1; i < FL_WAVES; ++i) t = better(t, sh[i]);
-    if (t.id == 0x7fffffff) t.id = 0;
-    a.w.top[(size_t)row * a.C + chunk] = t;
-    if (chunk == 0) a.w.listed[row] = 0;
-  }
+  for (int i = 1; i < FL_WAVES; ++i) t = better(t, sh[i]);
+  if (t.id == 0x7fffffff) t.id = 0;
+  return t;
+}
+struct RowTop { float v; int id; bool none; };                // none: no distribution
+__device__ __forceinline__ RowTop row_top(const FilterArgs& a, int row) {    // by every wave for itself
+  FilterTop t = {-INFINITY, 0, 0, 0, 0.0};
+  for (int c = threadIdx.x & 63; c < a.C; c += 64) t = better(t, a.w.top[(size_t)row * a.C + c]);
+  t = wave_better(t);
+  return RowTop{t.v, t.id, t.bad || t.v == -INFINITY};
 }
 
-__global__ __launch_bounds__(FL_THREADS) void filter_bins_kernel(FilterArgs a, int classes) {
-  __shared__ u64 mass[FL_BINS], sh[FL_WAVES];
-  __shared__ unsigned count[FL_BINS];
+// ---- greedy, temperature alone, min-p alone -------------------------------------------------------------------------
+__global__ __launch_bounds__(FL_THREADS) void filter_top_kernel(FilterArgs a, int sum) {
+  __shared__ FilterTop sh[FL_WAVES];
+  __shared__ double shd[FL_WAVES];
+  const int chunk = blockIdx.x, row = blockIdx.y;
+  float x[FL_QUADS][4];
+  load_chunk(a, row, chunk, x);
+  FilterTop t = chunk_top(a, chunk, x, sh);
+  if (sum && !t.bad && t.v > -INFINITY) {
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < FL_QUADS; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s += weight(distance(t.v, x[j][i], a.mult));
+    t.x = block_sum_t(s, shd);
+  }
+  if (threadIdx.x == 0) a.w.top[(size_t)row * a.C + chunk] = t;
+}
+__global__ __launch_bounds__(FL_THREADS) void filter_mass_kernel(FilterArgs a) {
+  __shared__ u64 sh[FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
   const RowTop top = row_top(a, row);
   if (top.none) return;
-  if (!classes) {
-    u64 sum = 0;
+  u64 sum = 0;
+#pragma unroll
+  for (int j = 0; j < FL_QUADS; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const double w = weight(distance(top.v, x[j][i], a.mult));
+      if (w >= a.min_p) sum += units(w);
+    }
+  sum = block_sum_t(sum, sh);
+  if (threadIdx.x == 0) a.w.kept[(size_t)row * a.C + chunk] = (double)sum;
+}
+
+// ---- classes --------------------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(FL_THREADS) void filter_bins_kernel(FilterArgs a) {
+  __shared__ FilterTop sh[FL_WAVES];
+  __shared__ u64 mass[FL_BINS];
+  __shared__ unsigned count[FL_BINS];
+  const int chunk = blockIdx.x, row = blockIdx.y;
+  float x[FL_QUADS][4];
+  load_chunk(a, row, chunk, x);
+  if (threadIdx.x < FL_BINS) mass[threadIdx.x] = 0, count[threadIdx.x] = 0;
+  FilterTop t = chunk_top(a, chunk, x, sh);
+  t.x = line_of(t.v, a.mult);
+  if (threadIdx.x == 0) {
+    a.w.top[(size_t)row * a.C + chunk] = t;
+    if (chunk == 0) a.w.listed[row] = 0;
+  }
+  if (t.bad) return;
+  if (t.v > -INFINITY) {
 #pragma unroll
     for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const double w = weight(distance(top.v, x[j][i], a.mult));
-        if (w >= a.min_p) sum += units(w);
-      }
-    sum = block_sum_u(sum, sh);
-    if (threadIdx.x == 0) a.w.sure[(size_t)row * a.C + chunk] = sum;
-    return;
-  }
-  if (threadIdx.x < FL_BINS) mass[threadIdx.x] = 0, count[threadIdx.x] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (id_of(chunk, j, i) < a.V) {
-        const double d = distance(top.v, x[j][i], a.mult);
-        const int b = bin_of(d);
-        atomicAdd(&count[b], 1u);
-        const u64 m = units(weight(d));
+        const int b = class_of(t.x, x[j][i], a.mult);
+        if (a.top_k && b < FL_BINS - 1) atomicAdd(&count[b], 1u);
+        const u64 m = units(weight(distance(t.v, x[j][i], a.mult)));
         if (m) atomicAdd(&mass[b], m);
       }
+  }
   __syncthreads();
   if (threadIdx.x < FL_BINS) {
     const size_t at = ((size_t)row * a.C + chunk) * FL_BINS + threadIdx.x;
     a.w.mass[at] = mass[threadIdx.x];
-    a.w.count[at] = count[threadIdx.x];
+    if (a.top_k) a.w.count[at] = count[threadIdx.x];
   }
 }
 
-// first class whose inclusive sum reaches a target, by one wave of which lane l holds classes 4 l .. 4 l + 3
+// The borders of a row by classes, by the first wave: lane l holds classes 4 l .. 4 l + 3 of mass and count.  The last class takes
+// all that lies further below, more than 31 in z: no mass in units, and the k-th id if no earlier class has it.
+__device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const double* mass, const unsigned* count) {
+  const int lane = threadIdx.x;
+  double m[4], sm = 0.0;
+  unsigned n[4], sn = 0;                           // inclusive sums inside the lane
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    sm += mass[lane * 4 + i];
+    sn += count[lane * 4 + i];
+    m[i] = sm;
+    n[i] = sn;
+  }
+  const double im = wave_scan_t(sm), up = __shfl_up(im, 1), bm = lane ? up : 0.0;
+  const unsigned in = wave_scan_t(sn), bn = in - sn;
+  FilterInfo f;
+  f.mass = __shfl(im, 63);
+  // first class whose inclusive sums `reached` accepts, else the last one, and the sums before it
+  auto first = [&](auto reached, double* before_m, int* before_n, double* upto) {
+    int k = -1;
+#pragma unroll
+    for (int i = 3; i >= 0; --i)
+      if (reached(bm + m[i], bn + n[i])) k = i;
+    const u64 some = __ballot(k >= 0);
+    const int at = some ? __ffsll((long long)some) - 1 : 63, pick = some ? k : 3;
+    double pm = bm, um = bm + m[0];
+    unsigned pn = bn;
+#pragma unroll
+    for (int i = 1; i < 4; ++i)
+      if (pick == i) pm = bm + m[i - 1], pn = bn + n[i - 1], um = bm + m[i];
+    *before_m = __shfl(pm, at);
+    *before_n = (int)__shfl(pn, at);
+    *upto = __shfl(um, at);
+    return __shfl(lane * 4 + pick, at);
+  };
+  double upto = f.mass, skip_m;
+  int skip_n;
+  f.kbin = FL_BINS;
+  f.m_before_k = f.mass;
+  f.n_before = 0;
+  if (a.top_k) f.kbin = first([&](double, unsigned c) { return c >= (unsigned)a.top_k; }, &f.m_before_k, &f.n_before, &upto);
+  f.plo = f.phi = FL_BINS;
+  f.m_before_p = 0.0;
+  if (a.top_p < 1.0) {                             // the k ids' mass lies between these two
+    const double lo = a.top_p * f.m_before_k, hi = a.top_p * upto;
+    double skip;
+    f.plo = first([&](double s, unsigned) { return s >= lo; }, &f.m_before_p, &skip_n, &skip);
+    f.phi = first([&](double s, unsigned) { return s >= hi; }, &skip_m, &skip_n, &skip);
+  }
+  return f;
+}
+
 __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a) {
-  __shared__ u64 mass[2][FL_BINS], sh[FL_WAVES];
+  __shared__ double mass[2][FL_BINS], factor[FL_CHUNKS_MAX];
   __shared__ unsigned count[2][FL_BINS], base;
+  __shared__ int shift[FL_CHUNKS_MAX];
+  __shared__ u64 sh[FL_WAVES];
   __shared__ FilterInfo info;
   const int chunk = blockIdx.x, row = blockIdx.y;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
   const RowTop top = row_top(a, row);
   if (top.none) return;
+  const double line = line_of(top.v, a.mult);
+  if (threadIdx.x < a.C) {                         // chunk c's classes count from its own largest z, on the same grid
+    const FilterTop t = a.w.top[(size_t)row * a.C + threadIdx.x];
+    const double s = line - t.x;
+    shift[threadIdx.x] = s < FL_BINS ? (int)s : FL_BINS;
+    factor[threadIdx.x] = weight(distance(top.v, t.v, a.mult)) / FL_ONE;
+  }
+  __syncthreads();
   {
     const int b = threadIdx.x & (FL_BINS - 1), half = threadIdx.x / FL_BINS;
-    u64 m = 0;
+    double m = 0.0;
     unsigned n = 0;
+#pragma unroll 4
     for (int c = half; c < a.C; c += FL_THREADS / FL_BINS) {
-      const size_t at = ((size_t)row * a.C + c) * FL_BINS + b;
-      m += a.w.mass[at];
-      n += a.w.count[at];
+      const int from = b - shift[c];
+      if (from >= 0) {
+        const size_t at = ((size_t)row * a.C + c) * FL_BINS + from;
+        m += (double)a.w.mass[at] * factor[c];
+        if (a.top_k) n += a.w.count[at];
+      }
     }
     mass[half][b] = m;
     count[half][b] = n;
   }
   __syncthreads();
+  if (threadIdx.x < FL_BINS) {
+    mass[0][threadIdx.x] += mass[1][threadIdx.x];
+    count[0][threadIdx.x] += count[1][threadIdx.x];
+  }
+  __syncthreads();
   if (threadIdx.x < 64) {
-    const int lane = threadIdx.x;
-    u64 m[4], n[4], sm = 0, sn = 0;                // inclusive sums inside the lane
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      sm += mass[0][lane * 4 + i] + mass[1][lane * 4 + i];
-      sn += count[0][lane * 4 + i] + count[1][lane * 4 + i];
-      m[i] = sm;
-      n[i] = sn;
-    }
-    const u64 bm = wave_scan_u(sm) - sm, bn = wave_scan_u(sn) - sn;
-    const u64 all = __shfl(bm + sm, 63);
-    // class (and the sums before it) of the first inclusive sum that `reached` accepts; the sums rise, so it is one lane's
-    auto first = [&](auto reached, int* bin, u64* before_m, u64* before_n) {
-      int k = -1;
-#pragma unroll
-      for (int i = 3; i >= 0; --i)
-        if (reached(bm + m[i], bn + n[i])) k = i;
-      const u64 some = __ballot(k >= 0);
-      const int at = some ? __ffsll((long long)some) - 1 : 63;
-      u64 pm = bm, pn = bn;
-#pragma unroll
-      for (int i = 1; i < 4; ++i)
-        if (k == i) pm = bm + m[i - 1], pn = bn + n[i - 1];
-      *bin = __shfl(lane * 4 + (k < 0 ? 3 : k), at);
-      *before_m = __shfl(pm, at);
-      *before_n = __shfl(pn, at);
-    };
-    FilterInfo f;
-    u64 nb = 0, unused_m, unused_n;
-    f.mass = all;
-    f.kbin = FL_BINS;
-    f.m_before_k = all;
-    if (a.top_k) first([&](u64, u64 c) { return c >= (u64)a.top_k; }, &f.kbin, &f.m_before_k, &nb);
-    f.n_before = (int)nb;
-    f.plo = f.phi = FL_BINS;
-    f.m_before_p = 0;
-    if (a.top_p < 1.0) {
-      u64 upto = all;                              // mass of the k ids at most: what kbin holds counted whole
-      if (a.top_k) {
-        u64 b0 = 0, b1 = 0;
-        int bin = 0;
-        first([&](u64, u64 c) { return c >= (u64)a.top_k; }, &bin, &b0, &b1);
-        upto = b0 + mass[0][bin] + mass[1][bin];
-      }
-      const double lo = a.top_p * (double)f.m_before_k, hi = a.top_p * (double)upto;
-      first([&](u64 s, u64) { return (double)s >= lo; }, &f.plo, &f.m_before_p, &unused_n);
-      first([&](u64 s, u64) { return (double)s >= hi; }, &f.phi, &unused_m, &unused_n);
-    }
-    if (lane == 0) {
+    const FilterInfo f = find_classes(a, mass[0], count[0]);
+    if (threadIdx.x == 0) {
       info = f;
       if (chunk == 0) a.w.info[row] = f;
     }
@@ -315,19 +411,18 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
   for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const double d = distance(top.v, x[j][i], a.mult);
-      const int b = bin_of(d);
+      const int b = class_of(line, x[j][i], a.mult);
       if (b < sure_below) {
-        const double w = weight(d);
+        const double w = weight(distance(top.v, x[j][i], a.mult));
         if (w >= a.min_p) sum += units(w);
       }
       if (id_of(chunk, j, i) < a.V && (b == kbin || (b >= plo && b <= phi))) mine |= 1u << (j * 4 + i);
     }
-  sum = block_sum_u(sum, sh);
+  sum = block_sum_t(sum, sh);
   u64 n;
   u64 at = block_scan_u(__popc(mine), sh, &n);
   if (threadIdx.x == 0) {
-    a.w.sure[(size_t)row * a.C + chunk] = sum;
+    a.w.kept[(size_t)row * a.C + chunk] = (double)sum;
     base = n ? atomicAdd(&a.w.listed[row], (unsigned)n) : 0;
   }
   __syncthreads();
@@ -342,223 +437,398 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
       }
 }
 
-// The candidates of a row, from the list or, where it did not hold them, from the row itself.
-struct Candidates {
-  const FilterArgs& a;
-  const FilterInfo& f;
-  const u64* list;
-  const float* row;
-  int n;
-  bool whole;
-  float top;
-  template <typename F>
-  __device__ __forceinline__ void each(F&& use) const {        // use(order, class, distance)
-    for (int i = threadIdx.x; i < n; i += FL_THREADS) {
-      const u64 o = whole ? order_of(row[i], i) : list[i];
-      const double d = distance(top, whole ? row[i] : logit_of(o), a.mult);
-      const int b = bin_of(d);
-      if (!whole || b == f.kbin || (b >= f.plo && b <= f.phi)) use(o, b, d);
+// Of the keys that each(visit(key, amount)) goes through (amount > 0, every key once), the one at which the running sum of the
+// amounts, by rising key, is first accepted by reached(sum); the last key, should none be; 0 without keys.  Digits of 8 bits from
+// the highest bit in which the keys still in question differ; done when one is left.
+struct SelectLds { u64 hist[256], lo[FL_WAVES], hi[FL_WAVES], pick[2]; };
+template <typename E, typename R>
+__device__ u64 select_key(const E& each, const R& reached, SelectLds& s) {
+  u64 first = 0, last = ~0ull, before = 0;         // keys in question, sum of what comes before them
+  while (true) {
+    u64 lo = ~0ull, hi = 0;
+    each([&](u64 k, u64) {
+      if (k >= first && k <= last) lo = k < lo ? k : lo, hi = k > hi ? k : hi;
+    });
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const u64 l = __shfl_xor(lo, o), h = __shfl_xor(hi, o);
+      lo = l < lo ? l : lo;
+      hi = h > hi ? h : hi;
     }
-  }
-};
-
-// The candidate at which the running sum, in order, of amount(order, class, distance) first reaches `target` (`base` before
-// the first); the last one that has any, should none.  Digits of 8 bits, from the highest down.
-template <typename A, typename T>
-__device__ u64 select(const Candidates& c, A amount, u64 base, T target, u64* hist, u64* sh) {
-  u64 prefix = 0;
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += FL_THREADS) hist[i] = 0;
+    if ((threadIdx.x & 63) == 0) s.lo[threadIdx.x >> 6] = lo, s.hi[threadIdx.x >> 6] = hi;
+    if (threadIdx.x < 256) s.hist[threadIdx.x] = 0;
     __syncthreads();
-    c.each([&](u64 o, int b, double d) {
-      if (shift == 56 || (o ^ prefix) >> (shift + 8) == 0) {
-        const u64 v = amount(o, b, d);
-        if (v) atomicAdd((u64*)&hist[o >> shift & 255], v);
-      }
+#pragma unroll
+    for (int i = 0; i < FL_WAVES; ++i) {
+      lo = s.lo[i] < lo ? s.lo[i] : lo;
+      hi = s.hi[i] > hi ? s.hi[i] : hi;
+    }
+    if (lo >= hi) {
+      __syncthreads();
+      return lo > hi ? 0 : lo;
+    }
+    const int top = 63 - __clzll((long long)(lo ^ hi)), shift = top > 7 ? top - 7 : 0;
+    each([&](u64 k, u64 amount) {
+      if (k >= first && k <= last) atomicAdd(&s.hist[(k >> shift) & 255], amount);
     });
     __syncthreads();
     if (threadIdx.x < 64) {
       const int lane = threadIdx.x;
-      u64 h[4], s = 0;
+      u64 h[4], sum = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s += hist[lane * 4 + i];
-        h[i] = s;
+        sum += s.hist[lane * 4 + i];
+        h[i] = sum;
       }
-      const u64 before = base + wave_scan_u(s) - s;
-      int k = -1, last = -1;
+      const u64 b = before + wave_scan_t(sum) - sum;
+      int k = -1, some = -1;
 #pragma unroll
       for (int i = 3; i >= 0; --i) {
-        if (h[i] != (i ? h[i - 1] : 0) && last < 0) last = i;
-        if (h[i] != (i ? h[i - 1] : 0) && target(before + h[i])) k = i;
+        const bool any = h[i] != (i ? h[i - 1] : 0);
+        if (any && some < 0) some = i;
+        if (any && reached(b + h[i])) k = i;
       }
-      const u64 some = __ballot(k >= 0), any = __ballot(last >= 0);
-      const int at = some ? __ffsll((long long)some) - 1 : any ? 63 - __clzll((long long)any) : 0;
-      const int pick = some ? k : last < 0 ? 0 : last;
-      u64 pm = before;
+      const u64 good = __ballot(k >= 0), filled = __ballot(some >= 0);
+      const int at = good ? __ffsll((long long)good) - 1 : 63 - __clzll((long long)filled), pick = good ? k : some;
+      u64 pm = b;
 #pragma unroll
       for (int i = 1; i < 4; ++i)
-        if (pick == i) pm = before + h[i - 1];
-      if (lane == at) {
-        sh[0] = (u64)(lane * 4 + pick);
-        sh[1] = pm;
-      }
+        if (pick == i) pm = b + h[i - 1];
+      if (lane == at) s.pick[0] = lane * 4 + pick, s.pick[1] = pm;
     }
     __syncthreads();
-    prefix |= sh[0] << shift;
-    base = sh[1];
-    __syncthreads();
+    // the keys share the bits above `top`, and top is bit shift + 7, so the digit has them all in order
+    first = (lo >> shift & ~255ull | s.pick[0]) << shift;
+    last = first | ((1ull << shift) - 1);
+    before = s.pick[1];
+    if (shift == 0) {
+      __syncthreads();
+      return first;
+    }
   }
-  return prefix;
 }
 
-__global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a, int classes) {
-  __shared__ u64 list[FL_LIST], hist[256], sh[FL_WAVES], chunk_mass[FL_CHUNKS_MAX];
-  __shared__ FilterInfo f;
-  __shared__ int place;
+// The border of a row among its candidates: the list, or where it did not hold them the row itself.
+__global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a) {
+  extern __shared__ u64 filter_lds[];              // FL_LIST orders, FL_LIST units
+  u64 *list = filter_lds, *amount = filter_lds + FL_LIST;
+  __shared__ u64 sh[FL_WAVES], chunk_mass[FL_CHUNKS_MAX];
+  __shared__ SelectLds lds;
   const int row = blockIdx.x;
   const RowTop top = row_top(a, row);
+  if (top.none) return;
+  const FilterInfo f = a.w.info[row];
+  const double line = line_of(top.v, a.mult);
+  const float* x = a.logits + (size_t)row * a.ld;
+  const unsigned listed = a.w.listed[row];
+  const bool whole = listed > FL_LIST;
+  const int n = whole ? a.V : (int)listed;
+  for (int c = threadIdx.x; c < a.C; c += FL_THREADS) chunk_mass[c] = 0;
+  if (!whole)
+    for (int i = threadIdx.x; i < n; i += FL_THREADS) {
+      const u64 o = a.w.list[(size_t)row * FL_LIST + i];
+      list[i] = o;
+      amount[i] = units(weight(distance(top.v, logit_of(o), a.mult)));
+    }
+  __syncthreads();
+  // use(order, class, units) of every candidate
+  auto candidates = [&](auto use) {
+    for (int i = threadIdx.x; i < n; i += FL_THREADS) {
+      const float v = whole ? x[i] : logit_of(list[i]);
+      const int b = class_of(line, v, a.mult);
+      if (!whole) use(list[i], b, amount[i]);
+      else if (b == f.kbin || (b >= f.plo && b <= f.phi)) use(order_of(v, i), b, units(weight(distance(top.v, v, a.mult))));
+    }
+  };
+  u64 last = ~0ull;
+  double mass_k = f.mass;
+  if (a.top_k) {
+    const u64 rank = (u64)(a.top_k - f.n_before);
+    last = select_key([&](auto visit) { candidates([&](u64 o, int b, u64) { if (b == f.kbin) visit(o, 1ull); }); },
+                      [&](u64 s) { return s >= rank; }, lds);
+    u64 m = 0;
+    candidates([&](u64 o, int b, u64 w) { if (b == f.kbin && o <= last) m += w; });
+    mass_k = f.m_before_k + (double)block_sum_t(m, sh) / FL_ONE;
+  }
+  if (a.top_p < 1.0) {
+    const double goal = (a.top_p * mass_k - f.m_before_p) * FL_ONE;
+    const u64 upto = last;
+    last = select_key([&](auto visit) { candidates([&](u64 o, int b, u64 w) { if (b >= f.plo && b <= f.phi && o <= upto && w) visit(o, w); }); },
+                      [&](u64 s) { return (double)s >= goal; }, lds);
+  }
+  candidates([&](u64 o, int, u64 w) {
+    if (o <= last && weight(distance(top.v, logit_of(o), a.mult)) >= a.min_p && w) atomicAdd(&chunk_mass[(unsigned)o / FL_CHUNK], w);
+  });
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.C; c += FL_THREADS) a.w.kept[(size_t)row * a.C + c] += (double)chunk_mass[c];
+  if (threadIdx.x == 0) a.w.end[row].last = last;
+}
+
+// ---- results --------------------------------------------------------------------------------------------------------
+enum { FINISH_ALL = 0 /* nothing truncated but by min-p = 0 */, FINISH_KEPT = 1 /* masses of the chunks */, FINISH_CLASSES = 2 /* and a border */,
+       FINISH_WRITE = 3 /* border, total and token are there */ };
+__global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a, int mode) {
+  __shared__ u64 sh[FL_WAVES];
+  const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
+  float x[FL_QUADS][4];
+  load_chunk(a, row, chunk, x);
+  const RowTop top = mode == FINISH_WRITE ? RowTop{a.w.top[row].v, 0, a.w.end[row].bad != 0} : row_top(a, row);
   if (a.greedy || top.none) {
-    if (threadIdx.x == 0) {
-      FilterEnd e;
-      e.tok = a.greedy ? top.id : -1;
-      e.bad = a.greedy ? 0 : 1;
-      e.last = 0;
-      e.total = 0;
-      a.w.end[row] = e;
-      if (a.tok) a.tok[row] = e.tok;
+    if (a.tok && chunk == 0 && threadIdx.x == 0 && mode != FINISH_WRITE) a.tok[row] = a.greedy ? top.id : -1;
+#pragma unroll
+    for (int j = 0; j < FL_QUADS; ++j) {
+      float q[4], m[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool on = id_of(chunk, j, i) == top.id;
+        q[i] = !a.greedy ? __builtin_nanf("") : on ? 1.0f : 0.0f;
+        m[i] = !a.greedy ? __builtin_nanf("") : on ? x[j][i] : -INFINITY;
+      }
+      if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), q);
+      if (a.masked) put4(a.masked, a, row, id_of(chunk, j, 0), m);
     }
     return;
   }
+  // units of every chunk, two per lane, and their running sums: the same in every wave and workgroup
+  double before = 0.0, here = 0.0, total;
+  bool mine = false;
   u64 last = ~0ull;
-  for (int c = threadIdx.x; c < a.C; c += FL_THREADS) chunk_mass[c] = a.w.sure[(size_t)row * a.C + c];
-  if (classes) {
-    if (threadIdx.x == 0) f = a.w.info[row];
-    const unsigned n = a.w.listed[row];
-    const bool whole = n > FL_LIST;
-    if (!whole)
-      for (unsigned i = threadIdx.x; i < n; i += FL_THREADS) list[i] = a.w.list[(size_t)row * FL_LIST + i];
-    __syncthreads();
-    const Candidates c = {a, f, list, a.logits + (size_t)row * a.ld, whole ? a.V : (int)n, whole, top.v};
-    u64 mass_k = f.mass;
-    if (a.top_k) {
-      const u64 rank = (u64)a.top_k - f.n_before;
-      last = select(c, [&](u64, int b, double) { return (u64)(b == f.kbin); }, 0, [&](u64 s) { return s >= rank; }, hist, sh);
-      u64 m = 0;
-      c.each([&](u64 o, int b, double d) {
-        if (b == f.kbin && o <= last) m += units(weight(d));
-      });
-      mass_k = f.m_before_k + block_sum_u(m, sh);
+  double goal = 0.0;
+  if (mode == FINISH_WRITE) {
+    last = a.w.end[row].last;
+    total = a.w.end[row].total;
+  } else {
+    if (mode == FINISH_CLASSES) last = a.w.end[row].last;
+    double m[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = lane * 2 + i;
+      const size_t at = (size_t)row * a.C + c;
+      m[i] = 0.0;
+      if (c < a.C) m[i] = mode == FINISH_ALL ? a.w.top[at].x * weight(distance(top.v, a.w.top[at].v, a.mult)) * FL_ONE : a.w.kept[at];
     }
-    if (a.top_p < 1.0) {
-      const double goal = a.top_p * (double)mass_k;
-      const u64 upto = last;
-      last = select(c, [&](u64 o, int b, double d) { return b >= f.plo && b <= f.phi && o <= upto ? units(weight(d)) : 0ull; },
-                    f.m_before_p, [&](u64 s) { return (double)s >= goal; }, hist, sh);
-    }
-    c.each([&](u64 o, int, double d) {
-      if (o <= last) {
-        const double w = weight(d);
-        if (w >= a.min_p) atomicAdd(&chunk_mass[(unsigned)o / FL_CHUNK], units(w));
+    const double in = wave_scan_t(m[0] + m[1]), up = __shfl_up(in, 1), ex = lane ? up : 0.0;
+    total = __shfl(in, 63);
+    if (a.tok) {
+      goal = fmin(fmax((double)a.u[row], 0.0), 1.0) * total;
+      // the first chunk whose running sum passes the goal, else the last one with any mass
+      const u64 p0 = __ballot(m[0] > 0.0 && ex + m[0] > goal), p1 = __ballot(m[1] > 0.0 && ex + m[0] + m[1] > goal);
+      const u64 f0 = __ballot(m[0] > 0.0), f1 = __ballot(m[1] > 0.0);
+      int c;
+      if (p0 | p1) {
+        const int l0 = p0 ? __ffsll((long long)p0) - 1 : 64, l1 = p1 ? __ffsll((long long)p1) - 1 : 64;
+        c = l0 <= l1 ? l0 * 2 : l1 * 2 + 1;
+      } else {
+        const int l0 = f0 ? 63 - __clzll((long long)f0) : -1, l1 = f1 ? 63 - __clzll((long long)f1) : -1;
+        c = l1 >= l0 ? l1 * 2 + 1 : l0 * 2;
       }
-    });
-  }
-  __syncthreads();
-  // the chunk that the draw falls into
-  u64 m = 0, total;
-  static_assert(FL_CHUNKS_MAX <= FL_THREADS, "a thread per chunk");
-  if (threadIdx.x < a.C) m = chunk_mass[threadIdx.x];
-  u64 before = block_scan_u(m, sh, &total);
-  if (threadIdx.x == 0) {
-    FilterEnd e;
-    e.last = last;
-    e.total = total;
-    e.bad = 0;
-    e.tok = 0;
-    a.w.end[row] = e;
-  }
-  if (!a.tok) return;
-  double u = (double)a.u[row];
-  if (!(u > 0.0)) u = 0.0;
-  u64 goal = (u64)(u * (double)total);
-  if (goal >= total) goal = total - 1;
-  if (before <= goal && goal < before + m) place = threadIdx.x;
-  __syncthreads();
-  const int chunk = place;
-  if (threadIdx.x == chunk) sh[0] = goal - before;          // (after the last read of sh in block_scan_u: a barrier lies between)
-  __syncthreads();
-  goal = sh[0];
-  float x[FL_QUADS][4];
-  load_chunk(a, row, chunk, x);
-  u64 start = 0;
-#pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j) {
-    u64 v[4], s = 0, all;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const double w = weight(distance(top.v, x[j][i], a.mult));
-      v[i] = order_of(x[j][i], id_of(chunk, j, i)) <= last && w >= a.min_p ? units(w) : 0;
-      s += v[i];
+      mine = c == chunk;
+      before = __shfl(chunk & 1 ? ex + m[0] : ex, chunk >> 1);
+      here = __shfl(chunk & 1 ? m[1] : m[0], chunk >> 1);
     }
-    u64 at = start + block_scan_u(s, sh, &all);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (at <= goal && goal < at + v[i]) a.tok[row] = id_of(chunk, j, i);
-      at += v[i];
-    }
-    start += all;
   }
-}
-
-__global__ __launch_bounds__(FL_THREADS) void filter_write_kernel(FilterArgs a) {
-  const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
-  load_chunk(a, row, chunk, x);
-  const FilterEnd e = a.w.end[row];
-  const RowTop top = row_top(a, row);
-  const double inv = 1.0 / ((double)e.total / FL_ONE);
+  if (!a.q && !a.masked && !mine) return;
+  const double inv = FL_ONE / total;
+  unsigned kept = 0;
 #pragma unroll
   for (int j = 0; j < FL_QUADS; ++j) {
     float q[4], m[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int id = id_of(chunk, j, i);
-      if (a.greedy) {
-        q[i] = id == e.tok ? 1.0f : 0.0f;
-        m[i] = id == e.tok ? x[j][i] : -INFINITY;
-      } else if (e.bad) {
-        q[i] = m[i] = __builtin_nanf("");
-      } else {
-        q[i] = 0.0f;
-        m[i] = -INFINITY;
-        if (order_of(x[j][i], id) <= e.last) {
-          const double w = weight(distance(top.v, x[j][i], a.mult));
-          if (w >= a.min_p) {
-            q[i] = (float)(w * inv);
-            m[i] = x[j][i];
-          }
+      q[i] = 0.0f;
+      m[i] = -INFINITY;
+      if (id < a.V && (last == ~0ull || order_of(x[j][i], id) <= last)) {
+        const double w = weight(distance(top.v, x[j][i], a.mult));
+        if (w >= a.min_p) {
+          kept |= 1u << (j * 4 + i);
+          q[i] = (float)(w * inv);
+          m[i] = x[j][i];
         }
       }
     }
-    const int id = id_of(chunk, j, 0);
-    const size_t at = (size_t)row * a.V + id;
-    if (id + 4 <= a.V) {
-      if (a.q) *reinterpret_cast<f32x4u*>(a.q + at) = f32x4u{q[0], q[1], q[2], q[3]};
-      if (a.masked) *reinterpret_cast<f32x4u*>(a.masked + at) = f32x4u{m[0], m[1], m[2], m[3]};
-    } else {
+    if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), q);
+    if (a.masked) put4(a.masked, a, row, id_of(chunk, j, 0), m);
+  }
+  if (!mine) return;
+  // The id inside the chunk, in units of the chunk's own largest weight (it is kept if any of the chunk is), so that there are
+  // some however small the chunk's share is.
+  const float ref = a.w.top[(size_t)row * a.C + chunk].v;
+  u64 start = 0, sums[FL_QUADS], scan[FL_QUADS];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (id + i < a.V) {
-          if (a.q) a.q[at + i] = q[i];
-          if (a.masked) a.masked[at + i] = m[i];
-        }
+  for (int j = 0; j < FL_QUADS; ++j) {
+    u64 s = 0, all;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s += kept >> (j * 4 + i) & 1 ? units(weight(distance(ref, x[j][i], a.mult))) : 0;
+    scan[j] = start + block_scan_u(s, sh, &all);
+    sums[j] = s;
+    start += all;
+  }
+  u64 want = (u64)(fmin(fmax((goal - before) / here, 0.0), 1.0) * (double)start);
+  if (want >= start) want = start - 1;
+#pragma unroll
+  for (int j = 0; j < FL_QUADS; ++j)
+    if (scan[j] <= want && want < scan[j] + sums[j]) {
+      u64 at = scan[j];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const u64 v = kept >> (j * 4 + i) & 1 ? units(weight(distance(ref, x[j][i], a.mult))) : 0;
+        if (at <= want && want < at + v) a.tok[row] = id_of(chunk, j, i);
+        at += v;
+      }
+    }
+}
+
+// ---- few ids --------------------------------------------------------------------------------------------------------
+// The largest of every 16 ids (four lanes' quads), and the results cleared unless they replace the logits.
+__global__ __launch_bounds__(FL_THREADS) void filter_groups_kernel(FilterArgs a, int clear) {
+  const int chunk = blockIdx.x, row = blockIdx.y;
+  float x[FL_QUADS][4];
+  load_chunk(a, row, chunk, x);
+#pragma unroll
+  for (int j = 0; j < FL_QUADS; ++j) {
+    float v = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v = x[j][i] < INFINITY ? fmaxf(v, x[j][i]) : INFINITY;
+    v = fmaxf(v, __shfl_xor(v, 1));
+    v = fmaxf(v, __shfl_xor(v, 2));
+    const int g = id_of(chunk, j, 0) / FL_GROUP;
+    if ((threadIdx.x & 3) == 0 && g < a.G) a.w.group[(size_t)row * a.G + g] = v;
+    if (clear) {
+      const float zero[4] = {0.f, 0.f, 0.f, 0.f}, none[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), zero);
+      if (a.masked) put4(a.masked, a, row, id_of(chunk, j, 0), none);
     }
   }
 }
 
+// One workgroup per row: the groups that may matter, their ids, the borders, the draw and the results.
+#define FL_FEW_LIST 4096
+__global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, int clear) {
+  __shared__ u64 list[FL_FEW_LIST], amount[FL_FEW_LIST], sh[FL_WAVES];
+  __shared__ float shf[FL_WAVES];
+  __shared__ unsigned count[FL_BINS], picked, listed;
+  __shared__ int bin;
+  __shared__ SelectLds lds;
+  int* groups = reinterpret_cast<int*>(amount);    // until the ids are listed
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
+  const float* g = a.w.group + (size_t)row * a.G;
+  const float* x = a.logits + (size_t)row * a.ld;
+  float mx = -INFINITY;
+  for (int i = threadIdx.x; i < a.G; i += FL_THREADS) mx = fmaxf(mx, g[i]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  if (lane == 0) shf[threadIdx.x >> 6] = mx;
+  if (threadIdx.x < FL_BINS) count[threadIdx.x] = 0;
+  if (threadIdx.x == 0) picked = listed = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < FL_WAVES; ++i) mx = fmaxf(mx, shf[i]);
+  if (!(mx < INFINITY) || mx == -INFINITY) {       // no distribution
+    if (threadIdx.x == 0) {
+      if (a.tok) a.tok[row] = -1;
+      a.w.end[row].bad = 1;
+    }
+    if (clear)
+      for (int i = threadIdx.x; i < a.V; i += FL_THREADS) {
+        if (a.q) a.q[(size_t)row * a.V + i] = __builtin_nanf("");
+        if (a.masked) a.masked[(size_t)row * a.V + i] = __builtin_nanf("");
+      }
+    return;
+  }
+  // the class of the k-th largest group; where fewer groups are that near, everything
+  const double line = line_of(mx, a.mult);
+  for (int i = threadIdx.x; i < a.G; i += FL_THREADS) {
+    const int b = class_of(line, g[i], a.mult);
+    if (b < FL_BINS - 1) atomicAdd(&count[b], 1u);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    unsigned n[4], s = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s += count[lane * 4 + i];
+      n[i] = s;
+    }
+    const unsigned b = wave_scan_t(s) - s;
+    int k = 4;
+#pragma unroll
+    for (int i = 3; i >= 0; --i)
+      if (b + n[i] >= (unsigned)a.top_k) k = i;
+    const u64 some = __ballot(k < 4);
+    if (some ? lane == __ffsll((long long)some) - 1 : lane == 0) bin = some ? lane * 4 + k : FL_BINS - 1;
+  }
+  __syncthreads();
+  const int lowest = bin;
+  for (int i = threadIdx.x; i < a.G; i += FL_THREADS)
+    if (class_of(line, g[i], a.mult) <= lowest) {
+      const unsigned at = atomicAdd(&picked, 1u);
+      if (at < 2 * FL_FEW_LIST) groups[at] = i;
+    }
+  __syncthreads();
+  bool whole = picked > 2 * FL_FEW_LIST;           // then every id of the row is looked at
+  if (!whole) {
+    const int n = (int)picked * FL_GROUP;
+    for (int i = threadIdx.x; i < n; i += FL_THREADS) {
+      const int id = groups[i / FL_GROUP] * FL_GROUP + i % FL_GROUP;
+      if (id < a.V && class_of(line, x[id], a.mult) <= lowest) {
+        const unsigned at = atomicAdd(&listed, 1u);
+        if (at < FL_FEW_LIST) list[at] = order_of(x[id], id);
+      }
+    }
+    __syncthreads();
+    whole = listed > FL_FEW_LIST;
+  }
+  const int n = whole ? a.V : (int)listed;
+  if (!whole)
+    for (int i = threadIdx.x; i < n; i += FL_THREADS) amount[i] = units(weight(distance(mx, logit_of(list[i]), a.mult)));
+  __syncthreads();
+  auto candidates = [&](auto use) {                // use(order, units) of every one
+    for (int i = threadIdx.x; i < n; i += FL_THREADS) {
+      if (!whole) use(list[i], amount[i]);
+      else if (class_of(line, x[i], a.mult) <= lowest) use(order_of(x[i], i), units(weight(distance(mx, x[i], a.mult))));
+    }
+  };
+  u64 last = select_key([&](auto visit) { candidates([&](u64 o, u64) { visit(o, 1ull); }); },
+                        [&](u64 s) { return s >= (u64)a.top_k; }, lds);
+  if (a.top_p < 1.0) {
+    u64 m = 0;
+    const u64 upto = last;
+    candidates([&](u64 o, u64 w) { if (o <= upto) m += w; });
+    const double goal = a.top_p * (double)block_sum_t(m, sh);
+    last = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (o <= upto && w) visit(o, w); }); },
+                      [&](u64 s) { return (double)s >= goal; }, lds);
+  }
+  u64 m = 0;
+  auto kept = [&](u64 o) { return o <= last && (a.min_p == 0.0 || weight(distance(mx, logit_of(o), a.mult)) >= a.min_p); };
+  candidates([&](u64 o, u64 w) { if (kept(o)) m += w; });
+  const u64 total = block_sum_t(m, sh);
+  if (a.tok) {
+    u64 goal = (u64)(fmin(fmax((double)a.u[row], 0.0), 1.0) * (double)total);
+    if (goal >= total) goal = total - 1;
+    const u64 id = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (w && kept(o)) visit((u64)(unsigned)o, w); }); },
+                              [&](u64 s) { return s > goal; }, lds);
+    if (threadIdx.x == 0) a.tok[row] = (int)id;
+  }
+  if (!clear) {
+    if (threadIdx.x == 0) {
+      a.w.end[row] = FilterEnd{last, (double)total, 0, 0};
+      a.w.top[row].v = mx;
+    }
+    return;
+  }
+  const double inv = FL_ONE / (double)total;
+  candidates([&](u64 o, u64) {
+    if (!kept(o)) return;
+    const size_t at = (size_t)row * a.V + (unsigned)o;
+    if (a.q) a.q[at] = (float)(weight(distance(mx, logit_of(o), a.mult)) * inv);
+    if (a.masked) a.masked[at] = x[(unsigned)o];
+  });
+}
+
 // ---- the call -------------------------------------------------------------------------------------------------------
 static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
-  const size_t C = (V + FL_CHUNK - 1) / FL_CHUNK, n = rows;
+  const size_t C = (V + FL_CHUNK - 1) / FL_CHUNK, G = (V + FL_GROUP - 1) / FL_GROUP, n = rows;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* p = base + at;
@@ -568,11 +838,14 @@ static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
   w->mass = (u64*)take(n * C * FL_BINS * 8);
   w->list = (u64*)take(n * FL_LIST * 8);
   w->count = (unsigned*)take(n * C * FL_BINS * 4);
-  w->sure = (u64*)take(n * C * 8);
+  w->kept = (double*)take(n * C * 8);
   w->top = (FilterTop*)take(n * C * sizeof(FilterTop));
   w->info = (FilterInfo*)take(n * sizeof(FilterInfo));
   w->end = (FilterEnd*)take(n * sizeof(FilterEnd));
   w->listed = (unsigned*)take(n * 4);
+  w->group = (float*)w->mass;                      // few ids need no classes; C * FL_BINS * 8 >= G * 4
+  static_assert(FL_BINS * 8 >= FL_CHUNK / FL_GROUP * 4, "groups fit in place of the classes' masses");
+  (void)G;
   return at;
 }
 size_t filter_work_bytes(int rows, int V) {
@@ -586,6 +859,7 @@ hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, c
   a.ld = ld;
   a.V = V;
   a.C = (V + FL_CHUNK - 1) / FL_CHUNK;
+  a.G = (V + FL_GROUP - 1) / FL_GROUP;
   a.greedy = s.temperature == 0.0f;
   a.mult = a.greedy ? 1.0 : (double)s.logit_scale / (double)s.temperature;
   a.top_k = s.top_k > 0 && s.top_k < V ? s.top_k : 0;
@@ -596,12 +870,27 @@ hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, c
   a.masked = masked;
   a.tok = tok;
   filter_layout(rows, V, (char*)work, &a.w);
-  const int classes = a.top_k || a.top_p < 1.0;
-  const dim3 grid(a.C, rows);
-  filter_top_kernel<<<grid, FL_THREADS, 0, st>>>(a);
-  if (!a.greedy) filter_bins_kernel<<<grid, FL_THREADS, 0, st>>>(a, classes);
-  if (!a.greedy && classes) filter_collect_kernel<<<grid, FL_THREADS, 0, st>>>(a);
-  filter_resolve_kernel<<<rows, FL_THREADS, 0, st>>>(a, classes);
-  if (q || masked) filter_write_kernel<<<grid, FL_THREADS, 0, st>>>(a);
+  const dim3 grid(a.C, rows), block(FL_THREADS);
+  if (!a.greedy && a.top_k && a.top_k <= FL_FEW) {
+    const int clear = q != logits && masked != logits;
+    filter_groups_kernel<<<grid, block, 0, st>>>(a, clear);
+    filter_few_kernel<<<rows, block, 0, st>>>(a, clear);
+    if (!clear) filter_finish_kernel<<<grid, block, 0, st>>>(a, FINISH_WRITE);
+    return hipGetLastError();
+  }
+  if (!a.greedy && (a.top_k || a.top_p < 1.0)) {
+    const int bytes = 2 * FL_LIST * 8;
+    hipError_t e = hipFuncSetAttribute((const void*)filter_resolve_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    filter_bins_kernel<<<grid, block, 0, st>>>(a);
+    filter_collect_kernel<<<grid, block, 0, st>>>(a);
+    filter_resolve_kernel<<<rows, block, bytes, st>>>(a);
+    filter_finish_kernel<<<grid, block, 0, st>>>(a, FINISH_CLASSES);
+    return hipGetLastError();
+  }
+  const int all = !a.greedy && a.min_p == 0.0;
+  filter_top_kernel<<<grid, block, 0, st>>>(a, all);
+  if (!a.greedy && !all) filter_mass_kernel<<<grid, block, 0, st>>>(a);
+  filter_finish_kernel<<<grid, block, 0, st>>>(a, all ? FINISH_ALL : FINISH_KEPT);
   return hipGetLastError();
 }
