@@ -38,12 +38,6 @@ typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 static_assert(SPEC_SAMPLE_VOCAB_MAX <= 1 << 20, "sums of weights fit 64 bits");
 static_assert(FL_CHUNKS_MAX <= 128, "two chunks per lane");
 
-struct FilterTop {               // of a chunk
-  float v;                       // largest logit ...
-  int id;                        // ... its lowest id
-  int bad, pad;                  // NaN or +inf seen
-  double x;                      // sum of exp(z - this chunk's largest z), or the grid line below its largest z
-};
 struct FilterInfo {              // of a row: borders by classes, masses relative to its largest weight
   int kbin, plo, phi, n_before;  // class of the k-th id; classes that top-p may end in; ids before kbin
   double m_before_k, m_before_p, mass;
@@ -51,10 +45,11 @@ struct FilterInfo {              // of a row: borders by classes, masses relativ
 struct FilterEnd {
   u64 last;                      // order of the last kept id
   double total;                  // units kept
-  int bad, tok;
 };
 struct FilterWork {              // arrays over the rows of a call
-  FilterTop* top;                // [row][C]
+  float* top;                    // [row][C]: largest logit of a chunk; +inf for one with a NaN, unless greedy
+  int* top_id;                   // [row][C]: greedy: its lowest id
+  double* sum;                   // [row][C]: sum of exp(z - the chunk's largest z)
   double* kept;                  // [row][C]: units kept
   u64* mass;                     // [row][C][FL_BINS]
   unsigned* count;               // [row][C][FL_BINS]
@@ -62,7 +57,7 @@ struct FilterWork {              // arrays over the rows of a call
   FilterInfo* info;              // [row]
   FilterEnd* end;                // [row]
   unsigned* listed;              // [row]
-  float* group;                  // [row][G]: +inf for one with a NaN
+  float* group;                  // [row][G]: largest logit of 16 ids, +inf with a NaN
 };
 struct FilterArgs {
   const float* logits;
@@ -113,48 +108,77 @@ __device__ __forceinline__ int class_of(double line, float x, double mult) {
   return b < FL_BINS - 1 ? (int)b : FL_BINS - 1;
 }
 
-// ---- a workgroup ----------------------------------------------------------------------------------------------------
-template <typename T>
-__device__ __forceinline__ T wave_sum_t(T v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+// ---- a wave, a workgroup --------------------------------------------------------------------------------------------
+// Neighbours' values inside rows of 16 lanes and on to the rows behind: no trip through LDS.  `rest` where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp_32(unsigned rest, unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp((int)rest, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T dpp_add(T v) {
+  if constexpr (sizeof(T) == 4) {
+    return v + __builtin_bit_cast(T, dpp_32<CTRL, ROWS>(0u, __builtin_bit_cast(unsigned, v)));
+  } else {
+    const u64 b = __builtin_bit_cast(u64, v);
+    const u64 n = (u64)dpp_32<CTRL, ROWS>(0u, (unsigned)(b >> 32)) << 32 | dpp_32<CTRL, ROWS>(0u, (unsigned)b);
+    return v + __builtin_bit_cast(T, n);
+  }
 }
 template <typename T>
 __device__ __forceinline__ T wave_scan_t(T v) {               // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const T t = __shfl_up(v, o);
-    if (lane >= o) v += t;
-  }
-  return v;
+  v = dpp_add<0x111, 0xf>(v);
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);
+  return dpp_add<0x143, 0xc>(v);
 }
+template <typename T>
+__device__ __forceinline__ T lane_t(T v, int lane) {          // lane: uniform
+  if constexpr (sizeof(T) == 4) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+  } else {
+    const u64 b = __builtin_bit_cast(u64, v);
+    const unsigned hi = __builtin_amdgcn_readlane((int)(b >> 32), lane), lo = __builtin_amdgcn_readlane((int)b, lane);
+    return __builtin_bit_cast(T, (u64)hi << 32 | lo);
+  }
+}
+template <typename T>
+__device__ __forceinline__ T wave_sum_t(T v) { return lane_t(wave_scan_t(v), 63); }
+template <typename T>
+__device__ __forceinline__ T wave_before_t(T scan) {          // the lane before's; 0 in the first
+  const T up = __shfl_up(scan, 1);
+  return (threadIdx.x & 63) ? up : T(0);
+}
+__device__ __forceinline__ float wave_max_f(float v) {
+  const unsigned none = __float_as_uint(-INFINITY);
+  v = fmaxf(v, __uint_as_float(dpp_32<0x111, 0xf>(none, __float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp_32<0x112, 0xf>(none, __float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp_32<0x114, 0xf>(none, __float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp_32<0x118, 0xf>(none, __float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp_32<0x142, 0xa>(none, __float_as_uint(v))));
+  v = fmaxf(v, __uint_as_float(dpp_32<0x143, 0xc>(none, __float_as_uint(v))));
+  return lane_t(v, 63);
+}
+__device__ __forceinline__ unsigned wave_or(unsigned v) {
+  v |= dpp_32<0x111, 0xf>(0u, v);
+  v |= dpp_32<0x112, 0xf>(0u, v);
+  v |= dpp_32<0x114, 0xf>(0u, v);
+  v |= dpp_32<0x118, 0xf>(0u, v);
+  v |= dpp_32<0x142, 0xa>(0u, v);
+  v |= dpp_32<0x143, 0xc>(0u, v);
+  return lane_t(v, 63);
+}
+// sh is free again for whoever has passed one more barrier
 template <typename T>
 __device__ __forceinline__ T block_sum_t(T v, T* sh) {        // to every thread
   v = wave_sum_t(v);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
   T t = 0;
 #pragma unroll
   for (int i = 0; i < FL_WAVES; ++i) t += sh[i];
   return t;
-}
-__device__ __forceinline__ u64 block_scan_u(u64 v, u64* sh, u64* total) {   // exclusive
-  const int w = threadIdx.x >> 6;
-  const u64 s = wave_scan_t(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) sh[w] = s;
-  __syncthreads();
-  u64 before = 0, all = 0;
-#pragma unroll
-  for (int i = 0; i < FL_WAVES; ++i) {
-    if (i == w) before = all;
-    all += sh[i];
-  }
-  *total = all;
-  return before + s - v;
 }
 
 // the chunk's ids j * 2048 + 4 * thread + i; beyond V: -inf, which has no weight and comes last
@@ -186,82 +210,97 @@ __device__ __forceinline__ void put4(float* out, const FilterArgs& a, int row, i
   }
 }
 
-__device__ __forceinline__ FilterTop better(FilterTop a, FilterTop b) {
-  const bool take = b.v > a.v || (b.v == a.v && b.id < a.id);
-  a.v = take ? b.v : a.v;
-  a.id = take ? b.id : a.id;
-  a.bad |= b.bad;
-  return a;
-}
-__device__ __forceinline__ FilterTop wave_better(FilterTop t) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    FilterTop s;
-    s.v = __shfl_xor(t.v, o);
-    s.id = __shfl_xor(t.id, o);
-    s.bad = __shfl_xor(t.bad, o);
-    t = better(t, s);
-  }
-  return t;
-}
-// of the chunk, to every thread; id 0 where nothing is above -inf
-__device__ __forceinline__ FilterTop chunk_top(const FilterArgs& a, int chunk, const float (&x)[FL_QUADS][4], FilterTop* sh) {
-  FilterTop t = {-INFINITY, 0x7fffffff, 0, 0, 0.0};
+// largest logit of the chunk, to every thread; +inf if there is a NaN
+__device__ __forceinline__ float chunk_top(const float (&x)[FL_QUADS][4], float* sh) {
+  float t = -INFINITY;
 #pragma unroll
   for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (x[j][i] > t.v) t.v = x[j][i], t.id = id_of(chunk, j, i);     // a thread's ids ascend; NaN is never larger
-      t.bad |= !(x[j][i] < INFINITY);
-    }
-  t = wave_better(t);
+    for (int i = 0; i < 4; ++i) t = x[j][i] < INFINITY ? fmaxf(t, x[j][i]) : INFINITY;
+  t = wave_max_f(t);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = t;
   __syncthreads();
   t = sh[0];
 #pragma unroll
-  for (int i = 1; i < FL_WAVES; ++i) t = better(t, sh[i]);
-  if (t.id == 0x7fffffff) t.id = 0;
+  for (int i = 1; i < FL_WAVES; ++i) t = fmaxf(t, sh[i]);
   return t;
 }
-struct RowTop { float v; int id; bool none; };                // none: no distribution
-__device__ __forceinline__ RowTop row_top(const FilterArgs& a, int row) {    // by every wave for itself
-  FilterTop t = {-INFINITY, 0, 0, 0, 0.0};
-  for (int c = threadIdx.x & 63; c < a.C; c += 64) t = better(t, a.w.top[(size_t)row * a.C + c]);
-  t = wave_better(t);
-  return RowTop{t.v, t.id, t.bad || t.v == -INFINITY};
+__device__ __forceinline__ bool has_none(float top) { return !(top < INFINITY) || top == -INFINITY; }   // no distribution
+__device__ __forceinline__ float row_top(const FilterArgs& a, int row) {     // by every wave for itself
+  const int lane = threadIdx.x & 63;
+  const float* p = a.w.top + (size_t)row * a.C;
+  float t = lane < a.C ? p[lane] : -INFINITY;
+  if (64 + lane < a.C) t = fmaxf(t, p[64 + lane]);
+  return wave_max_f(t);
 }
 
 // ---- greedy, temperature alone, min-p alone -------------------------------------------------------------------------
 __global__ __launch_bounds__(FL_THREADS) void filter_top_kernel(FilterArgs a, int sum) {
-  __shared__ FilterTop sh[FL_WAVES];
+  __shared__ float sh[FL_WAVES];
   __shared__ double shd[FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
-  FilterTop t = chunk_top(a, chunk, x, sh);
-  if (sum && !t.bad && t.v > -INFINITY) {
+  const float t = chunk_top(x, sh);
+  if (sum && !has_none(t)) {
     double s = 0.0;
 #pragma unroll
     for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s += weight(distance(t.v, x[j][i], a.mult));
-    t.x = block_sum_t(s, shd);
+      for (int i = 0; i < 4; ++i) s += weight(distance(t, x[j][i], a.mult));
+    s = block_sum_t(s, shd);
+    if (threadIdx.x == 0) a.w.sum[(size_t)row * a.C + chunk] = s;
   }
   if (threadIdx.x == 0) a.w.top[(size_t)row * a.C + chunk] = t;
+}
+// the lowest id of the largest logit, NaN counting as none; id 0 where nothing is above -inf
+__global__ __launch_bounds__(FL_THREADS) void filter_greedy_kernel(FilterArgs a) {
+  __shared__ float sh[FL_WAVES];
+  __shared__ int lowest;
+  const int chunk = blockIdx.x, row = blockIdx.y;
+  float x[FL_QUADS][4];
+  load_chunk(a, row, chunk, x);
+  if (threadIdx.x == 0) lowest = 0x7fffffff;
+#pragma unroll
+  for (int j = 0; j < FL_QUADS; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[j][i] = x[j][i] >= -INFINITY ? x[j][i] : -INFINITY;
+  float t = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < FL_QUADS; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = fmaxf(t, x[j][i]);
+  t = wave_max_f(t);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = t;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < FL_WAVES; ++i) t = fmaxf(t, sh[i]);
+  int id = 0x7fffffff;
+#pragma unroll
+  for (int j = FL_QUADS - 1; j >= 0; --j)
+#pragma unroll
+    for (int i = 3; i >= 0; --i)
+      if (x[j][i] == t) id = id_of(chunk, j, i);
+  if (id < 0x7fffffff) atomicMin(&lowest, id);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.w.top[(size_t)row * a.C + chunk] = t;
+    a.w.top_id[(size_t)row * a.C + chunk] = t == -INFINITY ? 0 : lowest;
+  }
 }
 __global__ __launch_bounds__(FL_THREADS) void filter_mass_kernel(FilterArgs a) {
   __shared__ u64 sh[FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
-  const RowTop top = row_top(a, row);
-  if (top.none) return;
+  const float top = row_top(a, row);
+  if (has_none(top)) return;
   u64 sum = 0;
 #pragma unroll
   for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const double w = weight(distance(top.v, x[j][i], a.mult));
+      const double w = weight(distance(top, x[j][i], a.mult));
       if (w >= a.min_p) sum += units(w);
     }
   sum = block_sum_t(sum, sh);
@@ -270,28 +309,28 @@ __global__ __launch_bounds__(FL_THREADS) void filter_mass_kernel(FilterArgs a) {
 
 // ---- classes --------------------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(FL_THREADS) void filter_bins_kernel(FilterArgs a) {
-  __shared__ FilterTop sh[FL_WAVES];
+  __shared__ float sh[FL_WAVES];
   __shared__ u64 mass[FL_BINS];
   __shared__ unsigned count[FL_BINS];
   const int chunk = blockIdx.x, row = blockIdx.y;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
   if (threadIdx.x < FL_BINS) mass[threadIdx.x] = 0, count[threadIdx.x] = 0;
-  FilterTop t = chunk_top(a, chunk, x, sh);
-  t.x = line_of(t.v, a.mult);
+  const float t = chunk_top(x, sh);
   if (threadIdx.x == 0) {
     a.w.top[(size_t)row * a.C + chunk] = t;
     if (chunk == 0) a.w.listed[row] = 0;
   }
-  if (t.bad) return;
-  if (t.v > -INFINITY) {
+  if (!(t < INFINITY)) return;
+  if (t > -INFINITY) {
+    const double line = line_of(t, a.mult);
 #pragma unroll
     for (int j = 0; j < FL_QUADS; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int b = class_of(t.x, x[j][i], a.mult);
+        const int b = class_of(line, x[j][i], a.mult);
         if (a.top_k && b < FL_BINS - 1) atomicAdd(&count[b], 1u);
-        const u64 m = units(weight(distance(t.v, x[j][i], a.mult)));
+        const u64 m = units(weight(distance(t, x[j][i], a.mult)));
         if (m) atomicAdd(&mass[b], m);
       }
   }
@@ -316,10 +355,10 @@ __device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const do
     m[i] = sm;
     n[i] = sn;
   }
-  const double im = wave_scan_t(sm), up = __shfl_up(im, 1), bm = lane ? up : 0.0;
+  const double im = wave_scan_t(sm), bm = wave_before_t(im);
   const unsigned in = wave_scan_t(sn), bn = in - sn;
   FilterInfo f;
-  f.mass = __shfl(im, 63);
+  f.mass = lane_t(im, 63);
   // first class whose inclusive sums `reached` accepts, else the last one, and the sums before it
   auto first = [&](auto reached, double* before_m, int* before_n, double* upto) {
     int k = -1;
@@ -333,10 +372,10 @@ __device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const do
 #pragma unroll
     for (int i = 1; i < 4; ++i)
       if (pick == i) pm = bm + m[i - 1], pn = bn + n[i - 1], um = bm + m[i];
-    *before_m = __shfl(pm, at);
-    *before_n = (int)__shfl(pn, at);
-    *upto = __shfl(um, at);
-    return __shfl(lane * 4 + pick, at);
+    *before_m = lane_t(pm, at);
+    *before_n = (int)lane_t(pn, at);
+    *upto = lane_t(um, at);
+    return lane_t(lane * 4 + pick, at);
   };
   double upto = f.mass, skip_m;
   int skip_n;
@@ -357,34 +396,41 @@ __device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const do
 
 __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a) {
   __shared__ double mass[2][FL_BINS], factor[FL_CHUNKS_MAX];
-  __shared__ unsigned count[2][FL_BINS], base;
+  __shared__ unsigned count[2][FL_BINS], listed[FL_WAVES], base;
   __shared__ int shift[FL_CHUNKS_MAX];
-  __shared__ u64 sh[FL_WAVES];
+  __shared__ u64 sums[FL_WAVES];
   __shared__ FilterInfo info;
-  const int chunk = blockIdx.x, row = blockIdx.y;
+  const int chunk = blockIdx.x, row = blockIdx.y, w = threadIdx.x >> 6;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
-  const RowTop top = row_top(a, row);
-  if (top.none) return;
-  const double line = line_of(top.v, a.mult);
+  const float top = row_top(a, row);
+  if (has_none(top)) return;
+  const double line = line_of(top, a.mult);
   if (threadIdx.x < a.C) {                         // chunk c's classes count from its own largest z, on the same grid
-    const FilterTop t = a.w.top[(size_t)row * a.C + threadIdx.x];
-    const double s = line - t.x;
+    const float t = a.w.top[(size_t)row * a.C + threadIdx.x];
+    const double s = line - line_of(t, a.mult);
     shift[threadIdx.x] = s < FL_BINS ? (int)s : FL_BINS;
-    factor[threadIdx.x] = weight(distance(top.v, t.v, a.mult)) / FL_ONE;
+    factor[threadIdx.x] = weight(distance(top, t, a.mult)) / FL_ONE;
   }
   __syncthreads();
   {
     const int b = threadIdx.x & (FL_BINS - 1), half = threadIdx.x / FL_BINS;
+    const size_t rows = (size_t)row * a.C * FL_BINS;
     double m = 0.0;
     unsigned n = 0;
-#pragma unroll 4
-    for (int c = half; c < a.C; c += FL_THREADS / FL_BINS) {
-      const int from = b - shift[c];
-      if (from >= 0) {
-        const size_t at = ((size_t)row * a.C + c) * FL_BINS + from;
-        m += (double)a.w.mass[at] * factor[c];
-        if (a.top_k) n += a.w.count[at];
+    for (int c = half; c < a.C; c += 16) {         // eight chunks' loads at a time
+      u64 v[8];
+      unsigned k[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int d = c + 2 * i, from = d < a.C ? b - shift[d] : -1;
+        v[i] = from >= 0 ? a.w.mass[rows + (size_t)d * FL_BINS + from] : 0;
+        k[i] = a.top_k && from >= 0 ? a.w.count[rows + (size_t)d * FL_BINS + from] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (c + 2 * i < a.C) m += (double)v[i] * factor[c + 2 * i];
+        n += k[i];
       }
     }
     mass[half][b] = m;
@@ -413,17 +459,27 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
     for (int i = 0; i < 4; ++i) {
       const int b = class_of(line, x[j][i], a.mult);
       if (b < sure_below) {
-        const double w = weight(distance(top.v, x[j][i], a.mult));
-        if (w >= a.min_p) sum += units(w);
+        const double v = weight(distance(top, x[j][i], a.mult));
+        if (v >= a.min_p) sum += units(v);
       }
       if (id_of(chunk, j, i) < a.V && (b == kbin || (b >= plo && b <= phi))) mine |= 1u << (j * 4 + i);
     }
-  sum = block_sum_t(sum, sh);
-  u64 n;
-  u64 at = block_scan_u(__popc(mine), sh, &n);
+  sum = wave_sum_t(sum);
+  const unsigned n = __popc(mine), in = wave_scan_t(n);
+  if ((threadIdx.x & 63) == 63) sums[w] = sum, listed[w] = in;
+  __syncthreads();
+  unsigned at = in - n, all = 0;
+#pragma unroll
+  for (int i = 0; i < FL_WAVES; ++i) {
+    if (i == w) at += all;
+    all += listed[i];
+  }
   if (threadIdx.x == 0) {
+    base = all ? atomicAdd(&a.w.listed[row], all) : 0;
+    sum = 0;
+#pragma unroll
+    for (int i = 0; i < FL_WAVES; ++i) sum += sums[i];
     a.w.kept[(size_t)row * a.C + chunk] = (double)sum;
-    base = n ? atomicAdd(&a.w.listed[row], (unsigned)n) : 0;
   }
   __syncthreads();
   at += base;
@@ -439,73 +495,83 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
 
 // Of the keys that each(visit(key, amount)) goes through (amount > 0, every key once), the one at which the running sum of the
 // amounts, by rising key, is first accepted by reached(sum); the last key, should none be; 0 without keys.  Digits of 8 bits from
-// the highest bit in which the keys still in question differ; done when one is left.
-struct SelectLds { u64 hist[256], lo[FL_WAVES], hi[FL_WAVES], pick[2]; };
+// the highest bit in which a key differs from `like`; done when one key is left.
+struct SelectLds {
+  u64 hist[2][256], before, key;
+  unsigned count[2][256], differ[2][FL_WAVES], pick, left;
+};
 template <typename E, typename R>
-__device__ u64 select_key(const E& each, const R& reached, SelectLds& s) {
-  u64 first = 0, last = ~0ull, before = 0;         // keys in question, sum of what comes before them
-  while (true) {
-    u64 lo = ~0ull, hi = 0;
-    each([&](u64 k, u64) {
-      if (k >= first && k <= last) lo = k < lo ? k : lo, hi = k > hi ? k : hi;
-    });
+__device__ u64 select_key(const E& each, const R& reached, u64 like, SelectLds& s) {
+  const int lane = threadIdx.x & 63;
+  u64 differ = 0;
+  each([&](u64 k, u64) { differ |= k ^ like; });
+  {
+    const unsigned h = wave_or((unsigned)(differ >> 32)), l = wave_or((unsigned)differ);
+    if (lane == 0) s.differ[0][threadIdx.x >> 6] = h, s.differ[1][threadIdx.x >> 6] = l;
+  }
+  for (int i = threadIdx.x; i < 256; i += FL_THREADS) s.hist[0][i] = 0, s.count[0][i] = 0;
+  if (threadIdx.x == 0) s.key = 0;
+  __syncthreads();
+  differ = 0;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const u64 l = __shfl_xor(lo, o), h = __shfl_xor(hi, o);
-      lo = l < lo ? l : lo;
-      hi = h > hi ? h : hi;
-    }
-    if ((threadIdx.x & 63) == 0) s.lo[threadIdx.x >> 6] = lo, s.hi[threadIdx.x >> 6] = hi;
-    if (threadIdx.x < 256) s.hist[threadIdx.x] = 0;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < FL_WAVES; ++i) {
-      lo = s.lo[i] < lo ? s.lo[i] : lo;
-      hi = s.hi[i] > hi ? s.hi[i] : hi;
-    }
-    if (lo >= hi) {
-      __syncthreads();
-      return lo > hi ? 0 : lo;
-    }
-    const int top = 63 - __clzll((long long)(lo ^ hi)), shift = top > 7 ? top - 7 : 0;
+  for (int i = 0; i < FL_WAVES; ++i) differ |= (u64)s.differ[0][i] << 32 | s.differ[1][i];
+  int shift = differ >> 8 ? 56 - __clzll((long long)differ) : 0;
+  // the keys in question, and the sum of what comes before them
+  u64 first = shift == 56 ? 0 : like >> (shift + 8) << (shift + 8), last = shift == 56 ? ~0ull : first | ((1ull << (shift + 8)) - 1);
+  u64 before = 0;
+  for (int b = 0;; b ^= 1) {
     each([&](u64 k, u64 amount) {
-      if (k >= first && k <= last) atomicAdd(&s.hist[(k >> shift) & 255], amount);
+      if (k >= first && k <= last) {
+        atomicAdd(&s.hist[b][k >> shift & 255], amount);
+        atomicAdd(&s.count[b][k >> shift & 255], 1u);
+      }
     });
     __syncthreads();
     if (threadIdx.x < 64) {
-      const int lane = threadIdx.x;
       u64 h[4], sum = 0;
+      unsigned c[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sum += s.hist[lane * 4 + i];
+        sum += s.hist[b][lane * 4 + i];
         h[i] = sum;
+        c[i] = s.count[b][lane * 4 + i];
       }
-      const u64 b = before + wave_scan_t(sum) - sum;
+      const u64 start = before + wave_scan_t(sum) - sum;
       int k = -1, some = -1;
 #pragma unroll
       for (int i = 3; i >= 0; --i) {
-        const bool any = h[i] != (i ? h[i - 1] : 0);
-        if (any && some < 0) some = i;
-        if (any && reached(b + h[i])) k = i;
+        if (c[i] && some < 0) some = i;
+        if (c[i] && reached(start + h[i])) k = i;
       }
       const u64 good = __ballot(k >= 0), filled = __ballot(some >= 0);
-      const int at = good ? __ffsll((long long)good) - 1 : 63 - __clzll((long long)filled), pick = good ? k : some;
-      u64 pm = b;
+      const int at = good ? __ffsll((long long)good) - 1 : filled ? 63 - __clzll((long long)filled) : 0, pick = good ? k : some < 0 ? 0 : some;
+      u64 pm = start;
+      unsigned n = c[0];
 #pragma unroll
       for (int i = 1; i < 4; ++i)
-        if (pick == i) pm = b + h[i - 1];
-      if (lane == at) s.pick[0] = lane * 4 + pick, s.pick[1] = pm;
+        if (pick == i) pm = start + h[i - 1], n = c[i];
+      if (lane == at) s.pick = lane * 4 + pick, s.before = pm, s.left = n;
+    } else if (threadIdx.x >= FL_THREADS - 256) {
+      s.hist[b ^ 1][threadIdx.x - (FL_THREADS - 256)] = 0;
+      s.count[b ^ 1][threadIdx.x - (FL_THREADS - 256)] = 0;
     }
     __syncthreads();
-    // the keys share the bits above `top`, and top is bit shift + 7, so the digit has them all in order
-    first = (lo >> shift & ~255ull | s.pick[0]) << shift;
+    first = (first >> shift & ~255ull | s.pick) << shift;
     last = first | ((1ull << shift) - 1);
-    before = s.pick[1];
-    if (shift == 0) {
+    before = s.before;
+    if (shift == 0) break;
+    if (s.left <= 1) {                             // the one key of this digit
+      each([&](u64 k, u64) {
+        if (k >= first && k <= last) s.key = k;
+      });
       __syncthreads();
-      return first;
+      first = s.key;
+      break;
     }
+    shift = shift > 8 ? shift - 8 : 0;
   }
+  __syncthreads();
+  return first;
 }
 
 // The border of a row among its candidates: the list, or where it did not hold them the row itself.
@@ -515,10 +581,11 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
   __shared__ u64 sh[FL_WAVES], chunk_mass[FL_CHUNKS_MAX];
   __shared__ SelectLds lds;
   const int row = blockIdx.x;
-  const RowTop top = row_top(a, row);
-  if (top.none) return;
+  const float top = row_top(a, row);
+  if (has_none(top)) return;
   const FilterInfo f = a.w.info[row];
-  const double line = line_of(top.v, a.mult);
+  const double line = line_of(top, a.mult);
+  const u64 like = order_of(top, 0);
   const float* x = a.logits + (size_t)row * a.ld;
   const unsigned listed = a.w.listed[row];
   const bool whole = listed > FL_LIST;
@@ -528,7 +595,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
     for (int i = threadIdx.x; i < n; i += FL_THREADS) {
       const u64 o = a.w.list[(size_t)row * FL_LIST + i];
       list[i] = o;
-      amount[i] = units(weight(distance(top.v, logit_of(o), a.mult)));
+      amount[i] = units(weight(distance(top, logit_of(o), a.mult)));
     }
   __syncthreads();
   // use(order, class, units) of every candidate
@@ -537,7 +604,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
       const float v = whole ? x[i] : logit_of(list[i]);
       const int b = class_of(line, v, a.mult);
       if (!whole) use(list[i], b, amount[i]);
-      else if (b == f.kbin || (b >= f.plo && b <= f.phi)) use(order_of(v, i), b, units(weight(distance(top.v, v, a.mult))));
+      else if (b == f.kbin || (b >= f.plo && b <= f.phi)) use(order_of(v, i), b, units(weight(distance(top, v, a.mult))));
     }
   };
   u64 last = ~0ull;
@@ -545,7 +612,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
   if (a.top_k) {
     const u64 rank = (u64)(a.top_k - f.n_before);
     last = select_key([&](auto visit) { candidates([&](u64 o, int b, u64) { if (b == f.kbin) visit(o, 1ull); }); },
-                      [&](u64 s) { return s >= rank; }, lds);
+                      [&](u64 s) { return s >= rank; }, like, lds);
     u64 m = 0;
     candidates([&](u64 o, int b, u64 w) { if (b == f.kbin && o <= last) m += w; });
     mass_k = f.m_before_k + (double)block_sum_t(m, sh) / FL_ONE;
@@ -554,10 +621,10 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
     const double goal = (a.top_p * mass_k - f.m_before_p) * FL_ONE;
     const u64 upto = last;
     last = select_key([&](auto visit) { candidates([&](u64 o, int b, u64 w) { if (b >= f.plo && b <= f.phi && o <= upto && w) visit(o, w); }); },
-                      [&](u64 s) { return (double)s >= goal; }, lds);
+                      [&](u64 s) { return (double)s >= goal; }, like, lds);
   }
   candidates([&](u64 o, int, u64 w) {
-    if (o <= last && weight(distance(top.v, logit_of(o), a.mult)) >= a.min_p && w) atomicAdd(&chunk_mass[(unsigned)o / FL_CHUNK], w);
+    if (o <= last && weight(distance(top, logit_of(o), a.mult)) >= a.min_p && w) atomicAdd(&chunk_mass[(unsigned)o / FL_CHUNK], w);
   });
   __syncthreads();
   for (int c = threadIdx.x; c < a.C; c += FL_THREADS) a.w.kept[(size_t)row * a.C + c] += (double)chunk_mass[c];
@@ -568,19 +635,26 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
 enum { FINISH_ALL = 0 /* nothing truncated but by min-p = 0 */, FINISH_KEPT = 1 /* masses of the chunks */, FINISH_CLASSES = 2 /* and a border */,
        FINISH_WRITE = 3 /* border, total and token are there */ };
 __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a, int mode) {
-  __shared__ u64 sh[FL_WAVES];
+  __shared__ u64 sums[FL_QUADS][FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
   float x[FL_QUADS][4];
   load_chunk(a, row, chunk, x);
-  const RowTop top = mode == FINISH_WRITE ? RowTop{a.w.top[row].v, 0, a.w.end[row].bad != 0} : row_top(a, row);
-  if (a.greedy || top.none) {
-    if (a.tok && chunk == 0 && threadIdx.x == 0 && mode != FINISH_WRITE) a.tok[row] = a.greedy ? top.id : -1;
+  const float top = mode == FINISH_WRITE ? a.w.top[(size_t)row * a.C] : row_top(a, row);
+  if (a.greedy || has_none(top)) {
+    int best = 0;
+    if (a.greedy) {                                // the lowest chunk that has the largest logit
+      const int* ids = a.w.top_id + (size_t)row * a.C;
+      const float* tops = a.w.top + (size_t)row * a.C;
+      const u64 low = __ballot(lane < a.C && tops[lane] == top), high = __ballot(64 + lane < a.C && tops[64 + lane] == top);
+      best = ids[low ? __ffsll((long long)low) - 1 : high ? 63 + __ffsll((long long)high) : 0];
+    }
+    if (a.tok && chunk == 0 && threadIdx.x == 0 && mode != FINISH_WRITE) a.tok[row] = a.greedy ? best : -1;
 #pragma unroll
     for (int j = 0; j < FL_QUADS; ++j) {
       float q[4], m[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool on = id_of(chunk, j, i) == top.id;
+        const bool on = id_of(chunk, j, i) == best;
         q[i] = !a.greedy ? __builtin_nanf("") : on ? 1.0f : 0.0f;
         m[i] = !a.greedy ? __builtin_nanf("") : on ? x[j][i] : -INFINITY;
       }
@@ -605,10 +679,10 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
       const int c = lane * 2 + i;
       const size_t at = (size_t)row * a.C + c;
       m[i] = 0.0;
-      if (c < a.C) m[i] = mode == FINISH_ALL ? a.w.top[at].x * weight(distance(top.v, a.w.top[at].v, a.mult)) * FL_ONE : a.w.kept[at];
+      if (c < a.C) m[i] = mode == FINISH_ALL ? (a.w.top[at] > -INFINITY ? a.w.sum[at] * weight(distance(top, a.w.top[at], a.mult)) * FL_ONE : 0.0) : a.w.kept[at];
     }
-    const double in = wave_scan_t(m[0] + m[1]), up = __shfl_up(in, 1), ex = lane ? up : 0.0;
-    total = __shfl(in, 63);
+    const double in = wave_scan_t(m[0] + m[1]), ex = wave_before_t(in);
+    total = lane_t(in, 63);
     if (a.tok) {
       goal = fmin(fmax((double)a.u[row], 0.0), 1.0) * total;
       // the first chunk whose running sum passes the goal, else the last one with any mass
@@ -623,8 +697,8 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
         c = l1 >= l0 ? l1 * 2 + 1 : l0 * 2;
       }
       mine = c == chunk;
-      before = __shfl(chunk & 1 ? ex + m[0] : ex, chunk >> 1);
-      here = __shfl(chunk & 1 ? m[1] : m[0], chunk >> 1);
+      before = lane_t(chunk & 1 ? ex + m[0] : ex, chunk >> 1);
+      here = lane_t(chunk & 1 ? m[1] : m[0], chunk >> 1);
     }
   }
   if (!a.q && !a.masked && !mine) return;
@@ -639,7 +713,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
       q[i] = 0.0f;
       m[i] = -INFINITY;
       if (id < a.V && (last == ~0ull || order_of(x[j][i], id) <= last)) {
-        const double w = weight(distance(top.v, x[j][i], a.mult));
+        const double w = weight(distance(top, x[j][i], a.mult));
         if (w >= a.min_p) {
           kept |= 1u << (j * 4 + i);
           q[i] = (float)(w * inv);
@@ -653,22 +727,29 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
   if (!mine) return;
   // The id inside the chunk, in units of the chunk's own largest weight (it is kept if any of the chunk is), so that there are
   // some however small the chunk's share is.
-  const float ref = a.w.top[(size_t)row * a.C + chunk].v;
-  u64 start = 0, sums[FL_QUADS], scan[FL_QUADS];
+  const float ref = a.w.top[(size_t)row * a.C + chunk];
+  u64 start = 0, own[FL_QUADS], scan[FL_QUADS];
 #pragma unroll
   for (int j = 0; j < FL_QUADS; ++j) {
-    u64 s = 0, all;
+    own[j] = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s += kept >> (j * 4 + i) & 1 ? units(weight(distance(ref, x[j][i], a.mult))) : 0;
-    scan[j] = start + block_scan_u(s, sh, &all);
-    sums[j] = s;
-    start += all;
+    for (int i = 0; i < 4; ++i) own[j] += kept >> (j * 4 + i) & 1 ? units(weight(distance(ref, x[j][i], a.mult))) : 0;
+    scan[j] = wave_scan_t(own[j]);
+    if (lane == 63) sums[j][threadIdx.x >> 6] = scan[j];
   }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < FL_QUADS; ++j)
+#pragma unroll
+    for (int i = 0; i < FL_WAVES; ++i) {
+      if (i == (int)(threadIdx.x >> 6)) scan[j] += start - own[j];       // exclusive, from the chunk's first id on
+      start += sums[j][i];
+    }
   u64 want = (u64)(fmin(fmax((goal - before) / here, 0.0), 1.0) * (double)start);
   if (want >= start) want = start - 1;
 #pragma unroll
   for (int j = 0; j < FL_QUADS; ++j)
-    if (scan[j] <= want && want < scan[j] + sums[j]) {
+    if (scan[j] <= want && want < scan[j] + own[j]) {
       u64 at = scan[j];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -693,7 +774,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_groups_kernel(FilterArgs a,
     v = fmaxf(v, __shfl_xor(v, 1));
     v = fmaxf(v, __shfl_xor(v, 2));
     const int g = id_of(chunk, j, 0) / FL_GROUP;
-    if ((threadIdx.x & 3) == 0 && g < a.G) a.w.group[(size_t)row * a.G + g] = v;
+    if ((threadIdx.x & 3) == 0) a.w.group[(size_t)row * a.G + g] = v;
     if (clear) {
       const float zero[4] = {0.f, 0.f, 0.f, 0.f}, none[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), zero);
@@ -714,20 +795,37 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const float* g = a.w.group + (size_t)row * a.G;
   const float* x = a.logits + (size_t)row * a.ld;
-  float mx = -INFINITY;
-  for (int i = threadIdx.x; i < a.G; i += FL_THREADS) mx = fmaxf(mx, g[i]);
+  // use(group, largest logit) of all of them, sixteen loads of a thread at a time
+  auto all_groups = [&](auto use) {
+    for (int i0 = threadIdx.x * 4; i0 < a.G; i0 += FL_THREADS * 16) {
+      f32x4 v[4];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * FL_THREADS * 4;
+        if (i < a.G) v[k] = *reinterpret_cast<const f32x4*>(g + i);       // rows of groups are padded to fours
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int i = i0 + k * FL_THREADS * 4 + e;
+          if (i < a.G) use(i, v[k][e]);
+        }
+    }
+  };
+  float mx = -INFINITY;
+  all_groups([&](int, float v) { mx = fmaxf(mx, v); });
+  mx = wave_max_f(mx);
   if (lane == 0) shf[threadIdx.x >> 6] = mx;
   if (threadIdx.x < FL_BINS) count[threadIdx.x] = 0;
   if (threadIdx.x == 0) picked = listed = 0;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < FL_WAVES; ++i) mx = fmaxf(mx, shf[i]);
-  if (!(mx < INFINITY) || mx == -INFINITY) {       // no distribution
+  if (has_none(mx)) {
     if (threadIdx.x == 0) {
       if (a.tok) a.tok[row] = -1;
-      a.w.end[row].bad = 1;
+      a.w.top[(size_t)row * a.C] = INFINITY;
     }
     if (clear)
       for (int i = threadIdx.x; i < a.V; i += FL_THREADS) {
@@ -738,10 +836,10 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   }
   // the class of the k-th largest group; where fewer groups are that near, everything
   const double line = line_of(mx, a.mult);
-  for (int i = threadIdx.x; i < a.G; i += FL_THREADS) {
-    const int b = class_of(line, g[i], a.mult);
+  all_groups([&](int, float v) {
+    const int b = class_of(line, v, a.mult);
     if (b < FL_BINS - 1) atomicAdd(&count[b], 1u);
-  }
+  });
   __syncthreads();
   if (threadIdx.x < 64) {
     unsigned n[4], s = 0;
@@ -760,21 +858,39 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   }
   __syncthreads();
   const int lowest = bin;
-  for (int i = threadIdx.x; i < a.G; i += FL_THREADS)
-    if (class_of(line, g[i], a.mult) <= lowest) {
+  all_groups([&](int i, float v) {
+    if (class_of(line, v, a.mult) <= lowest) {
       const unsigned at = atomicAdd(&picked, 1u);
       if (at < 2 * FL_FEW_LIST) groups[at] = i;
     }
+  });
   __syncthreads();
   bool whole = picked > 2 * FL_FEW_LIST;           // then every id of the row is looked at
   if (!whole) {
-    const int n = (int)picked * FL_GROUP;
-    for (int i = threadIdx.x; i < n; i += FL_THREADS) {
-      const int id = groups[i / FL_GROUP] * FL_GROUP + i % FL_GROUP;
-      if (id < a.V && class_of(line, x[id], a.mult) <= lowest) {
-        const unsigned at = atomicAdd(&listed, 1u);
-        if (at < FL_FEW_LIST) list[at] = order_of(x[id], id);
+    const int n = (int)picked * 4;                 // quads, four loads of a thread at a time
+    for (int i0 = threadIdx.x; i0 < n; i0 += FL_THREADS * 4) {
+      f32x4 v[4];
+      int id[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * FL_THREADS;
+        id[k] = i < n ? groups[i >> 2] * FL_GROUP + (i & 3) * 4 : a.V;
+        if (id[k] + 4 <= a.V) {
+          v[k] = *reinterpret_cast<const f32x4u*>(x + id[k]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (id[k] + e < a.V) v[k][e] = x[id[k] + e];
+        }
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (id[k] + e < a.V && class_of(line, v[k][e], a.mult) <= lowest) {
+            const unsigned at = atomicAdd(&listed, 1u);
+            if (at < FL_FEW_LIST) list[at] = order_of(v[k][e], id[k] + e);
+          }
     }
     __syncthreads();
     whole = listed > FL_FEW_LIST;
@@ -789,15 +905,17 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
       else if (class_of(line, x[i], a.mult) <= lowest) use(order_of(x[i], i), units(weight(distance(mx, x[i], a.mult))));
     }
   };
+  const u64 like = order_of(mx, 0);
   u64 last = select_key([&](auto visit) { candidates([&](u64 o, u64) { visit(o, 1ull); }); },
-                        [&](u64 s) { return s >= (u64)a.top_k; }, lds);
+                        [&](u64 s) { return s >= (u64)a.top_k; }, like, lds);
   if (a.top_p < 1.0) {
     u64 m = 0;
     const u64 upto = last;
     candidates([&](u64 o, u64 w) { if (o <= upto) m += w; });
     const double goal = a.top_p * (double)block_sum_t(m, sh);
     last = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (o <= upto && w) visit(o, w); }); },
-                      [&](u64 s) { return (double)s >= goal; }, lds);
+                      [&](u64 s) { return (double)s >= goal; }, like, lds);
+    __syncthreads();
   }
   u64 m = 0;
   auto kept = [&](u64 o) { return o <= last && (a.min_p == 0.0 || weight(distance(mx, logit_of(o), a.mult)) >= a.min_p); };
@@ -807,13 +925,13 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
     u64 goal = (u64)(fmin(fmax((double)a.u[row], 0.0), 1.0) * (double)total);
     if (goal >= total) goal = total - 1;
     const u64 id = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (w && kept(o)) visit((u64)(unsigned)o, w); }); },
-                              [&](u64 s) { return s > goal; }, lds);
+                              [&](u64 s) { return s > goal; }, 0, lds);
     if (threadIdx.x == 0) a.tok[row] = (int)id;
   }
   if (!clear) {
     if (threadIdx.x == 0) {
-      a.w.end[row] = FilterEnd{last, (double)total, 0, 0};
-      a.w.top[row].v = mx;
+      a.w.end[row] = FilterEnd{last, (double)total};
+      a.w.top[(size_t)row * a.C] = mx;
     }
     return;
   }
@@ -828,7 +946,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
 
 // ---- the call -------------------------------------------------------------------------------------------------------
 static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
-  const size_t C = (V + FL_CHUNK - 1) / FL_CHUNK, G = (V + FL_GROUP - 1) / FL_GROUP, n = rows;
+  const size_t C = (V + FL_CHUNK - 1) / FL_CHUNK, n = rows;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* p = base + at;
@@ -839,13 +957,14 @@ static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
   w->list = (u64*)take(n * FL_LIST * 8);
   w->count = (unsigned*)take(n * C * FL_BINS * 4);
   w->kept = (double*)take(n * C * 8);
-  w->top = (FilterTop*)take(n * C * sizeof(FilterTop));
+  w->top = (float*)take(n * C * 4);
+  w->top_id = (int*)take(n * C * 4);
+  w->sum = (double*)take(n * C * 8);
   w->info = (FilterInfo*)take(n * sizeof(FilterInfo));
   w->end = (FilterEnd*)take(n * sizeof(FilterEnd));
   w->listed = (unsigned*)take(n * 4);
   w->group = (float*)w->mass;                      // few ids need no classes; C * FL_BINS * 8 >= G * 4
   static_assert(FL_BINS * 8 >= FL_CHUNK / FL_GROUP * 4, "groups fit in place of the classes' masses");
-  (void)G;
   return at;
 }
 size_t filter_work_bytes(int rows, int V) {
@@ -859,7 +978,7 @@ hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, c
   a.ld = ld;
   a.V = V;
   a.C = (V + FL_CHUNK - 1) / FL_CHUNK;
-  a.G = (V + FL_GROUP - 1) / FL_GROUP;
+  a.G = a.C * (FL_CHUNK / FL_GROUP);                // whole chunks of them
   a.greedy = s.temperature == 0.0f;
   a.mult = a.greedy ? 1.0 : (double)s.logit_scale / (double)s.temperature;
   a.top_k = s.top_k > 0 && s.top_k < V ? s.top_k : 0;
@@ -889,7 +1008,8 @@ hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, c
     return hipGetLastError();
   }
   const int all = !a.greedy && a.min_p == 0.0;
-  filter_top_kernel<<<grid, block, 0, st>>>(a, all);
+  if (a.greedy) filter_greedy_kernel<<<grid, block, 0, st>>>(a);
+  else filter_top_kernel<<<grid, block, 0, st>>>(a, all);
   if (!a.greedy && !all) filter_mass_kernel<<<grid, block, 0, st>>>(a);
   filter_finish_kernel<<<grid, block, 0, st>>>(a, all ? FINISH_ALL : FINISH_KEPT);
   return hipGetLastError();
