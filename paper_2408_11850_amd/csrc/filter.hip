@@ -8,7 +8,7 @@
 // they are integers, in units of 2^-43 (2^20 of them fit 64 bits): the same sum in whatever order; all other sums have a fixed
 // order.
 //
-// A row is cut into chunks of 8192 ids (a workgroup each), so that few rows use many compute units.  By what is asked for:
+// A row is cut into chunks of 2048 to 8192 ids (a workgroup each), so that few rows use many compute units.  By what is asked for:
 //   greedy, or temperature alone   top (a chunk's largest logit, sum of weights), finish
 //   min-p alone                    top, mass (what a chunk keeps), finish
 //   top-k up to 1024 ids           groups (largest logit of every 16 ids), few.  The k-th largest group is no more than the k-th
@@ -24,9 +24,9 @@
 
 #define FL_THREADS 512
 #define FL_WAVES (FL_THREADS / 64)
-#define FL_CHUNK 8192                     // ids of a chunk: 16 per thread, 4 neighbours at a time
-#define FL_QUADS (FL_CHUNK / FL_THREADS / 4)
-#define FL_CHUNKS_MAX (SPEC_SAMPLE_VOCAB_MAX / FL_CHUNK)
+#define FL_QUAD (FL_THREADS * 4)           // ids that a workgroup takes at a time, 4 neighbours per thread
+#define FL_QUADS_MAX 4                     // of them in a chunk: 1, 2 or 4
+#define FL_CHUNKS_MAX (SPEC_SAMPLE_VOCAB_MAX / (FL_QUAD * FL_QUADS_MAX))
 #define FL_BINS 256
 #define FL_GRID 8.0                       // classes per unit of z
 #define FL_LIST 8192                      // candidates that are kept as a list; beyond, the row is read again
@@ -62,7 +62,7 @@ struct FilterWork {              // arrays over the rows of a call
 struct FilterArgs {
   const float* logits;
   size_t ld;
-  int V, C, G, greedy, top_k;    // top_k 0: off
+  int V, chunk, C, G, greedy, top_k;    // ids of a chunk, chunks, groups; top_k 0: off
   double mult, top_p, min_p;     // top_p 1: off
   const float* u;
   float *q, *masked;
@@ -182,11 +182,14 @@ __device__ __forceinline__ T block_sum_t(T v, T* sh) {        // to every thread
 }
 
 // the chunk's ids j * 2048 + 4 * thread + i; beyond V: -inf, which has no weight and comes last
-__device__ __forceinline__ void load_chunk(const FilterArgs& a, int row, int chunk, float (&x)[FL_QUADS][4]) {
+template <int Q>
+__device__ __forceinline__ int id_of(int chunk, int j, int i) { return (chunk * Q + j) * FL_QUAD + threadIdx.x * 4 + i; }
+template <int Q>
+__device__ __forceinline__ void load_chunk(const FilterArgs& a, int row, int chunk, float (&x)[Q][4]) {
   const float* p = a.logits + (size_t)row * a.ld;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j) {
-    const int id = chunk * FL_CHUNK + j * FL_THREADS * 4 + threadIdx.x * 4;
+  for (int j = 0; j < Q; ++j) {
+    const int id = id_of<Q>(chunk, j, 0);
     if (id + 4 <= a.V) {
       const f32x4u v = *reinterpret_cast<const f32x4u*>(p + id);
 #pragma unroll
@@ -197,7 +200,6 @@ __device__ __forceinline__ void load_chunk(const FilterArgs& a, int row, int chu
     }
   }
 }
-__device__ __forceinline__ int id_of(int chunk, int j, int i) { return chunk * FL_CHUNK + j * FL_THREADS * 4 + threadIdx.x * 4 + i; }
 // four results from the id of i = 0 on
 __device__ __forceinline__ void put4(float* out, const FilterArgs& a, int row, int id, const float (&v)[4]) {
   float* p = out + (size_t)row * a.V + id;
@@ -211,10 +213,11 @@ __device__ __forceinline__ void put4(float* out, const FilterArgs& a, int row, i
 }
 
 // largest logit of the chunk, to every thread; +inf if there is a NaN
-__device__ __forceinline__ float chunk_top(const float (&x)[FL_QUADS][4], float* sh) {
+template <int Q>
+__device__ __forceinline__ float chunk_top(const float (&x)[Q][4], float* sh) {
   float t = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) t = x[j][i] < INFINITY ? fmaxf(t, x[j][i]) : INFINITY;
   t = wave_max_f(t);
@@ -235,17 +238,18 @@ __device__ __forceinline__ float row_top(const FilterArgs& a, int row) {     // 
 }
 
 // ---- greedy, temperature alone, min-p alone -------------------------------------------------------------------------
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_top_kernel(FilterArgs a, int sum) {
   __shared__ float sh[FL_WAVES];
   __shared__ double shd[FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
   const float t = chunk_top(x, sh);
   if (sum && !has_none(t)) {
     double s = 0.0;
 #pragma unroll
-    for (int j = 0; j < FL_QUADS; ++j)
+    for (int j = 0; j < Q; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) s += weight(distance(t, x[j][i], a.mult));
     s = block_sum_t(s, shd);
@@ -254,20 +258,21 @@ __global__ __launch_bounds__(FL_THREADS) void filter_top_kernel(FilterArgs a, in
   if (threadIdx.x == 0) a.w.top[(size_t)row * a.C + chunk] = t;
 }
 // the lowest id of the largest logit, NaN counting as none; id 0 where nothing is above -inf
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_greedy_kernel(FilterArgs a) {
   __shared__ float sh[FL_WAVES];
   __shared__ int lowest;
   const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
   if (threadIdx.x == 0) lowest = 0x7fffffff;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[j][i] = x[j][i] >= -INFINITY ? x[j][i] : -INFINITY;
   float t = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) t = fmaxf(t, x[j][i]);
   t = wave_max_f(t);
@@ -277,10 +282,10 @@ __global__ __launch_bounds__(FL_THREADS) void filter_greedy_kernel(FilterArgs a)
   for (int i = 0; i < FL_WAVES; ++i) t = fmaxf(t, sh[i]);
   int id = 0x7fffffff;
 #pragma unroll
-  for (int j = FL_QUADS - 1; j >= 0; --j)
+  for (int j = Q - 1; j >= 0; --j)
 #pragma unroll
     for (int i = 3; i >= 0; --i)
-      if (x[j][i] == t) id = id_of(chunk, j, i);
+      if (x[j][i] == t) id = id_of<Q>(chunk, j, i);
   if (id < 0x7fffffff) atomicMin(&lowest, id);
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -288,16 +293,17 @@ __global__ __launch_bounds__(FL_THREADS) void filter_greedy_kernel(FilterArgs a)
     a.w.top_id[(size_t)row * a.C + chunk] = t == -INFINITY ? 0 : lowest;
   }
 }
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_mass_kernel(FilterArgs a) {
   __shared__ u64 sh[FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
   const float top = row_top(a, row);
   if (has_none(top)) return;
   u64 sum = 0;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const double w = weight(distance(top, x[j][i], a.mult));
@@ -308,12 +314,13 @@ __global__ __launch_bounds__(FL_THREADS) void filter_mass_kernel(FilterArgs a) {
 }
 
 // ---- classes --------------------------------------------------------------------------------------------------------
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_bins_kernel(FilterArgs a) {
   __shared__ float sh[FL_WAVES];
   __shared__ u64 mass[FL_BINS];
   __shared__ unsigned count[FL_BINS];
   const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
   if (threadIdx.x < FL_BINS) mass[threadIdx.x] = 0, count[threadIdx.x] = 0;
   const float t = chunk_top(x, sh);
@@ -325,7 +332,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_bins_kernel(FilterArgs a) {
   if (t > -INFINITY) {
     const double line = line_of(t, a.mult);
 #pragma unroll
-    for (int j = 0; j < FL_QUADS; ++j)
+    for (int j = 0; j < Q; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int b = class_of(line, x[j][i], a.mult);
@@ -394,6 +401,7 @@ __device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const do
   return f;
 }
 
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a) {
   __shared__ double mass[2][FL_BINS], factor[FL_CHUNKS_MAX];
   __shared__ unsigned count[2][FL_BINS], listed[FL_WAVES], base;
@@ -401,13 +409,13 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
   __shared__ u64 sums[FL_WAVES];
   __shared__ FilterInfo info;
   const int chunk = blockIdx.x, row = blockIdx.y, w = threadIdx.x >> 6;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
+  const float t = threadIdx.x < a.C ? a.w.top[(size_t)row * a.C + threadIdx.x] : -INFINITY;
   const float top = row_top(a, row);
   if (has_none(top)) return;
   const double line = line_of(top, a.mult);
   if (threadIdx.x < a.C) {                         // chunk c's classes count from its own largest z, on the same grid
-    const float t = a.w.top[(size_t)row * a.C + threadIdx.x];
     const double s = line - line_of(t, a.mult);
     shift[threadIdx.x] = s < FL_BINS ? (int)s : FL_BINS;
     factor[threadIdx.x] = weight(distance(top, t, a.mult)) / FL_ONE;
@@ -454,7 +462,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
   u64 sum = 0;
   unsigned mine = 0;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int b = class_of(line, x[j][i], a.mult);
@@ -462,7 +470,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
         const double v = weight(distance(top, x[j][i], a.mult));
         if (v >= a.min_p) sum += units(v);
       }
-      if (id_of(chunk, j, i) < a.V && (b == kbin || (b >= plo && b <= phi))) mine |= 1u << (j * 4 + i);
+      if (id_of<Q>(chunk, j, i) < a.V && (b == kbin || (b >= plo && b <= phi))) mine |= 1u << (j * 4 + i);
     }
   sum = wave_sum_t(sum);
   const unsigned n = __popc(mine), in = wave_scan_t(n);
@@ -484,34 +492,59 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
   __syncthreads();
   at += base;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (mine >> (j * 4 + i) & 1) {
-        if (at < FL_LIST) a.w.list[(size_t)row * FL_LIST + at] = order_of(x[j][i], id_of(chunk, j, i));
+        if (at < FL_LIST) a.w.list[(size_t)row * FL_LIST + at] = order_of(x[j][i], id_of<Q>(chunk, j, i));
         ++at;
       }
 }
 
 // Of the keys that each(visit(key, amount)) goes through (amount > 0, every key once), the one at which the running sum of the
 // amounts, by rising key, is first accepted by reached(sum); the last key, should none be; 0 without keys.  Digits of 8 bits from
-// the highest bit in which a key differs from `like`; done when one key is left.
+// the highest bit in which a key differs from `like`; once few are left, each thread adds up what comes up to its own.
+#define FL_RANK 128               // keys that are compared with each other instead
 struct SelectLds {
-  u64 hist[2][256], before, key;
-  unsigned count[2][256], differ[2][FL_WAVES], pick, left;
+  u64 hist[2][256], keys[FL_RANK], amounts[FL_RANK], upto[FL_RANK], before, key;
+  unsigned count[2][256], rank[FL_RANK], differ[2][FL_WAVES], n[FL_WAVES], pick, left, filled;
 };
+// For each of n <= FL_RANK different keys, how many are no larger (rank) and what these amount to (upto; both cleared before): a
+// lane's two keys against an eighth of them per wave.
+__device__ __forceinline__ void rank_keys(int n, const u64* keys, const u64* amounts, SelectLds& s) {
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const u64 k0 = lane < n ? keys[lane] : 0, k1 = 64 + lane < n ? keys[64 + lane] : 0;
+  u64 u0 = 0, u1 = 0;
+  unsigned r0 = 0, r1 = 0;
+#pragma unroll 4
+  for (int i = w * n / FL_WAVES; i < (w + 1) * n / FL_WAVES; ++i) {
+    const u64 k = keys[i], m = amounts[i];
+    u0 += k <= k0 ? m : 0;
+    u1 += k <= k1 ? m : 0;
+    r0 += k <= k0;
+    r1 += k <= k1;
+  }
+  if (lane < n) atomicAdd(&s.upto[lane], u0), atomicAdd(&s.rank[lane], r0);
+  if (64 + lane < n) atomicAdd(&s.upto[64 + lane], u1), atomicAdd(&s.rank[64 + lane], r1);
+  __syncthreads();
+}
 template <typename E, typename R>
 __device__ u64 select_key(const E& each, const R& reached, u64 like, SelectLds& s) {
   const int lane = threadIdx.x & 63;
   u64 differ = 0;
-  each([&](u64 k, u64) { differ |= k ^ like; });
+  unsigned left = 0;
+  each([&](u64 k, u64) { differ |= k ^ like, ++left; });
   {
-    const unsigned h = wave_or((unsigned)(differ >> 32)), l = wave_or((unsigned)differ);
-    if (lane == 0) s.differ[0][threadIdx.x >> 6] = h, s.differ[1][threadIdx.x >> 6] = l;
+    const unsigned h = wave_or((unsigned)(differ >> 32)), l = wave_or((unsigned)differ), n = wave_sum_t(left);
+    if (lane == 0) s.differ[0][threadIdx.x >> 6] = h, s.differ[1][threadIdx.x >> 6] = l, s.n[threadIdx.x >> 6] = n;
   }
   for (int i = threadIdx.x; i < 256; i += FL_THREADS) s.hist[0][i] = 0, s.count[0][i] = 0;
-  if (threadIdx.x == 0) s.key = 0;
+  if (threadIdx.x < FL_RANK) s.upto[threadIdx.x] = 0, s.rank[threadIdx.x] = 0;
+  if (threadIdx.x == 0) s.key = 0, s.filled = 0;
   __syncthreads();
+  left = 0;
+#pragma unroll
+  for (int i = 0; i < FL_WAVES; ++i) left += s.n[i];
   differ = 0;
 #pragma unroll
   for (int i = 0; i < FL_WAVES; ++i) differ |= (u64)s.differ[0][i] << 32 | s.differ[1][i];
@@ -520,6 +553,26 @@ __device__ u64 select_key(const E& each, const R& reached, u64 like, SelectLds& 
   u64 first = shift == 56 ? 0 : like >> (shift + 8) << (shift + 8), last = shift == 56 ? ~0ull : first | ((1ull << (shift + 8)) - 1);
   u64 before = 0;
   for (int b = 0;; b ^= 1) {
+    if (left <= FL_RANK) {
+      each([&](u64 k, u64 amount) {
+        if (k >= first && k <= last) {
+          const unsigned at = atomicAdd(&s.filled, 1u);
+          s.keys[at] = k;
+          s.amounts[at] = amount;
+        }
+      });
+      __syncthreads();
+      rank_keys(left, s.keys, s.amounts, s);
+      if (threadIdx.x < left) {
+        const u64 upto = before + s.upto[threadIdx.x];
+        const unsigned rank = s.rank[threadIdx.x];
+        const bool good = reached(upto);
+        if (good ? rank == 1 || !reached(upto - s.amounts[threadIdx.x]) : rank == left) s.key = s.keys[threadIdx.x];
+      }
+      __syncthreads();
+      first = s.key;
+      break;
+    }
     each([&](u64 k, u64 amount) {
       if (k >= first && k <= last) {
         atomicAdd(&s.hist[b][k >> shift & 255], amount);
@@ -559,15 +612,8 @@ __device__ u64 select_key(const E& each, const R& reached, u64 like, SelectLds& 
     first = (first >> shift & ~255ull | s.pick) << shift;
     last = first | ((1ull << shift) - 1);
     before = s.before;
+    left = s.left;
     if (shift == 0) break;
-    if (s.left <= 1) {                             // the one key of this digit
-      each([&](u64 k, u64) {
-        if (k >= first && k <= last) s.key = k;
-      });
-      __syncthreads();
-      first = s.key;
-      break;
-    }
     shift = shift > 8 ? shift - 8 : 0;
   }
   __syncthreads();
@@ -624,7 +670,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
                       [&](u64 s) { return (double)s >= goal; }, like, lds);
   }
   candidates([&](u64 o, int, u64 w) {
-    if (o <= last && weight(distance(top, logit_of(o), a.mult)) >= a.min_p && w) atomicAdd(&chunk_mass[(unsigned)o / FL_CHUNK], w);
+    if (o <= last && weight(distance(top, logit_of(o), a.mult)) >= a.min_p && w) atomicAdd(&chunk_mass[(unsigned)o / (unsigned)a.chunk], w);
   });
   __syncthreads();
   for (int c = threadIdx.x; c < a.C; c += FL_THREADS) a.w.kept[(size_t)row * a.C + c] += (double)chunk_mass[c];
@@ -634,57 +680,63 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
 // ---- results --------------------------------------------------------------------------------------------------------
 enum { FINISH_ALL = 0 /* nothing truncated but by min-p = 0 */, FINISH_KEPT = 1 /* masses of the chunks */, FINISH_CLASSES = 2 /* and a border */,
        FINISH_WRITE = 3 /* border, total and token are there */ };
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a, int mode) {
-  __shared__ u64 sums[FL_QUADS][FL_WAVES];
+  __shared__ u64 sums[Q][FL_WAVES];
   const int chunk = blockIdx.x, row = blockIdx.y, lane = threadIdx.x & 63;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
-  const float top = mode == FINISH_WRITE ? a.w.top[(size_t)row * a.C] : row_top(a, row);
+  // whatever the row's passes have left, read at once
+  const float* tops = a.w.top + (size_t)row * a.C;
+  float t[2];
+  double m[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int c = lane * 2 + i;
+    t[i] = mode == FINISH_WRITE ? tops[0] : c < a.C ? tops[c] : -INFINITY;
+    m[i] = 0.0;
+    if (c < a.C && mode < FINISH_WRITE && !a.greedy) m[i] = (mode == FINISH_ALL ? a.w.sum : a.w.kept)[(size_t)row * a.C + c];
+  }
+  const float ref = tops[mode == FINISH_WRITE ? 0 : chunk];
+  const u64 last = mode >= FINISH_CLASSES ? a.w.end[row].last : ~0ull;
+  const double u = a.tok && a.u ? (double)a.u[row] : 0.0;
+  const float top = wave_max_f(fmaxf(t[0], t[1]));
   if (a.greedy || has_none(top)) {
     int best = 0;
     if (a.greedy) {                                // the lowest chunk that has the largest logit
-      const int* ids = a.w.top_id + (size_t)row * a.C;
-      const float* tops = a.w.top + (size_t)row * a.C;
-      const u64 low = __ballot(lane < a.C && tops[lane] == top), high = __ballot(64 + lane < a.C && tops[64 + lane] == top);
-      best = ids[low ? __ffsll((long long)low) - 1 : high ? 63 + __ffsll((long long)high) : 0];
+      const u64 even = __ballot(lane * 2 < a.C && t[0] == top), odd = __ballot(lane * 2 + 1 < a.C && t[1] == top);
+      const int e = even ? __ffsll((long long)even) * 2 - 2 : 256, o = odd ? __ffsll((long long)odd) * 2 - 1 : 256;
+      best = a.w.top_id[(size_t)row * a.C + min(e, o)];
     }
     if (a.tok && chunk == 0 && threadIdx.x == 0 && mode != FINISH_WRITE) a.tok[row] = a.greedy ? best : -1;
 #pragma unroll
-    for (int j = 0; j < FL_QUADS; ++j) {
+    for (int j = 0; j < Q; ++j) {
       float q[4], m[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const bool on = id_of(chunk, j, i) == best;
+        const bool on = id_of<Q>(chunk, j, i) == best;
         q[i] = !a.greedy ? __builtin_nanf("") : on ? 1.0f : 0.0f;
         m[i] = !a.greedy ? __builtin_nanf("") : on ? x[j][i] : -INFINITY;
       }
-      if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), q);
-      if (a.masked) put4(a.masked, a, row, id_of(chunk, j, 0), m);
+      if (a.q) put4(a.q, a, row, id_of<Q>(chunk, j, 0), q);
+      if (a.masked) put4(a.masked, a, row, id_of<Q>(chunk, j, 0), m);
     }
     return;
   }
   // units of every chunk, two per lane, and their running sums: the same in every wave and workgroup
-  double before = 0.0, here = 0.0, total;
+  double before = 0.0, here = 0.0, total, goal = 0.0;
   bool mine = false;
-  u64 last = ~0ull;
-  double goal = 0.0;
   if (mode == FINISH_WRITE) {
-    last = a.w.end[row].last;
     total = a.w.end[row].total;
   } else {
-    if (mode == FINISH_CLASSES) last = a.w.end[row].last;
-    double m[2];
+    if (mode == FINISH_ALL) {                      // sums that count from the chunk's own largest weight
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int c = lane * 2 + i;
-      const size_t at = (size_t)row * a.C + c;
-      m[i] = 0.0;
-      if (c < a.C) m[i] = mode == FINISH_ALL ? (a.w.top[at] > -INFINITY ? a.w.sum[at] * weight(distance(top, a.w.top[at], a.mult)) * FL_ONE : 0.0) : a.w.kept[at];
+      for (int i = 0; i < 2; ++i) m[i] = t[i] > -INFINITY ? m[i] * weight(distance(top, t[i], a.mult)) * FL_ONE : 0.0;
     }
     const double in = wave_scan_t(m[0] + m[1]), ex = wave_before_t(in);
     total = lane_t(in, 63);
     if (a.tok) {
-      goal = fmin(fmax((double)a.u[row], 0.0), 1.0) * total;
+      goal = fmin(fmax(u, 0.0), 1.0) * total;
       // the first chunk whose running sum passes the goal, else the last one with any mass
       const u64 p0 = __ballot(m[0] > 0.0 && ex + m[0] > goal), p1 = __ballot(m[1] > 0.0 && ex + m[0] + m[1] > goal);
       const u64 f0 = __ballot(m[0] > 0.0), f1 = __ballot(m[1] > 0.0);
@@ -705,11 +757,11 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
   const double inv = FL_ONE / total;
   unsigned kept = 0;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j) {
+  for (int j = 0; j < Q; ++j) {
     float q[4], m[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int id = id_of(chunk, j, i);
+      const int id = id_of<Q>(chunk, j, i);
       q[i] = 0.0f;
       m[i] = -INFINITY;
       if (id < a.V && (last == ~0ull || order_of(x[j][i], id) <= last)) {
@@ -721,16 +773,15 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
         }
       }
     }
-    if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), q);
-    if (a.masked) put4(a.masked, a, row, id_of(chunk, j, 0), m);
+    if (a.q) put4(a.q, a, row, id_of<Q>(chunk, j, 0), q);
+    if (a.masked) put4(a.masked, a, row, id_of<Q>(chunk, j, 0), m);
   }
   if (!mine) return;
   // The id inside the chunk, in units of the chunk's own largest weight (it is kept if any of the chunk is), so that there are
   // some however small the chunk's share is.
-  const float ref = a.w.top[(size_t)row * a.C + chunk];
-  u64 start = 0, own[FL_QUADS], scan[FL_QUADS];
+  u64 start = 0, own[Q], scan[Q];
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j) {
+  for (int j = 0; j < Q; ++j) {
     own[j] = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) own[j] += kept >> (j * 4 + i) & 1 ? units(weight(distance(ref, x[j][i], a.mult))) : 0;
@@ -739,7 +790,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
   }
   __syncthreads();
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
 #pragma unroll
     for (int i = 0; i < FL_WAVES; ++i) {
       if (i == (int)(threadIdx.x >> 6)) scan[j] += start - own[j];       // exclusive, from the chunk's first id on
@@ -748,13 +799,13 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
   u64 want = (u64)(fmin(fmax((goal - before) / here, 0.0), 1.0) * (double)start);
   if (want >= start) want = start - 1;
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j)
+  for (int j = 0; j < Q; ++j)
     if (scan[j] <= want && want < scan[j] + own[j]) {
       u64 at = scan[j];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const u64 v = kept >> (j * 4 + i) & 1 ? units(weight(distance(ref, x[j][i], a.mult))) : 0;
-        if (at <= want && want < at + v) a.tok[row] = id_of(chunk, j, i);
+        if (at <= want && want < at + v) a.tok[row] = id_of<Q>(chunk, j, i);
         at += v;
       }
     }
@@ -762,23 +813,24 @@ __global__ __launch_bounds__(FL_THREADS) void filter_finish_kernel(FilterArgs a,
 
 // ---- few ids --------------------------------------------------------------------------------------------------------
 // The largest of every 16 ids (four lanes' quads), and the results cleared unless they replace the logits.
+template <int Q>
 __global__ __launch_bounds__(FL_THREADS) void filter_groups_kernel(FilterArgs a, int clear) {
   const int chunk = blockIdx.x, row = blockIdx.y;
-  float x[FL_QUADS][4];
+  float x[Q][4];
   load_chunk(a, row, chunk, x);
 #pragma unroll
-  for (int j = 0; j < FL_QUADS; ++j) {
+  for (int j = 0; j < Q; ++j) {
     float v = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v = x[j][i] < INFINITY ? fmaxf(v, x[j][i]) : INFINITY;
     v = fmaxf(v, __shfl_xor(v, 1));
     v = fmaxf(v, __shfl_xor(v, 2));
-    const int g = id_of(chunk, j, 0) / FL_GROUP;
+    const int g = id_of<Q>(chunk, j, 0) / FL_GROUP;
     if ((threadIdx.x & 3) == 0) a.w.group[(size_t)row * a.G + g] = v;
     if (clear) {
       const float zero[4] = {0.f, 0.f, 0.f, 0.f}, none[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-      if (a.q) put4(a.q, a, row, id_of(chunk, j, 0), zero);
-      if (a.masked) put4(a.masked, a, row, id_of(chunk, j, 0), none);
+      if (a.q) put4(a.q, a, row, id_of<Q>(chunk, j, 0), zero);
+      if (a.masked) put4(a.masked, a, row, id_of<Q>(chunk, j, 0), none);
     }
   }
 }
@@ -795,22 +847,32 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const float* g = a.w.group + (size_t)row * a.G;
   const float* x = a.logits + (size_t)row * a.ld;
-  // use(group, largest logit) of all of them, sixteen loads of a thread at a time
-  auto all_groups = [&](auto use) {
-    for (int i0 = threadIdx.x * 4; i0 < a.G; i0 += FL_THREADS * 16) {
-      f32x4 v[4];
+  // use(group, largest logit) of all of them: sixteen of a thread's at a time, the first sixteen stay in registers
+  f32x4 own_groups[4];
+  auto load_groups = [&](int i0, f32x4 (&v)[4]) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int i = i0 + k * FL_THREADS * 4;
-        if (i < a.G) v[k] = *reinterpret_cast<const f32x4*>(g + i);       // rows of groups are padded to fours
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + k * FL_THREADS * 4;
+      v[k] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (i < a.G) v[k] = *reinterpret_cast<const f32x4*>(g + i);         // a multiple of 128 of them
+    }
+  };
+  auto use_groups = [&](int i0, const f32x4 (&v)[4], auto use) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = i0 + k * FL_THREADS * 4 + e;
+        if (i < a.G) use(i, v[k][e]);
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = i0 + k * FL_THREADS * 4 + e;
-          if (i < a.G) use(i, v[k][e]);
-        }
+  };
+  load_groups(threadIdx.x * 4, own_groups);
+  auto all_groups = [&](auto use) {
+    use_groups(threadIdx.x * 4, own_groups, use);
+    for (int i0 = threadIdx.x * 4 + FL_THREADS * 16; i0 < a.G; i0 += FL_THREADS * 16) {
+      f32x4 v[4];
+      load_groups(i0, v);
+      use_groups(i0, v, use);
     }
   };
   float mx = -INFINITY;
@@ -868,12 +930,12 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   bool whole = picked > 2 * FL_FEW_LIST;           // then every id of the row is looked at
   if (!whole) {
     const int n = (int)picked * 4;                 // quads, four loads of a thread at a time
-    for (int i0 = threadIdx.x; i0 < n; i0 += FL_THREADS * 4) {
+    for (int i0 = 0; i0 < n; i0 += FL_THREADS * 4) {          // whole waves: they count together
       f32x4 v[4];
       int id[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int i = i0 + k * FL_THREADS;
+        const int i = i0 + k * FL_THREADS + threadIdx.x;
         id[k] = i < n ? groups[i >> 2] * FL_GROUP + (i & 3) * 4 : a.V;
         if (id[k] + 4 <= a.V) {
           v[k] = *reinterpret_cast<const f32x4u*>(x + id[k]);
@@ -883,13 +945,25 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
             if (id[k] + e < a.V) v[k][e] = x[id[k] + e];
         }
       }
+      unsigned mine = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (id[k] + e < a.V && class_of(line, v[k][e], a.mult) <= lowest) {
-            const unsigned at = atomicAdd(&listed, 1u);
-            if (at < FL_FEW_LIST) list[at] = order_of(v[k][e], id[k] + e);
+          if (id[k] + e < a.V && class_of(line, v[k][e], a.mult) <= lowest) mine |= 1u << (k * 4 + e);
+      const unsigned in = wave_scan_t((unsigned)__popc(mine)), all = lane_t(in, 63);
+      unsigned at = 0;
+      if (lane == 0 && all) at = atomicAdd(&listed, all);
+      at = lane_t(at, 0) + in - __popc(mine);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine >> (k * 4 + e) & 1) {
+            if (at < FL_FEW_LIST) {
+              list[at] = order_of(v[k][e], id[k] + e);
+            }
+            ++at;
           }
     }
     __syncthreads();
@@ -898,6 +972,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   const int n = whole ? a.V : (int)listed;
   if (!whole)
     for (int i = threadIdx.x; i < n; i += FL_THREADS) amount[i] = units(weight(distance(mx, logit_of(list[i]), a.mult)));
+  if (threadIdx.x < FL_RANK) lds.upto[threadIdx.x] = 0, lds.rank[threadIdx.x] = 0;
   __syncthreads();
   auto candidates = [&](auto use) {                // use(order, units) of every one
     for (int i = threadIdx.x; i < n; i += FL_THREADS) {
@@ -905,28 +980,58 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
       else if (class_of(line, x[i], a.mult) <= lowest) use(order_of(x[i], i), units(weight(distance(mx, x[i], a.mult))));
     }
   };
-  const u64 like = order_of(mx, 0);
-  u64 last = select_key([&](auto visit) { candidates([&](u64 o, u64) { visit(o, 1ull); }); },
-                        [&](u64 s) { return s >= (u64)a.top_k; }, like, lds);
-  if (a.top_p < 1.0) {
-    u64 m = 0;
-    const u64 upto = last;
-    candidates([&](u64 o, u64 w) { if (o <= upto) m += w; });
-    const double goal = a.top_p * (double)block_sum_t(m, sh);
-    last = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (o <= upto && w) visit(o, w); }); },
-                      [&](u64 s) { return (double)s >= goal; }, like, lds);
-    __syncthreads();
-  }
-  u64 m = 0;
+  const double u = a.tok ? fmin(fmax((double)a.u[row], 0.0), 1.0) : 0.0;
+  u64 last, total;
   auto kept = [&](u64 o) { return o <= last && (a.min_p == 0.0 || weight(distance(mx, logit_of(o), a.mult)) >= a.min_p); };
-  candidates([&](u64 o, u64 w) { if (kept(o)) m += w; });
-  const u64 total = block_sum_t(m, sh);
-  if (a.tok) {
-    u64 goal = (u64)(fmin(fmax((double)a.u[row], 0.0), 1.0) * (double)total);
+  if (n <= FL_RANK) {                              // one comparison of all with all gives both borders, a second one the draw
+    rank_keys(n, list, amount, lds);
+    const bool in = (int)threadIdx.x < n;
+    const u64 own = in ? list[threadIdx.x] : ~0ull, w = in ? amount[threadIdx.x] : 0, upto = in ? lds.upto[threadIdx.x] : 0;
+    const int rank = in ? (int)lds.rank[threadIdx.x] : n + 1;
+    if (rank == min(a.top_k, n)) lds.key = own, lds.before = upto;
+    __syncthreads();
+    last = lds.key;
+    if (a.top_p < 1.0) {
+      const double goal = a.top_p * (double)lds.before;
+      __syncthreads();
+      if (own <= last && (double)upto >= goal && (rank == 1 || (double)(upto - w) < goal)) lds.key = own;
+      __syncthreads();
+      last = lds.key;
+    }
+    const u64 mine = in && kept(own) ? w : 0;
+    if (threadIdx.x < FL_RANK) {
+      lds.keys[threadIdx.x] = (unsigned)own;
+      lds.amounts[threadIdx.x] = mine;
+      lds.upto[threadIdx.x] = 0;
+    }
+    total = block_sum_t(mine, sh);
+    rank_keys(n, lds.keys, lds.amounts, lds);
+    u64 goal = (u64)(u * (double)total);
     if (goal >= total) goal = total - 1;
-    const u64 id = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (w && kept(o)) visit((u64)(unsigned)o, w); }); },
-                              [&](u64 s) { return s > goal; }, 0, lds);
-    if (threadIdx.x == 0) a.tok[row] = (int)id;
+    const u64 sum = in ? lds.upto[threadIdx.x] : 0;
+    if (a.tok && sum > goal && sum - mine <= goal) a.tok[row] = (int)(unsigned)own;
+  } else {
+    const u64 like = order_of(mx, 0);
+    last = select_key([&](auto visit) { candidates([&](u64 o, u64) { visit(o, 1ull); }); },
+                      [&](u64 s) { return s >= (u64)a.top_k; }, like, lds);
+    if (a.top_p < 1.0) {
+      u64 m = 0;
+      const u64 upto = last;
+      candidates([&](u64 o, u64 w) { if (o <= upto) m += w; });
+      const double goal = a.top_p * (double)block_sum_t(m, sh);
+      last = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (o <= upto && w) visit(o, w); }); },
+                        [&](u64 s) { return (double)s >= goal; }, like, lds);
+    }
+    u64 m = 0;
+    candidates([&](u64 o, u64 w) { if (kept(o)) m += w; });
+    total = block_sum_t(m, sh);
+    if (a.tok) {
+      u64 goal = (u64)(u * (double)total);
+      if (goal >= total) goal = total - 1;
+      const u64 id = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (w && kept(o)) visit((u64)(unsigned)o, w); }); },
+                                [&](u64 s) { return s > goal; }, 0, lds);
+      if (threadIdx.x == 0) a.tok[row] = (int)id;
+    }
   }
   if (!clear) {
     if (threadIdx.x == 0) {
@@ -945,17 +1050,32 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
 }
 
 // ---- the call -------------------------------------------------------------------------------------------------------
+// Quads of a chunk: as few as still leave no more than two workgroups per CU (256 of them), so that a workgroup's share of 64-bit
+// work is small; but every workgroup of `collect` adds up all chunks' classes, so not beyond 32 chunks for it (128 else: two per
+// lane).  By rows and ids alone, so that the workspace can be sized.
+static int filter_quads(int rows, int V, bool classes) {
+  int q = FL_QUADS_MAX;
+  while (q > 1) {
+    const int C = (V + FL_QUAD * (q / 2) - 1) / (FL_QUAD * (q / 2));
+    if ((long long)C * rows > 512 || C > (classes ? 32 : 128)) break;
+    q /= 2;
+  }
+  return q;
+}
+static size_t filter_chunks(int V, int quads) { return ((size_t)V + FL_QUAD * quads - 1) / (FL_QUAD * quads); }
 static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
-  const size_t C = (V + FL_CHUNK - 1) / FL_CHUNK, n = rows;
+  const size_t n = rows, classes = filter_chunks(V, filter_quads(rows, V, true));
+  const size_t few = filter_chunks(V, filter_quads(rows, V, false)), C = few > classes ? few : classes;
+  const size_t groups = filter_chunks(V, FL_QUADS_MAX) * (FL_QUAD * FL_QUADS_MAX / FL_GROUP);      // whole chunks of any size
   size_t at = 0;
   auto take = [&](size_t bytes) {
     char* p = base + at;
     at += (bytes + 15) & ~(size_t)15;
     return p;
   };
-  w->mass = (u64*)take(n * C * FL_BINS * 8);
+  w->mass = (u64*)take(n * classes * FL_BINS * 8);
   w->list = (u64*)take(n * FL_LIST * 8);
-  w->count = (unsigned*)take(n * C * FL_BINS * 4);
+  w->count = (unsigned*)take(n * classes * FL_BINS * 4);
   w->kept = (double*)take(n * C * 8);
   w->top = (float*)take(n * C * 4);
   w->top_id = (int*)take(n * C * 4);
@@ -963,22 +1083,49 @@ static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
   w->info = (FilterInfo*)take(n * sizeof(FilterInfo));
   w->end = (FilterEnd*)take(n * sizeof(FilterEnd));
   w->listed = (unsigned*)take(n * 4);
-  w->group = (float*)w->mass;                      // few ids need no classes; C * FL_BINS * 8 >= G * 4
-  static_assert(FL_BINS * 8 >= FL_CHUNK / FL_GROUP * 4, "groups fit in place of the classes' masses");
+  w->group = (float*)take(n * groups * 4);
   return at;
 }
 size_t filter_work_bytes(int rows, int V) {
   FilterWork w;
   return filter_layout(rows, V, nullptr, &w);
 }
+template <int Q>
+static hipError_t launch_filter(FilterArgs a, int rows, hipStream_t st) {
+  a.chunk = Q * FL_QUAD;
+  a.C = (a.V + a.chunk - 1) / a.chunk;
+  a.G = a.C * (a.chunk / FL_GROUP);                // whole chunks of them
+  const dim3 grid(a.C, rows), block(FL_THREADS);
+  if (!a.greedy && a.top_k && a.top_k <= FL_FEW) {
+    const int clear = a.q != a.logits && a.masked != a.logits;
+    filter_groups_kernel<Q><<<grid, block, 0, st>>>(a, clear);
+    filter_few_kernel<<<rows, block, 0, st>>>(a, clear);
+    if (!clear) filter_finish_kernel<Q><<<grid, block, 0, st>>>(a, FINISH_WRITE);
+    return hipGetLastError();
+  }
+  if (!a.greedy && (a.top_k || a.top_p < 1.0)) {
+    const int bytes = 2 * FL_LIST * 8;
+    hipError_t e = hipFuncSetAttribute((const void*)filter_resolve_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    filter_bins_kernel<Q><<<grid, block, 0, st>>>(a);
+    filter_collect_kernel<Q><<<grid, block, 0, st>>>(a);
+    filter_resolve_kernel<<<rows, block, bytes, st>>>(a);
+    filter_finish_kernel<Q><<<grid, block, 0, st>>>(a, FINISH_CLASSES);
+    return hipGetLastError();
+  }
+  const int all = !a.greedy && a.min_p == 0.0;
+  if (a.greedy) filter_greedy_kernel<Q><<<grid, block, 0, st>>>(a);
+  else filter_top_kernel<Q><<<grid, block, 0, st>>>(a, all);
+  if (!a.greedy && !all) filter_mass_kernel<Q><<<grid, block, 0, st>>>(a);
+  filter_finish_kernel<Q><<<grid, block, 0, st>>>(a, all ? FINISH_ALL : FINISH_KEPT);
+  return hipGetLastError();
+}
 hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, const spec_sampling& s, const float* u, float* q,
                               float* masked, int* tok, void* work, hipStream_t st) {
-  FilterArgs a;
+  FilterArgs a = {};
   a.logits = logits;
   a.ld = ld;
   a.V = V;
-  a.C = (V + FL_CHUNK - 1) / FL_CHUNK;
-  a.G = a.C * (FL_CHUNK / FL_GROUP);                // whole chunks of them
   a.greedy = s.temperature == 0.0f;
   a.mult = a.greedy ? 1.0 : (double)s.logit_scale / (double)s.temperature;
   a.top_k = s.top_k > 0 && s.top_k < V ? s.top_k : 0;
@@ -989,28 +1136,9 @@ hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, c
   a.masked = masked;
   a.tok = tok;
   filter_layout(rows, V, (char*)work, &a.w);
-  const dim3 grid(a.C, rows), block(FL_THREADS);
-  if (!a.greedy && a.top_k && a.top_k <= FL_FEW) {
-    const int clear = q != logits && masked != logits;
-    filter_groups_kernel<<<grid, block, 0, st>>>(a, clear);
-    filter_few_kernel<<<rows, block, 0, st>>>(a, clear);
-    if (!clear) filter_finish_kernel<<<grid, block, 0, st>>>(a, FINISH_WRITE);
-    return hipGetLastError();
-  }
-  if (!a.greedy && (a.top_k || a.top_p < 1.0)) {
-    const int bytes = 2 * FL_LIST * 8;
-    hipError_t e = hipFuncSetAttribute((const void*)filter_resolve_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != hipSuccess) return e;
-    filter_bins_kernel<<<grid, block, 0, st>>>(a);
-    filter_collect_kernel<<<grid, block, 0, st>>>(a);
-    filter_resolve_kernel<<<rows, block, bytes, st>>>(a);
-    filter_finish_kernel<<<grid, block, 0, st>>>(a, FINISH_CLASSES);
-    return hipGetLastError();
-  }
-  const int all = !a.greedy && a.min_p == 0.0;
-  if (a.greedy) filter_greedy_kernel<<<grid, block, 0, st>>>(a);
-  else filter_top_kernel<<<grid, block, 0, st>>>(a, all);
-  if (!a.greedy && !all) filter_mass_kernel<<<grid, block, 0, st>>>(a);
-  filter_finish_kernel<<<grid, block, 0, st>>>(a, all ? FINISH_ALL : FINISH_KEPT);
-  return hipGetLastError();
+  const bool classes = !a.greedy && (a.top_k > FL_FEW || (!a.top_k && a.top_p < 1.0));
+  const int quads = filter_quads(rows, V, classes);
+  if (quads == 1) return launch_filter<1>(a, rows, st);
+  if (quads == 2) return launch_filter<2>(a, rows, st);
+  return launch_filter<4>(a, rows, st);
 }
