@@ -39,7 +39,7 @@ static_assert(SPEC_SAMPLE_VOCAB_MAX <= 1 << 20, "sums of weights fit 64 bits");
 static_assert(FL_CHUNKS_MAX <= 128, "two chunks per lane");
 
 struct FilterInfo {              // of a row: borders by classes, masses relative to its largest weight
-  int kbin, plo, phi, n_before;  // class of the k-th id; classes that top-p may end in; ids before kbin
+  int kbin, plo, phi, low, n_before;  // class of the k-th id; classes that top-p may end in; first that min-p leaves out; ids before kbin
   double m_before_k, m_before_p, mass;
 };
 struct FilterEnd {
@@ -81,6 +81,9 @@ __device__ __forceinline__ float logit_of(u64 order) {
   const unsigned key = ~(unsigned)(order >> 32);
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
+// Bounds of the orders of logits up to / from a value that roundings have moved by less than 1e-6 of it.
+__device__ __forceinline__ u64 first_order(float x) { return order_of(x + (fabsf(x) * 1e-6f + 1e-44f), 0); }
+__device__ __forceinline__ u64 last_order(float x) { return order_of(x - (fabsf(x) * 1e-6f + 1e-44f), -1); }
 // exp(-d), d >= 0: 2^-n times the Taylor series of 2^f, |f| <= 1/2, to the 12th power (6e-15 of the value)
 __device__ __forceinline__ double weight(double d) {
   const double y = fmin(d, 1000.0) * 1.4426950408889634074, n = rint(y), t = (n - y) * 0.69314718055994530942;
@@ -351,7 +354,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_bins_kernel(FilterArgs a) {
 
 // The borders of a row by classes, by the first wave: lane l holds classes 4 l .. 4 l + 3 of mass and count.  The last class takes
 // all that lies further below, more than 31 in z: no mass in units, and the k-th id if no earlier class has it.
-__device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const double* mass, const unsigned* count) {
+__device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, float top, double line, const double* mass, const unsigned* count) {
   const int lane = threadIdx.x;
   double m[4], sm = 0.0;
   unsigned n[4], sn = 0;                           // inclusive sums inside the lane
@@ -398,6 +401,21 @@ __device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, const do
     f.plo = first([&](double s, unsigned) { return s >= lo; }, &f.m_before_p, &skip_n, &skip);
     f.phi = first([&](double s, unsigned) { return s >= hi; }, &skip_m, &skip_n, &skip);
   }
+  f.low = FL_BINS;
+  if (a.min_p > 0.0) {                             // a class's largest z is that of the grid line above it
+    int k = 4;
+#pragma unroll
+    for (int i = 3; i >= 0; --i)
+      if (weight(fmax((double)top * a.mult - (line - (lane * 4 + i) + 1.0) / FL_GRID, 0.0)) < a.min_p * 0.999) k = i;
+    const u64 some = __ballot(k < 4);
+    if (some) {
+      const int at = __ffsll((long long)some) - 1;
+      f.low = at * 4 + lane_t(k, at);
+    }
+    // borders among ids that min-p leaves out anyway
+    if (f.kbin >= f.low) f.kbin = FL_BINS;
+    if (f.plo >= f.low) f.plo = f.phi = FL_BINS;
+  }
   return f;
 }
 
@@ -431,14 +449,18 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
       unsigned k[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int d = c + 2 * i, from = d < a.C ? b - shift[d] : -1;
-        v[i] = from >= 0 ? a.w.mass[rows + (size_t)d * FL_BINS + from] : 0;
-        k[i] = a.top_k && from >= 0 ? a.w.count[rows + (size_t)d * FL_BINS + from] : 0;
+        const int d = min(c + 2 * i, a.C - 1), from = max(b - shift[d], 0);
+        v[i] = a.w.mass[rows + (size_t)d * FL_BINS + from];
+        k[i] = 0;
+        if (a.top_k) k[i] = a.w.count[rows + (size_t)d * FL_BINS + from];
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (c + 2 * i < a.C) m += (double)v[i] * factor[c + 2 * i];
-        n += k[i];
+        const int d = c + 2 * i;
+        if (d < a.C && b >= shift[d]) {
+          m += (double)v[i] * factor[d];
+          n += k[i];
+        }
       }
     }
     mass[half][b] = m;
@@ -451,14 +473,14 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
   }
   __syncthreads();
   if (threadIdx.x < 64) {
-    const FilterInfo f = find_classes(a, mass[0], count[0]);
+    const FilterInfo f = find_classes(a, top, line, mass[0], count[0]);
     if (threadIdx.x == 0) {
       info = f;
       if (chunk == 0) a.w.info[row] = f;
     }
   }
   __syncthreads();
-  const int kbin = info.kbin, plo = info.plo, phi = info.phi, sure_below = plo < kbin ? plo : kbin;
+  const int kbin = info.kbin, plo = info.plo, phi = info.phi, sure_below = min(min(plo, kbin), info.low);
   u64 sum = 0;
   unsigned mine = 0;
 #pragma unroll
@@ -501,9 +523,10 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
       }
 }
 
-// Of the keys that each(visit(key, amount)) goes through (amount > 0, every key once), the one at which the running sum of the
-// amounts, by rising key, is first accepted by reached(sum); the last key, should none be; 0 without keys.  Digits of 8 bits from
-// the highest bit in which a key differs from `like`; once few are left, each thread adds up what comes up to its own.
+// Of the keys that each(visit(key, amount)) goes through (amount > 0, every key once, `first` to `last`), the one at which the
+// running sum of the amounts, by rising key, is first accepted by reached(sum); the last key, should none be; 0 without keys.
+// Digits of 8 bits from the highest bit that is not the same in `first` and `last`; once few are left, they are compared with
+// each other.
 #define FL_RANK 128               // keys that are compared with each other instead
 struct SelectLds {
   u64 hist[2][256], keys[FL_RANK], amounts[FL_RANK], upto[FL_RANK], before, key;
@@ -529,29 +552,14 @@ __device__ __forceinline__ void rank_keys(int n, const u64* keys, const u64* amo
   __syncthreads();
 }
 template <typename E, typename R>
-__device__ u64 select_key(const E& each, const R& reached, u64 like, SelectLds& s) {
+__device__ u64 select_key(const E& each, const R& reached, u64 first, u64 last, unsigned left, SelectLds& s) {
   const int lane = threadIdx.x & 63;
-  u64 differ = 0;
-  unsigned left = 0;
-  each([&](u64 k, u64) { differ |= k ^ like, ++left; });
-  {
-    const unsigned h = wave_or((unsigned)(differ >> 32)), l = wave_or((unsigned)differ), n = wave_sum_t(left);
-    if (lane == 0) s.differ[0][threadIdx.x >> 6] = h, s.differ[1][threadIdx.x >> 6] = l, s.n[threadIdx.x >> 6] = n;
-  }
   for (int i = threadIdx.x; i < 256; i += FL_THREADS) s.hist[0][i] = 0, s.count[0][i] = 0;
   if (threadIdx.x < FL_RANK) s.upto[threadIdx.x] = 0, s.rank[threadIdx.x] = 0;
   if (threadIdx.x == 0) s.key = 0, s.filled = 0;
   __syncthreads();
-  left = 0;
-#pragma unroll
-  for (int i = 0; i < FL_WAVES; ++i) left += s.n[i];
-  differ = 0;
-#pragma unroll
-  for (int i = 0; i < FL_WAVES; ++i) differ |= (u64)s.differ[0][i] << 32 | s.differ[1][i];
-  int shift = differ >> 8 ? 56 - __clzll((long long)differ) : 0;
-  // the keys in question, and the sum of what comes before them
-  u64 first = shift == 56 ? 0 : like >> (shift + 8) << (shift + 8), last = shift == 56 ? ~0ull : first | ((1ull << (shift + 8)) - 1);
-  u64 before = 0;
+  int shift = (first ^ last) >> 8 ? 56 - __clzll((long long)(first ^ last)) : 0;
+  u64 before = 0;                                  // sum of what comes before `first`
   for (int b = 0;; b ^= 1) {
     if (left <= FL_RANK) {
       each([&](u64 k, u64 amount) {
@@ -562,6 +570,7 @@ __device__ u64 select_key(const E& each, const R& reached, u64 like, SelectLds& 
         }
       });
       __syncthreads();
+      left = s.filled;
       rank_keys(left, s.keys, s.amounts, s);
       if (threadIdx.x < left) {
         const u64 upto = before + s.upto[threadIdx.x];
@@ -631,7 +640,9 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
   if (has_none(top)) return;
   const FilterInfo f = a.w.info[row];
   const double line = line_of(top, a.mult);
-  const u64 like = order_of(top, 0);
+  // orders of a class's ids lie between these (class 0 starts at the row's largest, the last one has no end)
+  auto from = [&](int b) { return b <= 0 ? order_of(top, 0) : first_order((float)((line - b + 1.0) / FL_GRID / a.mult)); };
+  auto to = [&](int b) { return b >= FL_BINS - 1 ? last_order(-INFINITY) : last_order((float)((line - b) / FL_GRID / a.mult)); };
   const float* x = a.logits + (size_t)row * a.ld;
   const unsigned listed = a.w.listed[row];
   const bool whole = listed > FL_LIST;
@@ -655,19 +666,19 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
   };
   u64 last = ~0ull;
   double mass_k = f.mass;
-  if (a.top_k) {
+  if (f.kbin < FL_BINS) {
     const u64 rank = (u64)(a.top_k - f.n_before);
     last = select_key([&](auto visit) { candidates([&](u64 o, int b, u64) { if (b == f.kbin) visit(o, 1ull); }); },
-                      [&](u64 s) { return s >= rank; }, like, lds);
+                      [&](u64 s) { return s >= rank; }, from(f.kbin), to(f.kbin), listed, lds);
     u64 m = 0;
     candidates([&](u64 o, int b, u64 w) { if (b == f.kbin && o <= last) m += w; });
     mass_k = f.m_before_k + (double)block_sum_t(m, sh) / FL_ONE;
   }
-  if (a.top_p < 1.0) {
+  if (f.plo < FL_BINS) {
     const double goal = (a.top_p * mass_k - f.m_before_p) * FL_ONE;
     const u64 upto = last;
     last = select_key([&](auto visit) { candidates([&](u64 o, int b, u64 w) { if (b >= f.plo && b <= f.phi && o <= upto && w) visit(o, w); }); },
-                      [&](u64 s) { return (double)s >= goal; }, like, lds);
+                      [&](u64 s) { return (double)s >= goal; }, from(f.plo), to(f.phi), listed, lds);
   }
   candidates([&](u64 o, int, u64 w) {
     if (o <= last && weight(distance(top, logit_of(o), a.mult)) >= a.min_p && w) atomicAdd(&chunk_mass[(unsigned)o / (unsigned)a.chunk], w);
@@ -896,10 +907,12 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
       }
     return;
   }
-  // the class of the k-th largest group; where fewer groups are that near, everything
-  const double line = line_of(mx, a.mult);
+  // The class of the k-th largest group; where fewer groups are that near, everything.  Any classes will do whose number falls
+  // with the logit: these, in fp32, are about 1/8 wide in z.
+  const float per = (float)fmin(fmax(a.mult * FL_GRID, 1e-30), 1e30);
+  auto class_f = [&](float v) { return fminf((mx - v) * per, FL_BINS - 1.0f); };
   all_groups([&](int, float v) {
-    const int b = class_of(line, v, a.mult);
+    const int b = (int)class_f(v);
     if (b < FL_BINS - 1) atomicAdd(&count[b], 1u);
   });
   __syncthreads();
@@ -919,9 +932,10 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
     if (some ? lane == __ffsll((long long)some) - 1 : lane == 0) bin = some ? lane * 4 + k : FL_BINS - 1;
   }
   __syncthreads();
-  const int lowest = bin;
+  const float beyond = (float)(bin + 1);
+  const u64 edge = bin == FL_BINS - 1 ? last_order(-INFINITY) : last_order(mx - beyond / per - fabsf(mx) * 1e-6f);
   all_groups([&](int i, float v) {
-    if (class_of(line, v, a.mult) <= lowest) {
+    if (class_f(v) < beyond) {
       const unsigned at = atomicAdd(&picked, 1u);
       if (at < 2 * FL_FEW_LIST) groups[at] = i;
     }
@@ -941,30 +955,27 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
           v[k] = *reinterpret_cast<const f32x4u*>(x + id[k]);
         } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (id[k] + e < a.V) v[k][e] = x[id[k] + e];
+          for (int e = 0; e < 4; ++e) v[k][e] = id[k] + e < a.V ? x[id[k] + e] : -INFINITY;
         }
       }
-      unsigned mine = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (id[k] + e < a.V && class_of(line, v[k][e], a.mult) <= lowest) mine |= 1u << (k * 4 + e);
-      const unsigned in = wave_scan_t((unsigned)__popc(mine)), all = lane_t(in, 63);
-      unsigned at = 0;
-      if (lane == 0 && all) at = atomicAdd(&listed, all);
-      at = lane_t(at, 0) + in - __popc(mine);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) {
+        if (i0 + k * FL_THREADS >= n) break;
+        unsigned mine = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (mine >> (k * 4 + e) & 1) {
-            if (at < FL_FEW_LIST) {
-              list[at] = order_of(v[k][e], id[k] + e);
-            }
+          if (id[k] + e < a.V && class_f(v[k][e]) < beyond) mine |= 1u << e;
+        const unsigned in = wave_scan_t((unsigned)__popc(mine)), all = lane_t(in, 63);
+        unsigned at = 0;
+        if (lane == 0 && all) at = atomicAdd(&listed, all);
+        at = lane_t(at, 0) + in - __popc(mine);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine >> e & 1) {
+            if (at < FL_FEW_LIST) list[at] = order_of(v[k][e], id[k] + e);
             ++at;
           }
+      }
     }
     __syncthreads();
     whole = listed > FL_FEW_LIST;
@@ -977,7 +988,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   auto candidates = [&](auto use) {                // use(order, units) of every one
     for (int i = threadIdx.x; i < n; i += FL_THREADS) {
       if (!whole) use(list[i], amount[i]);
-      else if (class_of(line, x[i], a.mult) <= lowest) use(order_of(x[i], i), units(weight(distance(mx, x[i], a.mult))));
+      else if (class_f(x[i]) < beyond) use(order_of(x[i], i), units(weight(distance(mx, x[i], a.mult))));
     }
   };
   const double u = a.tok ? fmin(fmax((double)a.u[row], 0.0), 1.0) : 0.0;
@@ -1013,14 +1024,14 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
   } else {
     const u64 like = order_of(mx, 0);
     last = select_key([&](auto visit) { candidates([&](u64 o, u64) { visit(o, 1ull); }); },
-                      [&](u64 s) { return s >= (u64)a.top_k; }, like, lds);
+                      [&](u64 s) { return s >= (u64)a.top_k; }, like, edge, n, lds);
     if (a.top_p < 1.0) {
       u64 m = 0;
       const u64 upto = last;
       candidates([&](u64 o, u64 w) { if (o <= upto) m += w; });
       const double goal = a.top_p * (double)block_sum_t(m, sh);
       last = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (o <= upto && w) visit(o, w); }); },
-                        [&](u64 s) { return (double)s >= goal; }, like, lds);
+                        [&](u64 s) { return (double)s >= goal; }, like, upto, n, lds);
     }
     u64 m = 0;
     candidates([&](u64 o, u64 w) { if (kept(o)) m += w; });
@@ -1029,7 +1040,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_few_kernel(FilterArgs a, in
       u64 goal = (u64)(u * (double)total);
       if (goal >= total) goal = total - 1;
       const u64 id = select_key([&](auto visit) { candidates([&](u64 o, u64 w) { if (w && kept(o)) visit((u64)(unsigned)o, w); }); },
-                                [&](u64 s) { return s > goal; }, 0, lds);
+                                [&](u64 s) { return s > goal; }, 0, a.V - 1, n, lds);
       if (threadIdx.x == 0) a.tok[row] = (int)id;
     }
   }
