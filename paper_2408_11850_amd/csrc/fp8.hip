@@ -225,9 +225,10 @@ hipError_t launch_quant_weight_fp8(const bf16* w, int N, int K, uint8_t* q, floa
   return hipGetLastError();
 }
 
-// Packed order: panel p (16 weight rows), block b of 128 columns: 2 KiB, row r at 128 r, its 16-byte piece i at place
-// i ^ (r % 8), zeros behind K.  Copied as it is to LDS, the 16 rows x 4 pieces of half an operand meet no bank twice.  The
-// scales come along per panel, [panel][block], so that matrices can be concatenated and interleaved by panels.
+// Packed order: panel p (16 weight rows), block b of 128 columns: 2 KiB in operand order, 16 bytes per lane, the 16-byte pieces
+// 0-3 of the rows and then the pieces 4-7: lane (c, g) = (lane % 16, lane / 16) has piece g, then g + 4, of row c; zeros behind K.
+// A load of a wave is 1 KiB in one run, whole lines of it.  The scales come along per panel, [panel][block], so that matrices
+// can be concatenated and interleaved by panels.
 __global__ __launch_bounds__(128) void pack_weight_fp8_kernel(const uint8_t* __restrict__ src, const float* __restrict__ src_scale,
                                                               int N, int K, int panel_start, int panel_step,
                                                               uint8_t* __restrict__ dst, float* __restrict__ dst_scale) {
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(128) void pack_weight_fp8_kernel(const uint8_t* __r
   u32x4 v = {0, 0, 0, 0};
   typedef __attribute__((ext_vector_type(4), aligned(1))) unsigned u32x4b;
   if (k < K) v = *reinterpret_cast<const u32x4b*>(src + (size_t)(panel * 16 + r) * K + k);
-  *reinterpret_cast<u32x4*>(dst + to * 2048 + r * 128 + (i ^ (r & 7)) * 16) = v;
+  *reinterpret_cast<u32x4*>(dst + to * 2048 + (i >> 2) * 1024 + ((i & 3) * 16 + r) * 16) = v;
   if (threadIdx.x == 0) dst_scale[to] = src_scale[(size_t)(panel / 8) * KB + b];
 }
 hipError_t launch_pack_weight_fp8(void* dst, float* dst_scale, const void* src, const float* src_scale, int N, int K,
@@ -265,20 +266,21 @@ __device__ __forceinline__ f32x4 block_product(const Operand& w, const Operand& 
   const i32x8 b = {(int)x.lo[0], (int)x.lo[1], (int)x.lo[2], (int)x.lo[3], (int)x.hi[0], (int)x.hi[1], (int)x.hi[2], (int)x.hi[3]};
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
-struct Operand16 { bf16x8 part[4]; };
+struct Half16 { bf16x8 part[2]; };               // 16 columns of a lane
 __device__ __forceinline__ bf16x8 to_bf16(unsigned a, unsigned b) {
   const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
   const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
   return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
 }
-__device__ __forceinline__ Operand16 to_bf16(const Operand& o) {
-  return Operand16{{to_bf16(o.lo[0], o.lo[1]), to_bf16(o.lo[2], o.lo[3]), to_bf16(o.hi[0], o.hi[1]), to_bf16(o.hi[2], o.hi[3])}};
-}
-__device__ __forceinline__ f32x4 block_product(const Operand16& w, const Operand16& x) {
-  f32x4 d = {0.f, 0.f, 0.f, 0.f};
+__device__ __forceinline__ Half16 to_bf16(u32x4 v) { return Half16{{to_bf16(v[0], v[1]), to_bf16(v[2], v[3])}}; }
+__device__ __forceinline__ f32x4 half_product(const Half16& w, const Half16& x, f32x4 d) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.part[i], x.part[i], d, 0, 0, 0);
+  for (int i = 0; i < 2; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.part[i], x.part[i], d, 0, 0, 0);
   return d;
+}
+struct Operand16 { Half16 lo, hi; };
+__device__ __forceinline__ f32x4 block_product(const Operand16& w, const Operand16& x) {
+  return half_product(w.hi, x.hi, half_product(w.lo, x.lo, f32x4{0.f, 0.f, 0.f, 0.f}));
 }
 __device__ __forceinline__ f32x4 scaled_add(f32x4 d, float s, f32x4 acc) {
 #pragma unroll
@@ -288,7 +290,7 @@ __device__ __forceinline__ f32x4 scaled_add(f32x4 d, float s, f32x4 acc) {
 
 template <typename T> __device__ __forceinline__ T as_operand(const Operand& o);
 template <> __device__ __forceinline__ Operand as_operand<Operand>(const Operand& o) { return o; }
-template <> __device__ __forceinline__ Operand16 as_operand<Operand16>(const Operand& o) { return to_bf16(o); }
+template <> __device__ __forceinline__ Operand16 as_operand<Operand16>(const Operand& o) { return Operand16{to_bf16(o.lo), to_bf16(o.hi)}; }
 
 struct Fp8Args {
   const uint8_t* x;      // [M][K]
@@ -316,33 +318,48 @@ __device__ __forceinline__ void fp8_store(const Fp8Args& a, int m, int panel, in
 // Up to 32 tokens: bound by the stream of the weights.  A workgroup of 8 waves owns a contiguous range of units (RP panels, SWIGLU:
 // a gate and an up panel); wave w takes its eighth of a unit's blocks of 128, through a ring of D register stages of one block
 // that runs on from unit to unit.  All ring loads are buffer loads whose range check turns "past the end" (blocks, rows, columns)
-// into zeros without traffic: unconditional, so that a stage waits for its own loads only.  The 8 waves' sums are added through
-// LDS in a fixed order: they depend on K alone.
+// into zeros without traffic: unconditional, so that a stage waits for its own loads only.  The two halves of a block (pieces 0-3
+// and 4-7) are summed apart, and the 8 waves' sums are added through LDS in a fixed order: a row's sums depend on K alone.
+//
+// What counts next to HBM is the address unit, which takes a load line by line.  Weights come 8 whole lines to a load.  Rows of x
+// are 128 bytes apart by K: of 16 of them a load brings half a line each.  PAIR (up to 8 tokens) loads 8 whole ones instead, lanes
+// c < 8 with the first half of a block and c >= 8 with the second, as one operand: of the product with the weights' first half
+// the columns 0-7 count, of the other one the columns 8-15.
 #define SK_WAVES 8
 #define SK_SKIP 0x7f000000u            // beyond every buffer
-template <int MT, int EPI, int RP, int D>
+template <bool PAIR, int MT, int EPI, int RP, int D>
 __global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny_kernel(Fp8Args a, int per, int rem) {
+  static_assert(!PAIR || MT == 1, "one tile of 8 tokens");
   __shared__ f32x4 red[2][SK_WAVES][RP][MT][64];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int b = blockIdx.x, u0 = b * per + min(b, rem), u1 = u0 + per + (b < rem ? 1 : 0);
   const int s0 = w * a.KB / SK_WAVES, ns = (w + 1) * a.KB / SK_WAVES - s0;
   const int rounds = ns > D ? (ns + D - 1) / D : 1;
-  const unsigned pbytes = (unsigned)a.KB * 2048u;
+  const unsigned pbytes = (unsigned)a.KB * 2048u, wlane = lane * 16u;
   const __amdgpu_buffer_rsrc_t xr =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x), 0, (unsigned)a.M * (unsigned)a.K, 0x00020000);
   const __amdgpu_buffer_rsrc_t sr =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.xs), 0, (unsigned)a.KB * (unsigned)a.M * 4u, 0x00020000);
-  const unsigned wlo = c * 128 + (g ^ (c & 7)) * 16, whi = wlo ^ 64;
+  const __amdgpu_buffer_rsrc_t pr =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(a.ws), 0, (unsigned)a.NT * (unsigned)a.KB * 4u, 0x00020000);
+  constexpr int XL = PAIR ? 1 : 2;                       // loads of x per tile
+  const int xcol = g * 16 + (PAIR ? (c >> 3) * 64 : 0);  // this lane's first column of a block
   unsigned xoff[MT], soff[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const int m = t * 16 + c;
-    xoff[t] = m < a.M ? (unsigned)m * (unsigned)a.K + g * 16 : SK_SKIP;
+    const int m = PAIR ? c & 7 : t * 16 + c;
+    xoff[t] = m < a.M ? (unsigned)m * (unsigned)a.K + xcol : SK_SKIP;
     soff[t] = m < a.M ? m * 4u : SK_SKIP;
   }
-  Operand wq[D][RP], xq[D][MT];
-  float xs[D][MT], ws[D][RP];
-  typedef const __attribute__((address_space(4))) float* scalar_floats;
+  u32x4 wq[D][RP][2], xq[D][MT][XL];
+  float xs[D][MT], ws[RP], wn[RP];     // lane l of ws, wn: the panel's scale in stage l of this round, of the next one
+  auto load_ws = [&](int u, int r, float (&to)[RP]) {
+#pragma unroll
+    for (int p = 0; p < RP; ++p) {
+      const unsigned at = (unsigned)min(u * RP + p, a.NT - 1) * (unsigned)a.KB + min(s0 + r * D, a.KB - 1);
+      to[p] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(pr, lane < D ? lane * 4u : SK_SKIP, at * 4u, 0));
+    }
+  };
   // stage s: block r * D + s of the wave's share of unit u.  What is not there is skipped by the lanes' offsets; the scalar ones
   // stay inside the buffers (a range check subtracts them from the size).
   auto load = [&](int s, int u, int r) {
@@ -351,45 +368,55 @@ __global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny
 #pragma unroll
     for (int p = 0; p < RP; ++p) {
       const int panel = min(u * RP + p, a.NT - 1);
-      const unsigned skip = on && u * RP + p < a.NT ? 0u : SK_SKIP;
+      const unsigned at = wlane | (on && u * RP + p < a.NT ? 0u : SK_SKIP);
       const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<uint8_t*>(a.w) + (size_t)panel * pbytes, 0, pbytes, 0x00020000);
-      wq[s][p].lo = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, skip | wlo, blk * 2048, 2));
-      wq[s][p].hi = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, skip | whi, blk * 2048, 2));
-      ws[s][p] = ((scalar_floats)a.ws)[(size_t)panel * a.KB + blk];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        wq[s][p][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, at + h * 1024, blk * 2048, 2));
     }
     const unsigned skip = on ? 0u : SK_SKIP;
-    const int left = a.K - blk * 128 - g * 16;       // columns behind this lane's first one
+    const int left = a.K - blk * 128 - xcol;         // columns behind this lane's first one
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       const unsigned at = skip | xoff[t];
-      xq[s][t].lo = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, left > 0 ? at : SK_SKIP, blk * 128, 0));
-      xq[s][t].hi = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, left > 64 ? at + 64 : SK_SKIP, blk * 128, 0));
+#pragma unroll
+      for (int h = 0; h < XL; ++h)
+        xq[s][t][h] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(xr, left > h * 64 ? at + h * 64 : SK_SKIP, blk * 128, 0));
       xs[s][t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(sr, skip | soff[t], blk * a.M * 4, 0));
     }
   };
 #pragma unroll
   for (int s = 0; s < D; ++s) load(s, u0, 0);
-  f32x4 acc[RP][MT];
+  load_ws(u0, 0, ws);
+  f32x4 acc[RP][MT][2];
 #pragma unroll
   for (int p = 0; p < RP; ++p)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int t = 0; t < MT; ++t) acc[p][t][0] = acc[p][t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
   int buf = 0;
 #pragma unroll 1
   for (int u = u0, r = 0; u < u1;) {
     const bool last = r + 1 == rounds;
     const int nu = last ? u + 1 : u, nr = last ? 0 : r + 1;
+    load_ws(nu, nr, wn);
 #pragma unroll
     for (int s = 0; s < D; ++s) {
-      Operand16 x16[MT];
+      Half16 x16[MT][XL];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) x16[t] = to_bf16(xq[s][t]);
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int h = 0; h < XL; ++h) x16[t][h] = to_bf16(xq[s][t][h]);
 #pragma unroll
       for (int p = 0; p < RP; ++p) {
-        const Operand16 w16 = to_bf16(wq[s][p]);
+        const float wscale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ws[p]), s));
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[p][t] = scaled_add(block_product(w16, x16[t]), xs[s][t] * ws[s][p], acc[p][t]);
+        for (int h = 0; h < 2; ++h) {
+          const Half16 w16 = to_bf16(wq[s][p][h]);
+#pragma unroll
+          for (int t = 0; t < MT; ++t)
+            acc[p][t][h] = scaled_add(half_product(w16, x16[t][PAIR ? 0 : h], f32x4{0.f, 0.f, 0.f, 0.f}), xs[s][t] * wscale, acc[p][t][h]);
+        }
       }
       load(s, nu, nr);
       __builtin_amdgcn_sched_barrier(0);              // stage by stage: the ring holds most registers
@@ -399,8 +426,10 @@ __global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny
       for (int p = 0; p < RP; ++p)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          red[buf][w][p][t][lane] = acc[p][t];
-          acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+          f32x4 v = acc[p][t][0] + acc[p][t][1];
+          if (PAIR) v = c < 8 ? acc[p][t][0] : acc[p][t][1];      // a token's halves meet when they are read
+          red[buf][w][p][t][lane] = v;
+          acc[p][t][0] = acc[p][t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
       // two buffers: nobody writes this one again before everybody has passed the next unit's barrier
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -411,22 +440,27 @@ __global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny
         f32x4 sum[2];
 #pragma unroll
         for (int q = 0; q < (EPI == FP8_SWIGLU ? 2 : 1); ++q) {
-          f32x4 e[4];
+          f32x4 e[SK_WAVES];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] = red[buf][2 * i][p0 + q][t][lane] + red[buf][2 * i + 1][p0 + q][t][lane];
-          sum[q] = (e[0] + e[1]) + (e[2] + e[3]);
+          for (int i = 0; i < SK_WAVES; ++i) {
+            e[i] = red[buf][i][p0 + q][t][lane];
+            if (PAIR) e[i] += red[buf][i][p0 + q][t][lane ^ 8];
+          }
+          sum[q] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         }
         if (m < a.M && u * RP + p0 < a.NT) fp8_store<EPI>(a, m, u * RP + p0, g, sum[0], sum[EPI == FP8_SWIGLU ? 1 : 0]);
       }
       buf ^= 1;
     }
     u = nu, r = nr;
+#pragma unroll
+    for (int p = 0; p < RP; ++p) ws[p] = wn[p];
   }
 }
 
 // From 33 tokens on: BMT token tiles x BNP panels per workgroup of WM x WN waves, a block of 128 columns per stage, ST stages.
 // Both operands, and their scales, go global -> LDS without a stop in registers: rows of x as 128 bytes, piece i of row r at
-// place i ^ (r % 8), as the weights are packed.  The loads are inline asm (they write no register), so that the compiler, which
+// place i ^ (r % 8): a fragment's 16 rows meet no bank twice; weights as they are packed.  The loads are inline asm (they write no register), so that the compiler, which
 // would wait for all of them before any LDS read, leaves the waiting to the explicit counts; everything else is ordinary code.
 // Buffer range checks turn rows behind M, panels behind NT and columns behind K into zeros.
 #define DMA_SKIP 0x7f000000u          // beyond every buffer
@@ -515,7 +549,7 @@ __global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int 
     else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
     if (i + ST - 1 < nb) issue(i + ST - 1, next);
     const u32x4* xl = fp8_lds + slot * (S::STAGE / 16) + wm * S::MT * 128 + c * 8;
-    const u32x4* wl = fp8_lds + slot * (S::STAGE / 16) + S::XB / 16 + wn * S::NP * 128 + c * 8;
+    const u32x4* wl = fp8_lds + slot * (S::STAGE / 16) + S::XB / 16 + wn * S::NP * 128 + lane;
     const float* sl = reinterpret_cast<const float*>(fp8_lds + slot * (S::STAGE / 16) + (S::XB + S::WB) / 16);
     const int lo = g ^ (c & 7), hi = lo ^ 4;
     typedef typename std::conditional<EPI == FP8_STORE, Operand16, Operand>::type Op;
@@ -528,7 +562,7 @@ __global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int 
     }
 #pragma unroll
     for (int p = 0; p < S::NP; ++p) {
-      const Op wf = as_operand<Op>(Operand{wl[p * 128 + lo], wl[p * 128 + hi]});
+      const Op wf = as_operand<Op>(Operand{wl[p * 128], wl[p * 128 + 64]});
       const float ws = sl[BMT * 16 + wn * S::NP + p];
 #pragma unroll
       for (int t = 0; t < S::MT; ++t) acc[p][t] = scaled_add(block_product(wf, xf[t]), xs[t] * ws, acc[p][t]);
@@ -571,8 +605,9 @@ template <int EPI>
 static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
   constexpr int RP = EPI == FP8_SWIGLU ? 2 : 1;
   const int units = (a.NT + RP - 1) / RP, G = min(units, 2 * spec_num_cu()), per = units / G, rem = units % G;
-  if (a.M <= 16) fp8_skinny_kernel<1, EPI, RP, RP == 2 ? 2 : 4><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
-  else fp8_skinny_kernel<2, EPI, RP, 2><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
+  if (a.M <= 8) fp8_skinny_kernel<true, 1, EPI, RP, RP == 2 ? 2 : 4><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
+  else if (a.M <= 16) fp8_skinny_kernel<false, 1, EPI, RP, RP == 2 ? 2 : 4><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
+  else fp8_skinny_kernel<false, 2, EPI, RP, 2><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
   return hipGetLastError();
 }
 template <int EPI>
