@@ -315,20 +315,20 @@ __device__ __forceinline__ void fp8_store(const Fp8Args& a, int m, int panel, in
   *reinterpret_cast<uint2*>((bf16*)a.out + at + g * 4) = *reinterpret_cast<const uint2*>(o);
 }
 
-// Up to 32 tokens: bound by the stream of the weights.  A workgroup of 8 waves owns a contiguous range of units (RP panels, SWIGLU:
-// a gate and an up panel); wave w takes its eighth of a unit's blocks of 128, through a ring of D register stages of one block
+// Up to 32 tokens: bound by the stream of the weights.  A workgroup of 4 waves owns a contiguous range of units (RP panels, SWIGLU:
+// gate and up panels); wave w takes its quarter of a unit's blocks of 128, through a ring of D register stages of one block
 // that runs on from unit to unit.  All ring loads are buffer loads whose range check turns "past the end" (blocks, rows, columns)
 // into zeros without traffic: unconditional, so that a stage waits for its own loads only.  The two halves of a block (pieces 0-3
-// and 4-7) are summed apart, and the 8 waves' sums are added through LDS in a fixed order: a row's sums depend on K alone.
+// and 4-7) are summed apart, and the waves' sums are added through LDS in a fixed order: a row's sums depend on K alone.
 //
 // What counts next to HBM is the address unit, which takes a load line by line.  Weights come 8 whole lines to a load.  Rows of x
 // are 128 bytes apart by K: of 16 of them a load brings half a line each.  PAIR (up to 8 tokens) loads 8 whole ones instead, lanes
 // c < 8 with the first half of a block and c >= 8 with the second, as one operand: of the product with the weights' first half
 // the columns 0-7 count, of the other one the columns 8-15.
-#define SK_WAVES 8
+#define SK_WAVES 4
 #define SK_SKIP 0x7f000000u            // beyond every buffer
-template <bool PAIR, int MT, int EPI, int RP, int D>
-__global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny_kernel(Fp8Args a, int per, int rem) {
+template <bool PAIR, int MT, int EPI, int RP, int D, int OCC>
+__global__ __launch_bounds__(SK_WAVES * 64, OCC) void fp8_skinny_kernel(Fp8Args a, int per, int rem) {
   static_assert(!PAIR || MT == 1, "one tile of 8 tokens");
   __shared__ f32x4 red[2][SK_WAVES][RP][MT][64];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -433,22 +433,22 @@ __global__ __launch_bounds__(SK_WAVES * 64, RP * MT > 2 ? 2 : 4) void fp8_skinny
         }
       // two buffers: nobody writes this one again before everybody has passed the next unit's barrier
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-      constexpr int JOBS = EPI == FP8_SWIGLU ? MT : RP * MT;       // a wave adds and stores one tile (SWIGLU: a pair)
-      const int job = (w + u) & (SK_WAVES - 1);
-      if (job < JOBS) {
-        const int t = job % MT, p0 = EPI == FP8_SWIGLU ? 0 : job / MT, m = t * 16 + c;
+      // a wave adds and stores a tile at a time (SWIGLU: those of a pair of panels)
+      constexpr int UP = EPI == FP8_SWIGLU ? 2 : 1, JOBS = RP / UP * MT;
+      for (int job = (w + u) & (SK_WAVES - 1); job < JOBS; job += SK_WAVES) {
+        const int t = job % MT, p0 = job / MT * UP, m = t * 16 + c;
         f32x4 sum[2];
 #pragma unroll
-        for (int q = 0; q < (EPI == FP8_SWIGLU ? 2 : 1); ++q) {
+        for (int q = 0; q < UP; ++q) {
           f32x4 e[SK_WAVES];
 #pragma unroll
           for (int i = 0; i < SK_WAVES; ++i) {
             e[i] = red[buf][i][p0 + q][t][lane];
             if (PAIR) e[i] += red[buf][i][p0 + q][t][lane ^ 8];
           }
-          sum[q] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+          sum[q] = (e[0] + e[1]) + (e[2] + e[3]);
         }
-        if (m < a.M && u * RP + p0 < a.NT) fp8_store<EPI>(a, m, u * RP + p0, g, sum[0], sum[EPI == FP8_SWIGLU ? 1 : 0]);
+        if (m < a.M && u * RP + p0 < a.NT) fp8_store<EPI>(a, m, u * RP + p0, g, sum[0], sum[UP - 1]);
       }
       buf ^= 1;
     }
@@ -601,14 +601,29 @@ static hipError_t launch_dense(const Fp8Args& a, int slices, hipStream_t st) {
   return hipGetLastError();
 }
 
+template <int EPI, bool PAIR, int MT, int RP, int D, int OCC, int WGS>
+static hipError_t launch_units(const Fp8Args& a, hipStream_t st) {
+  const int units = (a.NT + RP - 1) / RP, G = min(units, WGS * spec_num_cu());
+  fp8_skinny_kernel<PAIR, MT, EPI, RP, D, OCC><<<G, SK_WAVES * 64, 0, st>>>(a, units / G, units % G);
+  return hipGetLastError();
+}
+// Two panels share what is read of x where that counts (beyond 8 rows; SiLU * up has a pair anyway) and units suffice, four where
+// x is as much again (beyond 16); else single panels, more of them in flight (us, RP = 1 | 2 | 4 panels, weights from HBM):
+//   7 x 10240 x 8192   19.0 | 21.7        16 x 4096 x 11008  13.5 | 18.7         32 x 4096 x 4096     8.9 | 10.0 | 12.8
+//   7 x 8192 x 28672   41.2 | 40.6        16 x 8192 x 8192   17.1 | 16.7         32 x 8192 x 8192    23.7 | 19.4 | 25.5
+//                                         16 x 32000 x 8192  56.2 | 50.8         32 x 32000 x 8192   78.5 | 60.1 | 56.2
 template <int EPI>
 static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
-  constexpr int RP = EPI == FP8_SWIGLU ? 2 : 1;
-  const int units = (a.NT + RP - 1) / RP, G = min(units, 2 * spec_num_cu()), per = units / G, rem = units % G;
-  if (a.M <= 8) fp8_skinny_kernel<true, 1, EPI, RP, RP == 2 ? 2 : 4><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
-  else if (a.M <= 16) fp8_skinny_kernel<false, 1, EPI, RP, RP == 2 ? 2 : 4><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
-  else fp8_skinny_kernel<false, 2, EPI, RP, 2><<<G, SK_WAVES * 64, 0, st>>>(a, per, rem);
-  return hipGetLastError();
+  if (a.M > 16 && a.NT >= 1024) return launch_units<EPI, false, 2, 4, 2, 2, 2>(a, st);
+  if constexpr (EPI == FP8_SWIGLU) {
+    if (a.M <= 8) return launch_units<EPI, true, 1, 2, 4, 2, 2>(a, st);
+    if (a.M <= 16) return launch_units<EPI, false, 1, 2, 4, 2, 2>(a, st);
+    return launch_units<EPI, false, 2, 2, 4, 2, 2>(a, st);
+  } else {
+    if (a.M <= 8) return launch_units<EPI, true, 1, 1, 4, 4, 4>(a, st);
+    if (a.M <= 16) return a.NT < 512 ? launch_units<EPI, false, 1, 1, 4, 2, 4>(a, st) : launch_units<EPI, false, 1, 2, 4, 2, 2>(a, st);
+    return a.NT < 512 ? launch_units<EPI, false, 2, 1, 4, 2, 4>(a, st) : launch_units<EPI, false, 2, 2, 4, 2, 2>(a, st);
+  }
 }
 template <int EPI>
 static hipError_t launch_fp8(const Fp8Args& a, hipStream_t st) {
