@@ -458,23 +458,26 @@ __global__ __launch_bounds__(SK_WAVES * 64, OCC) void fp8_skinny_kernel(Fp8Args 
   }
 }
 
-// From 33 tokens on: BMT token tiles x BNP panels per workgroup of WM x WN waves, a block of 128 columns per stage, ST stages.
+// From 33 tokens on: BMT tiles of 16 tokens x BNP panels per workgroup of WM x WN waves, a block of 128 columns per stage, ST stages.
 // Both operands, and their scales, go global -> LDS without a stop in registers: rows of x as 128 bytes, piece i of row r at
-// place i ^ (r % 8): a fragment's 16 rows meet no bank twice; weights as they are packed.  The loads are inline asm (they write no register), so that the compiler, which
-// would wait for all of them before any LDS read, leaves the waiting to the explicit counts; everything else is ordinary code.
+// place i ^ (r % 8), so that no read of a fragment meets a bank twice; weights as they are packed.  The loads are inline asm
+// (they write no register), so that the compiler, which would wait for all of them before any LDS read, leaves the waiting to
+// the explicit counts; everything else is ordinary code.
 // Buffer range checks turn rows behind M, panels behind NT and columns behind K into zeros.
 #define DMA_SKIP 0x7f000000u          // beyond every buffer
 __device__ __forceinline__ u32x4 dma_rsrc(const void* base, unsigned bytes) {
   const uint64_t p = (uint64_t)base;
   return u32x4{(unsigned)p, (unsigned)(p >> 32) & 0xffffu, bytes, 0x00020000u};
 }
+// A wave's 64 x 16 (4) bytes to consecutive LDS addresses from `lds` on.  The s_nop keeps a scalar register that a vector
+// instruction has just written five cycles from its use as an offset: the compiler looks for that outside asm only.
 __device__ __forceinline__ void dma16(unsigned lds, u32x4 rsrc, unsigned voff, unsigned soff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               ::"s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+               ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(soff)));
 }
 __device__ __forceinline__ void dma4(unsigned lds, u32x4 rsrc, unsigned voff, unsigned soff) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, %3 offen lds"
-               ::"s"(lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+               ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(soff)));
 }
 
 template <int BMT, int BNP, int WM, int WN, int ST>
@@ -488,7 +491,7 @@ struct DenseShape {
 };
 
 template <int EPI, int BMT, int BNP, int WM, int WN, int ST>
-__global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int TM, int TN, int chunk, int slice) {
+__global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int TM, int TN, int chunk) {
   typedef DenseShape<BMT, BNP, WM, WN, ST> S;
   extern __shared__ u32x4 fp8_lds[];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
@@ -497,7 +500,6 @@ __global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int 
   if (j >= chunk || tile >= TM * TN) return;
   const int grp = tile / (TM * 4), idx = tile % (TM * 4), gw = min(4, TN - grp * 4);
   const int tm = idx / gw, tn = grp * 4 + idx % gw;
-  const int b0 = blockIdx.y * slice, nb = min(slice, a.KB - b0);
   const int m0 = tm * BMT * 16, p0 = tn * BNP;
   const int rows = min(BMT * 16, a.M - m0), panels = min(BNP, a.NT - p0);
   const u32x4 xr = dma_rsrc(a.x + (size_t)m0 * a.K, (unsigned)rows * (unsigned)a.K);
@@ -523,15 +525,17 @@ __global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int 
   soff = tokens ? (w * 64 + lane < rows ? (w * 64 + lane) * 4u : DMA_SKIP)
                 : (lane < panels ? (unsigned)lane * (unsigned)a.KB * 4u : DMA_SKIP);
   const bool tail = (a.K & 127) != 0;
-  auto issue = [&](int i, int slot) {           // block b0 + i
-    const unsigned b = b0 + i, base = lds0 + slot * S::STAGE;
-    const bool cut = tail && (int)b == a.KB - 1 && (int)(b * 128) + xpiece * 16 >= a.K;
-#pragma unroll
-    for (int q = 0; q < XJ; ++q) dma16(base + (w * XJ + q) * 1024, xr, cut ? DMA_SKIP : xoff[q], b * 128);
-#pragma unroll
-    for (int q = 0; q < WJ; ++q) dma16(base + S::XB + (w * WJ + q) * 1024, wr, woff[q], b * 2048);
-    if (tokens) dma4(base + S::XB + S::WB + w * 256, sxr, soff, b * (unsigned)a.M * 4u);
-    else dma4(base + S::XB + S::WB + BMT * 64, swr, soff, b * 4);
+  const unsigned cut = tail && xpiece * 16 >= (a.K & 127) ? DMA_SKIP : 0u;      // for the last block
+  const u32x4 sr = tokens ? sxr : swr;
+  const unsigned slds = S::XB + S::WB + (tokens ? w * 256 : BMT * 64), sstep = tokens ? (unsigned)a.M * 4u : 4u;
+  // Load q of a wave for block b into a slot.  Past the last block the buffers have no bytes: zeros into a slot that nobody reads,
+  // without traffic, so that one count of loads in flight serves every iteration.
+  auto issue = [&](unsigned b, bool there, unsigned last, unsigned base, int q) {
+    const unsigned o = there ? b : 0u;
+    auto cut_off = [&](u32x4 r) { return u32x4{r[0], r[1], there ? r[2] : 0u, r[3]}; };
+    if (q < XJ) dma16(base + (w * XJ + q) * 1024, cut_off(xr), xoff[q] | last, o * 128);
+    else if (q < XJ + WJ) dma16(base + S::XB + (w * WJ + q - XJ) * 1024, cut_off(wr), woff[q - XJ], o * 2048);
+    else dma4(base + slds, cut_off(sr), soff, o * sstep);
   };
   const int wm = w / WN, wn = w % WN;
   f32x4 acc[S::NP][S::MT];
@@ -541,63 +545,85 @@ __global__ __launch_bounds__(WM * WN * 64) void fp8_dense_kernel(Fp8Args a, int 
     for (int t = 0; t < S::MT; ++t) acc[p][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < ST - 1; ++s)
-    if (s < nb) issue(s, s);
+#pragma unroll
+    for (int q = 0; q < S::JOBS; ++q) issue(s, s < a.KB, s == a.KB - 1 ? cut : 0u, lds0 + s * S::STAGE, q);
   int slot = 0, next = ST - 1;
-  for (int i = 0; i < nb; ++i) {
+  for (int i = 0; i < a.KB; ++i) {
     // this wave's loads of block i have landed, then everybody's; everybody is past reading the slot that is filled next
-    if (i + ST - 1 <= nb) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 2) * S::JOBS) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    if (i + ST - 1 < nb) issue(i + ST - 1, next);
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((ST - 2) * S::JOBS) : "memory");
+    const int ahead = i + ST - 1;
+    const bool more = ahead < a.KB;
+    const unsigned cut_now = ahead == a.KB - 1 ? cut : 0u, to = lds0 + next * S::STAGE;
     const u32x4* xl = fp8_lds + slot * (S::STAGE / 16) + wm * S::MT * 128 + c * 8;
     const u32x4* wl = fp8_lds + slot * (S::STAGE / 16) + S::XB / 16 + wn * S::NP * 128 + lane;
     const float* sl = reinterpret_cast<const float*>(fp8_lds + slot * (S::STAGE / 16) + (S::XB + S::WB) / 16);
     const int lo = g ^ (c & 7), hi = lo ^ 4;
     typedef typename std::conditional<EPI == FP8_STORE, Operand16, Operand>::type Op;
-    Op xf[S::MT];
-    float xs[S::MT];
+    // Panel p is multiplied while the fragments of the next ones come from LDS and the sums of the one before are scaled and added.
+    // What the first products need is read first.  The loads go between panels (a wave that issues them back to back waits for the
+    // address unit meanwhile), early in the step if it is all the time they have.
+    constexpr int AHEAD = S::NP > 4 ? 2 : 1, SPREAD = ST == 2 ? (S::NP + 1) / 2 : S::NP;
+    Op xf[S::MT], wf[AHEAD + 1];
+    float xs[S::MT], ws[S::NP];
+    f32x4 d[2][S::MT];
+    wf[0] = as_operand<Op>(Operand{wl[0], wl[64]});
 #pragma unroll
     for (int t = 0; t < S::MT; ++t) {
       xf[t] = as_operand<Op>(Operand{xl[t * 128 + lo], xl[t * 128 + hi]});
-      xs[t] = sl[(wm * S::MT + t) * 16 + c];
+      __builtin_amdgcn_sched_barrier(0);                   // LDS reads stay in this order
     }
 #pragma unroll
-    for (int p = 0; p < S::NP; ++p) {
-      const Op wf = as_operand<Op>(Operand{wl[p * 128], wl[p * 128 + 64]});
-      const float ws = sl[BMT * 16 + wn * S::NP + p];
+    for (int p = 1; p < AHEAD; ++p) wf[p] = as_operand<Op>(Operand{wl[p * 128], wl[p * 128 + 64]});
 #pragma unroll
-      for (int t = 0; t < S::MT; ++t) acc[p][t] = scaled_add(block_product(wf, xf[t]), xs[t] * ws, acc[p][t]);
+    for (int t = 0; t < S::MT; ++t) xs[t] = sl[(wm * S::MT + t) * 16 + c];
+#pragma unroll
+    for (int p = 0; p < S::NP; ++p) ws[p] = sl[BMT * 16 + wn * S::NP + p];
+#pragma unroll
+    for (int p = 0; p <= S::NP; ++p) {
+      if (p + AHEAD < S::NP)
+        wf[(p + AHEAD) % (AHEAD + 1)] = as_operand<Op>(Operand{wl[(p + AHEAD) * 128], wl[(p + AHEAD) * 128 + 64]});
+#pragma unroll
+      for (int t = 0; t < S::MT; ++t) {
+        if (p < S::NP) d[p & 1][t] = block_product(wf[p % (AHEAD + 1)], xf[t]);
+        if (p > 0) acc[p - 1][t] = scaled_add(d[(p - 1) & 1][t], xs[t] * ws[p - 1], acc[p - 1][t]);
+      }
+      if (p > 0 && p < S::NP && EPI != FP8_STORE) {
+#pragma unroll
+        for (int t = 0; t < S::MT; ++t) { __builtin_amdgcn_sched_group_barrier(0x8, 1, 0); __builtin_amdgcn_sched_group_barrier(0x2, 5, 0); }
+      }
+      if (p < SPREAD)
+#pragma unroll
+        for (int q = p * S::JOBS / SPREAD; q < (p + 1) * S::JOBS / SPREAD; ++q) issue(ahead, more, cut_now, to, q);
+      __builtin_amdgcn_sched_barrier(0);
     }
     // its LDS reads are done before this wave meets the next barrier
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     slot = slot + 1 == ST ? 0 : slot + 1;
     next = next + 1 == ST ? 0 : next + 1;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // the last loads must not outlive the workgroup's LDS
 #pragma unroll
   for (int t = 0; t < S::MT; ++t) {
     const int m = m0 + (wm * S::MT + t) * 16 + c;
     if (m >= a.M) continue;
+    constexpr int UP = EPI == FP8_SWIGLU ? 2 : 1;
+    static_assert(S::NP % UP == 0, "whole pairs per wave");
 #pragma unroll
-    for (int p = 0; p < S::NP; p += 2) {
+    for (int p = 0; p < S::NP; p += UP) {
       const int panel = p0 + wn * S::NP + p;
-      if (EPI == FP8_SWIGLU) {
-        if (panel + 1 < a.NT) fp8_store<EPI>(a, m, panel, g, acc[p][t], acc[p + 1][t]);
-      } else {
-        if (panel < a.NT) fp8_store<EPI>(a, m, panel, g, acc[p][t], acc[p][t]);
-        if (panel + 1 < a.NT) fp8_store<EPI>(a, m, panel + 1, g, acc[p + 1][t], acc[p + 1][t]);
-      }
+      if (panel + UP <= a.NT) fp8_store<EPI>(a, m, panel, g, acc[p][t], acc[p + UP - 1][t]);
     }
   }
 }
 
 template <int EPI, int BMT, int BNP, int WM, int WN, int ST>
-static hipError_t launch_dense(const Fp8Args& a, int slices, hipStream_t st) {
+static hipError_t launch_dense(const Fp8Args& a, hipStream_t st) {
   typedef DenseShape<BMT, BNP, WM, WN, ST> S;
   const int TM = (a.M + BMT * 16 - 1) / (BMT * 16), TN = (a.NT + BNP - 1) / BNP, chunk = (TM * TN + 7) / 8;
-  const int slice = (a.KB + slices - 1) / slices;
   auto kernel = fp8_dense_kernel<EPI, BMT, BNP, WM, WN, ST>;
-  static const hipError_t attr = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
-  if (attr != hipSuccess) return attr;
-  kernel<<<dim3(chunk * 8, slices), S::WAVES * 64, S::BYTES, st>>>(a, TM, TN, chunk, slice);
+  const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
+  if (e != hipSuccess) return e;
+  kernel<<<chunk * 8, S::WAVES * 64, S::BYTES, st>>>(a, TM, TN, chunk);
   return hipGetLastError();
 }
 
@@ -625,11 +651,40 @@ static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
     return a.NT < 512 ? launch_units<EPI, false, 2, 1, 4, 2, 4>(a, st) : launch_units<EPI, false, 2, 2, 4, 2, 2>(a, st);
   }
 }
+// Tile by the time a launch takes (us): rounds of as many workgroups as fit, each a fixed part and a time per block of 128 columns
+// that grows with the share of them in use, fitted to 27 shapes of bf16 results (256 x 256 | 256 x 192 | 128 x 256 | 128 x 128 |
+// 64 x 64), of which it takes the fastest in 26, else one 1 % behind, and to 17 of fp32 ones (the last three):
+//   64 x 4096 x 4096       43 |  38 |  30 | 20.4 | 13.6     1023 x 12288 x 4096   66 |  61 |  74 |  79 | 108
+//   256 x 12288 x 4096     60 |  55 |  38 | 26.2 | 32.2     1023 x 8192 x 8192   107 | 101 |  79 |  91 | 139
+//   512 x 8192 x 8192     107 | 100 |  64 | 49.5 | 74.6     4095 x 8192 x 8192   248 | 292 | 293 | 346 | 501
+// 256 x 256 runs at 2.3 PFLOP/s (zeros instead of data: 3.0, so the chip's power is a part of what bounds it); 4 vector instructions
+// per MFMA scale and add, and every block passes LDS once per wave that uses it.
+static int fp8_tile(int M, int NT, int KB, bool exact) {
+  static const struct { int tokens, panels, per_cu; float round, step, busy; } T[2][5] = {
+      {{256, 16, 1, 3.0f, 1.415f, 0.480f}, {256, 12, 1, 1.9f, 1.302f, 0.333f}, {128, 16, 1, 4.2f, 0.854f, 0.255f}, {128, 8, 1, 3.2f, 0.537f, 0.124f}, {64, 4, 2, 3.2f, 0.304f, 0.151f}},
+      {{0, 0, 0, 0.f, 0.f, 0.f}, {0, 0, 0, 0.f, 0.f, 0.f}, {128, 16, 1, 4.4f, 1.525f, 0.315f}, {128, 8, 1, 3.4f, 0.969f, 0.170f}, {64, 4, 2, 2.9f, 0.479f, 0.210f}}};
+  int best = 4;
+  double best_us = 0.0;
+  for (int i = exact ? 2 : 0; i < 5; ++i) {
+    const auto& t = T[exact][i];
+    const long long tiles = (long long)((M + t.tokens - 1) / t.tokens) * ((NT + t.panels - 1) / t.panels);
+    const long long slots = (long long)t.per_cu * spec_num_cu(), rounds = (tiles + slots - 1) / slots;
+    const double us = rounds * (t.round + KB * (t.step + t.busy * (double)tiles / ((double)rounds * slots)));
+    if (i == (exact ? 2 : 0) || us < best_us) best = i, best_us = us;
+  }
+  return best;
+}
 template <int EPI>
 static hipError_t launch_fp8(const Fp8Args& a, hipStream_t st) {
   if (a.M <= 32) return launch_skinny<EPI>(a, st);
-  if (a.M <= 512 || EPI == FP8_STORE) return launch_dense<EPI, 8, 8, 4, 2, 3>(a, 1, st);
-  return launch_dense<EPI, 16, 16, 4, 2, 2>(a, 1, st);
+  const int tile = fp8_tile(a.M, a.NT, a.KB, EPI == FP8_STORE);
+  if constexpr (EPI != FP8_STORE) {
+    if (tile == 0) return launch_dense<EPI, 16, 16, 4, 2, 2>(a, st);
+    if (tile == 1) return launch_dense<EPI, 16, 12, 4, 2, 2>(a, st);
+  }
+  if (tile == 2) return launch_dense<EPI, 8, 16, 2, 4, 3>(a, st);
+  if (tile == 3) return launch_dense<EPI, 8, 8, 4, 2, 4>(a, st);
+  return launch_dense<EPI, 4, 4, 2, 2, 4>(a, st);
 }
 hipError_t launch_gemm_fp8(const uint8_t* x, const float* xs, const void* w, const float* ws, int M, int N, int K, int swiglu,
                            void* out, int out_type, hipStream_t st) {
