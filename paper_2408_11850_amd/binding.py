@@ -31,24 +31,19 @@ def _current_stream_ptr() -> int:
     return _raw_stream(torch.cuda.current_device()) if _raw_stream else _stream_ptr(torch.cuda.current_stream())
 
 
-class on_device:
-    """A tensor's device as the current one for a call, and its current stream's handle.  Where it is current already that costs
-    one query."""
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
-    __slots__ = ("index", "before")
 
-    def __init__(self, index: int):
-        self.index = index
-
-    def __enter__(self) -> int:
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return _raw_stream(self.index) if _raw_stream else _stream_ptr(torch.cuda.current_stream())
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+def call_on(index: int, fn, *args):
+    """fn(*args, stream) on GPU `index` and its current stream; raises what the library refuses.  Where that GPU is the current one
+    already, as mostly, this costs two queries."""
+    if _get_device() == index:
+        rc = fn(*args, _raw_stream(index) if _raw_stream else _stream_ptr(torch.cuda.current_stream()))
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, _stream_ptr(torch.cuda.current_stream()))
+    if rc < 0:
+        check(rc)
 
 
 def need(ok: bool, what: str):

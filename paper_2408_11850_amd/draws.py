@@ -9,25 +9,22 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import Sampling, check, load_library
-from .binding import need, on_device
+from . import Sampling, load_library
+from .binding import call_on, need
 
 
 def _call(logits: torch.Tensor, u, sampling, want_q: bool, masked, want_tokens: bool):
-    need(logits.is_cuda and logits.dim() == 2 and logits.dtype == torch.float32 and
-         (logits.shape[1] == 1 or logits.stride(1) == 1), "logits: rows in float32 on a GPU are wanted")
+    if not (logits.is_cuda and logits.dtype is torch.float32 and logits.dim() == 2 and
+            (logits.stride(1) == 1 or logits.shape[1] == 1)):
+        raise ValueError("logits: rows in float32 on a GPU are wanted")
     n, V = logits.shape
-    dev = logits.device
     lib = load_library()
-    size = lib.spec_sample_rows_workspace_bytes(n, V)
-    work = torch.empty(max(size, 16), dtype=torch.uint8, device=dev)
-    q = torch.empty((n, V), dtype=torch.float32, device=dev) if want_q else None
-    tokens = torch.empty(n, dtype=torch.int32, device=dev) if want_tokens else None
-    with on_device(dev.index) as st:
-        check(lib.spec_sample_rows(logits.data_ptr(), logits.stride(0) if n > 1 else V, n, V, C.byref(sampling),
-                                   u.data_ptr() if u is not None else None, q.data_ptr() if want_q else None,
-                                   masked.data_ptr() if masked is not None else None,
-                                   tokens.data_ptr() if want_tokens else None, work.data_ptr(), st))
+    work = logits.new_empty(lib.spec_sample_rows_workspace_bytes(n, V) or 16, dtype=torch.uint8)
+    q = logits.new_empty((n, V)) if want_q else None
+    tokens = logits.new_empty(n, dtype=torch.int32) if want_tokens else None
+    call_on(logits.get_device(), lib.spec_sample_rows, logits.data_ptr(), logits.stride(0) if n > 1 else V, n, V,
+            C.byref(sampling), u.data_ptr() if u is not None else None, q.data_ptr() if want_q else None,
+            masked.data_ptr() if masked is not None else None, tokens.data_ptr() if want_tokens else None, work.data_ptr())
     return tokens, q
 
 
@@ -37,8 +34,9 @@ def sample_rows(logits: torch.Tensor, u: Optional[torch.Tensor], temperature: fl
     """A token per row of fp32 logits [n][vocab] (any row stride) by the uniforms u [n] (fp32, on the GPU; None at temperature
     0): (tokens int32 [n], the distributions they were drawn from [n][vocab], or None if not wanted)."""
     if u is not None:
-        need(u.dtype == torch.float32 and u.is_contiguous() and u.device == logits.device and u.numel() == logits.shape[0],
-             "u: float32 [n] on the device of the logits is wanted")
+        if not (u.dtype is torch.float32 and u.is_contiguous() and u.get_device() == logits.get_device() and
+                u.numel() == logits.shape[0]):
+            raise ValueError("u: float32 [n] on the device of the logits is wanted")
     return _call(logits, u, Sampling(temperature, logit_scale, top_k, top_p, min_p), want_q, None, True)
 
 

@@ -8,8 +8,8 @@ from typing import List, Optional, Tuple
 
 import torch
 
-from . import EPI_STORE, EPI_SWIGLU, FP8_BLOCK, SPEC_BF16, SPEC_F32, check, load_library
-from .binding import need as _need, on_device as _On
+from . import EPI_STORE, EPI_SWIGLU, FP8_BLOCK, SPEC_BF16, SPEC_F32, load_library
+from .binding import call_on, need as _need
 
 _TYPES = {torch.float32: SPEC_F32, torch.bfloat16: SPEC_BF16}
 E4M3 = torch.float8_e4m3fn
@@ -21,8 +21,8 @@ def _blocks(k: int) -> int:
 
 def _rows(x: torch.Tensor, name: str) -> int:
     """Row stride of a matrix of rows in fp32 or bf16."""
-    _need(x.is_cuda and x.dim() == 2 and x.dtype in _TYPES, f"{name}: rows in float32 or bfloat16 on a GPU are wanted")
-    _need(x.shape[1] == 1 or x.stride(1) == 1, f"{name}: the elements of a row must be neighbours")
+    if not (x.is_cuda and x.dtype in _TYPES and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1)):
+        raise ValueError(f"{name}: rows in float32 or bfloat16 on a GPU, their elements neighbours, are wanted")
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
@@ -32,33 +32,29 @@ def add_norm_fp8(h: torch.Tensor, delta: Optional[torch.Tensor], gain: torch.Ten
 
     h [M][d] and delta [M][d] fp32 or bf16, rows at any stride (delta's may be 0: the same row for all); gain bf16 [d].
     q e4m3 [M][d], scale fp32 [ceil(d / 128)][M]."""
-    ldh = _rows(h, "h")
-    M, d = h.shape
-    _need(gain.dtype == torch.bfloat16 and gain.device == h.device and tuple(gain.shape) == (d,) and gain.is_contiguous(),
-          "gain: bfloat16 [d] on the device of h is wanted")
-    ldd = 0
+    ldh, (M, d), dev = _rows(h, "h"), h.shape, h.get_device()
+    if not (gain.dtype is torch.bfloat16 and gain.get_device() == dev and gain.shape == (d,) and gain.is_contiguous()):
+        raise ValueError("gain: bfloat16 [d] on the device of h is wanted")
+    dp, dt, ldd = None, 0, 0
     if delta is not None:
         ldd = _rows(delta, "delta")
-        _need(delta.device == h.device and delta.shape == h.shape, "delta: the shape and device of h are wanted")
-    lib = load_library()
-    q = torch.empty((M, d), dtype=E4M3, device=h.device)
-    scale = torch.empty((_blocks(d), M), dtype=torch.float32, device=h.device)
-    with _On(h.device.index) as st:
-        check(lib.spec_add_norm_quant(h.data_ptr(), _TYPES[h.dtype], ldh, delta.data_ptr() if delta is not None else None,
-                                    _TYPES[delta.dtype] if delta is not None else 0, ldd, gain.data_ptr(), eps, M, d,
-                                    q.data_ptr(), scale.data_ptr(), st))
+        if delta.get_device() != dev or delta.shape != h.shape:
+            raise ValueError("delta: the shape and device of h are wanted")
+        dp, dt = delta.data_ptr(), _TYPES[delta.dtype]
+    q = h.new_empty((M, d), dtype=E4M3)
+    scale = h.new_empty((_blocks(d), M), dtype=torch.float32)
+    call_on(dev, load_library().spec_add_norm_quant, h.data_ptr(), _TYPES[h.dtype], ldh, dp, dt, ldd, gain.data_ptr(), eps, M, d,
+            q.data_ptr(), scale.data_ptr())
     return q, scale
 
 
 def quant_fp8(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """(q, scale) of rows x [M][K] in fp32 or bf16 at any row stride: q e4m3 [M][K], scale fp32 [ceil(K / 128)][M]."""
-    ldx = _rows(x, "x")
-    M, K = x.shape
-    lib = load_library()
-    q = torch.empty((M, K), dtype=E4M3, device=x.device)
-    scale = torch.empty((_blocks(K), M), dtype=torch.float32, device=x.device)
-    with _On(x.device.index) as st:
-        check(lib.spec_quant_rows(x.data_ptr(), _TYPES[x.dtype], ldx, M, K, q.data_ptr(), scale.data_ptr(), st))
+    ldx, (M, K) = _rows(x, "x"), x.shape
+    q = x.new_empty((M, K), dtype=E4M3)
+    scale = x.new_empty((_blocks(K), M), dtype=torch.float32)
+    call_on(x.get_device(), load_library().spec_quant_rows, x.data_ptr(), _TYPES[x.dtype], ldx, M, K, q.data_ptr(),
+            scale.data_ptr())
     return q, scale
 
 
@@ -70,8 +66,7 @@ def quant_weight_fp8(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     lib = load_library()
     q = torch.empty((N, K), dtype=E4M3, device=w.device)
     scale = torch.empty((_blocks(N), _blocks(K)), dtype=torch.float32, device=w.device)
-    with _On(w.device.index) as st:
-        check(lib.spec_quant_weight(w.data_ptr(), N, K, q.data_ptr(), scale.data_ptr(), st))
+    call_on(w.get_device(), lib.spec_quant_weight, w.data_ptr(), N, K, q.data_ptr(), scale.data_ptr())
     return q, scale
 
 
@@ -100,12 +95,11 @@ def pack_weights_fp8(mats: List[Tuple[torch.Tensor, torch.Tensor]], interleave: 
     _need(all(lib.spec_packed_quant_bytes(q.shape[0], K) > 0 for q, _ in mats), "need N % 16 == 0 and K % 16 == 0")
     data = torch.empty(sum(lib.spec_packed_quant_bytes(q.shape[0], K) for q, _ in mats), dtype=torch.uint8, device=device)
     scale = torch.empty((N // 16, _blocks(K)), dtype=torch.float32, device=device)
-    with _On(device.index) as st:
-        start = 0
-        for i, (q, s) in enumerate(mats):
-            check(lib.spec_pack_quant(data.data_ptr(), scale.data_ptr(), q.data_ptr(), s.data_ptr(), q.shape[0], K,
-                                           i if interleave else start, len(mats) if interleave else 1, st))
-            start += q.shape[0] // 16
+    start = 0
+    for i, (q, s) in enumerate(mats):
+        call_on(data.get_device(), lib.spec_pack_quant, data.data_ptr(), scale.data_ptr(), q.data_ptr(), s.data_ptr(), q.shape[0], K,
+                i if interleave else start, len(mats) if interleave else 1)
+        start += q.shape[0] // 16
     return Fp8Weight(data, scale, N, K, interleave and len(mats) == 2)
 
 
@@ -115,17 +109,17 @@ def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: Fp8Weight, epilogue: int
 
     epilogue 0: returns y [M][N] in bfloat16 or float32; 2: z [M][N / 2] bf16 = silu(gate) * up of weights packed with
     interleave=True."""
-    M, K = x.shape
-    dev, N = x.device, w.N
-    _need(x.is_cuda and x.dtype == E4M3 and x.is_contiguous() and K == w.K and w.data.device == dev,
-          "x: contiguous e4m3 rows of the weights' width on their device are wanted")
-    _need(x_scale.dtype == torch.float32 and x_scale.is_contiguous() and x_scale.device == dev and
-          tuple(x_scale.shape) == (_blocks(K), M), "x_scale: float32 [ceil(K / 128)][M] is wanted")
-    _need(dtype in _TYPES, "results in bfloat16 or float32")
-    _need(epilogue != EPI_SWIGLU or w.interleaved, "epilogue 2 wants a gate and an up matrix packed with interleave=True")
-    lib = load_library()
-    out = torch.empty((M, N // 2 if epilogue == EPI_SWIGLU else N), dtype=dtype, device=dev)
-    with _On(dev.index) as st:
-        check(lib.spec_gemm_quant(out.data_ptr(), _TYPES[dtype], x.data_ptr(), x_scale.data_ptr(), w.data.data_ptr(),
-                                  w.scale.data_ptr(), M, N, K, epilogue, st))
+    (M, K), dev, N = x.shape, x.get_device(), w.N
+    if not (x.is_cuda and x.dtype is E4M3 and x.is_contiguous() and K == w.K and w.data.get_device() == dev):
+        raise ValueError("x: contiguous e4m3 rows of the weights' width on their device are wanted")
+    if not (x_scale.dtype is torch.float32 and x_scale.is_contiguous() and x_scale.get_device() == dev and
+            x_scale.shape == (_blocks(K), M)):
+        raise ValueError("x_scale: float32 [ceil(K / 128)][M] is wanted")
+    if dtype not in _TYPES:
+        raise ValueError("results in bfloat16 or float32")
+    if epilogue == EPI_SWIGLU and not w.interleaved:
+        raise ValueError("epilogue 2 wants a gate and an up matrix packed with interleave=True")
+    out = x.new_empty((M, N // 2 if epilogue == EPI_SWIGLU else N), dtype=dtype)
+    call_on(dev, load_library().spec_gemm_quant, out.data_ptr(), _TYPES[dtype], x.data_ptr(), x_scale.data_ptr(),
+            w.data.data_ptr(), w.scale.data_ptr(), M, N, K, epilogue)
     return out
