@@ -29,7 +29,7 @@
 #define FL_CHUNKS_MAX (SPEC_SAMPLE_VOCAB_MAX / (FL_QUAD * FL_QUADS_MAX))
 #define FL_BINS 256
 #define FL_GRID 8.0                       // classes per unit of z
-#define FL_LIST 8192                      // candidates that are kept as a list; beyond, the row is read again
+#define FL_LIST 8192                      // most candidates that are kept as a list; beyond, the row is read again
 #define FL_GROUP 16
 #define FL_FEW 1024                       // largest top-k that goes by groups
 #define FL_ONE 0x1p43                     // units of a weight of 1
@@ -53,7 +53,7 @@ struct FilterWork {              // arrays over the rows of a call
   double* kept;                  // [row][C]: units kept
   u64* mass;                     // [row][C][FL_BINS]
   unsigned* count;               // [row][C][FL_BINS]
-  u64* list;                     // [row][FL_LIST]
+  u64* list;                     // [row][L]
   FilterInfo* info;              // [row]
   FilterEnd* end;                // [row]
   unsigned* listed;              // [row]
@@ -62,7 +62,7 @@ struct FilterWork {              // arrays over the rows of a call
 struct FilterArgs {
   const float* logits;
   size_t ld;
-  int V, chunk, C, G, greedy, top_k;    // ids of a chunk, chunks, groups; top_k 0: off
+  int V, chunk, C, G, L, greedy, top_k;    // ids of a chunk, chunks, groups, room of a list; top_k 0: off
   double mult, top_p, min_p;     // top_p 1: off
   const float* u;
   float *q, *masked;
@@ -518,7 +518,7 @@ __global__ __launch_bounds__(FL_THREADS) void filter_collect_kernel(FilterArgs a
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (mine >> (j * 4 + i) & 1) {
-        if (at < FL_LIST) a.w.list[(size_t)row * FL_LIST + at] = order_of(x[j][i], id_of<Q>(chunk, j, i));
+        if (at < (unsigned)a.L) a.w.list[(size_t)row * a.L + at] = order_of(x[j][i], id_of<Q>(chunk, j, i));
         ++at;
       }
 }
@@ -646,12 +646,12 @@ __global__ __launch_bounds__(FL_THREADS) void filter_resolve_kernel(FilterArgs a
   auto to = [&](int b) { return b >= FL_BINS - 1 ? last_order(-INFINITY) : last_order((float)((line - b) / FL_GRID / a.mult)); };
   const float* x = a.logits + (size_t)row * a.ld;
   const unsigned listed = a.w.listed[row];
-  const bool whole = listed > FL_LIST;
+  const bool whole = listed > (unsigned)a.L;
   const int n = whole ? a.V : (int)listed;
   for (int c = threadIdx.x; c < a.C; c += FL_THREADS) chunk_mass[c] = 0;
   if (!whole)
     for (int i = threadIdx.x; i < n; i += FL_THREADS) {
-      const u64 o = a.w.list[(size_t)row * FL_LIST + i];
+      const u64 o = a.w.list[(size_t)row * a.L + i];
       list[i] = o;
       amount[i] = units(weight(distance(top, logit_of(o), a.mult)));
     }
@@ -1065,18 +1065,20 @@ __global__ __launch_bounds__(W * 64) void filter_few_kernel(FilterArgs a, int cl
 
 // ---- the call -------------------------------------------------------------------------------------------------------
 // Quads of a chunk: as few as still leave no more than two workgroups per CU (256 of them), so that a workgroup's share of 64-bit
-// work is small; but every workgroup of `collect` adds up all chunks' classes, so not beyond 32 chunks for it (128 else: two per
-// lane).  By rows and ids alone, so that the workspace can be sized.
+// work is small.  Every workgroup of `collect` reads all chunks' classes (3 KiB each), so there not beyond 25 MB of that: one row
+// of 160000 ids, top-p 0.9, 39 -> 31 us.  At most 128 chunks: two per lane.  By rows and ids alone, so that the workspace can be
+// sized.
 static int filter_quads(int rows, int V, bool classes) {
   int q = FL_QUADS_MAX;
   while (q > 1) {
-    const int C = (V + FL_QUAD * (q / 2) - 1) / (FL_QUAD * (q / 2));
-    if ((long long)C * rows > 512 || C > (classes ? 32 : 128)) break;
+    const long long C = (V + FL_QUAD * (q / 2) - 1) / (FL_QUAD * (q / 2));
+    if (C * rows > 512 || C > 128 || (classes && C * C * rows > 8192)) break;
     q /= 2;
   }
   return q;
 }
 static size_t filter_chunks(int V, int quads) { return ((size_t)V + FL_QUAD * quads - 1) / (FL_QUAD * quads); }
+static int filter_room(int V) { return V < FL_LIST ? V : FL_LIST; }
 static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
   const size_t n = rows, classes = filter_chunks(V, filter_quads(rows, V, true));
   const size_t few = filter_chunks(V, filter_quads(rows, V, false)), C = few > classes ? few : classes;
@@ -1088,7 +1090,7 @@ static size_t filter_layout(int rows, int V, char* base, FilterWork* w) {
     return p;
   };
   w->mass = (u64*)take(n * classes * FL_BINS * 8);
-  w->list = (u64*)take(n * FL_LIST * 8);
+  w->list = (u64*)take(n * filter_room(V) * 8);
   w->count = (unsigned*)take(n * classes * FL_BINS * 4);
   w->kept = (double*)take(n * C * 8);
   w->top = (float*)take(n * C * 4);
@@ -1142,6 +1144,7 @@ hipError_t launch_sample_rows(const float* logits, size_t ld, int rows, int V, c
   a.logits = logits;
   a.ld = ld;
   a.V = V;
+  a.L = filter_room(V);
   a.greedy = s.temperature == 0.0f;
   a.mult = a.greedy ? 1.0 : (double)s.logit_scale / (double)s.temperature;
   a.top_k = s.top_k > 0 && s.top_k < V ? s.top_k : 0;

@@ -202,6 +202,9 @@ hipError_t launch_pack_weight_fp8(void* dst, float* dst_scale, const void* src, 
                                   int panel_start, int panel_step, hipStream_t st);
 hipError_t launch_gemm_fp8(const uint8_t* x, const float* xs, const void* w, const float* ws, int M, int N, int K, int swiglu,
                            void* out, int out_type, hipStream_t st);
+// the tile that it takes from 33 rows on, by rows, panels and blocks of 128 columns, for bf16 or (exact) fp32 results: 0 = 256 x 256,
+// 1 = 256 x 192 (both bf16 only), 2 = 128 x 256, 3 = 128 x 128, 4 = 64 x 64
+int fp8_tile(int M, int NT, int KB, bool exact);
 
 // sampling / acceptance
 struct AcceptArgs {

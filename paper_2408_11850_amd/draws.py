@@ -13,6 +13,11 @@ from . import Sampling, load_library
 from .binding import call_on, need
 
 
+def _sampling(temperature: float, logit_scale: float, top_k: int, top_p: float, min_p: float) -> Sampling:
+    need(0 <= top_k < 1 << 31, "top_k: 0 or a number of ids")            # the struct would keep its low 32 bits
+    return Sampling(temperature, logit_scale, top_k, top_p, min_p)
+
+
 def _call(logits: torch.Tensor, u, sampling, want_q: bool, masked, want_tokens: bool):
     if not (logits.is_cuda and logits.dtype is torch.float32 and logits.dim() == 2 and
             (logits.stride(1) == 1 or logits.shape[1] == 1)):
@@ -37,7 +42,7 @@ def sample_rows(logits: torch.Tensor, u: Optional[torch.Tensor], temperature: fl
         if not (u.dtype is torch.float32 and u.is_contiguous() and u.get_device() == logits.get_device() and
                 u.numel() == logits.shape[0]):
             raise ValueError("u: float32 [n] on the device of the logits is wanted")
-    return _call(logits, u, Sampling(temperature, logit_scale, top_k, top_p, min_p), want_q, None, True)
+    return _call(logits, u, _sampling(temperature, logit_scale, top_k, top_p, min_p), want_q, None, True)
 
 
 def filter_rows(logits: torch.Tensor, temperature: float = 1.0, logit_scale: float = 1.0, top_k: int = 0, top_p: float = 1.0,
@@ -48,5 +53,5 @@ def filter_rows(logits: torch.Tensor, temperature: float = 1.0, logit_scale: flo
         out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
     need(out.dtype == torch.float32 and out.is_contiguous() and out.device == logits.device and out.shape == logits.shape,
          "out: contiguous float32 of the logits' shape is wanted")
-    _call(logits, None, Sampling(temperature, logit_scale, top_k, top_p, min_p), False, out, False)
+    _call(logits, None, _sampling(temperature, logit_scale, top_k, top_p, min_p), False, out, False)
     return out

@@ -46,6 +46,9 @@ def test_workspace_and_python_refusals(amd):
         amd.sample_rows(torch.zeros(2, 8), torch.zeros(2))
     with pytest.raises(ValueError):
         amd.filter_rows(torch.zeros(2, 8))
+    for k in (-1, 1 << 31, (1 << 32) + 5):
+        with pytest.raises(ValueError):
+            amd.sample_rows(torch.zeros(2, 8), torch.zeros(2), top_k=k)
 
 
 def test_the_oracle_on_hand_worked_rows():

@@ -176,6 +176,48 @@ def test_strided_rows_odd_addresses_and_results_in_place():
     assert torch.equal(own, ref[1])
 
 
+@pytest.mark.parametrize("V", [270001, 600001, 1048576])
+@pytest.mark.parametrize("how", [dict(), dict(top_k=1000), dict(top_k=5000, top_p=0.9), dict(top_p=0.95, temperature=1.3), dict(min_p=0.001)],
+                         ids=str)
+def test_the_longest_rows(V, how):
+    """Chunks of every size; more groups than registers hold; nuclei of tens of thousands of ids."""
+    amd = _amd()
+    print(f"draws V={V} {how}", flush=True)
+    x, u = _logits(1, V, 130), _u(1, 8)
+    tokens, q = amd.sample_rows(x.cuda(), u.cuda(), **how)
+    _check(x, u, tokens, q, amd.filter_rows(x.cuda(), **how), **how)
+
+
+@pytest.mark.parametrize("how", [dict(top_k=7), dict(top_p=0.7), dict(min_p=0.2), dict()], ids=str)
+def test_many_rows(how):
+    amd = _amd()
+    n, V = 3001, 67
+    x, u = _logits(n, V, 131), _u(n, 9)
+    tokens, q = amd.sample_rows(x.cuda(), u.cuda(), **how)
+    some = torch.tensor([0, 1, 1500, 2999, 3000])
+    _check(x[some], u[some], tokens.cpu()[some], q.cpu()[some], None, **how)
+    one = [amd.sample_rows(x[i:i + 1].cuda(), u[i:i + 1].cuda(), **how)[0] for i in range(0, n, 500)]
+    assert torch.equal(torch.cat(one), tokens[::500])
+
+
+def test_every_result_of_one_call():
+    """q, the truncated logits and the tokens together are what calls of their own give."""
+    import ctypes as C
+    amd = _amd()
+    n, V = 3, 33333
+    x, u = _logits(n, V, 132).cuda(), _u(n, 10).cuda()
+    lib = amd.load_library()
+    for how in (dict(), dict(top_k=30), dict(top_k=3000, top_p=0.6), dict(top_p=0.9, min_p=0.0001), dict(temperature=0.0)):
+        q, m = torch.empty_like(x), torch.empty_like(x)
+        tok = torch.empty(n, dtype=torch.int32, device="cuda")
+        work = torch.empty(lib.spec_sample_rows_workspace_bytes(n, V), dtype=torch.uint8, device="cuda")
+        s = amd.Sampling(how.get("temperature", 1.0), 1.0, how.get("top_k", 0), how.get("top_p", 1.0), how.get("min_p", 0.0))
+        amd.check(lib.spec_sample_rows(x.data_ptr(), V, n, V, C.byref(s), u.data_ptr(), q.data_ptr(), m.data_ptr(), tok.data_ptr(),
+                                       work.data_ptr(), torch.cuda.current_stream().cuda_stream))
+        ref = amd.sample_rows(x, u, **how)
+        assert torch.equal(tok, ref[0]) and torch.equal(q, ref[1]) and torch.equal(m, amd.filter_rows(x, **how))
+
+
 def test_streams_graphs_and_repeats():
     amd = _amd()
     x, u = _logits(4, 70000, 57, True).cuda(), _u(4, 6).cuda()
