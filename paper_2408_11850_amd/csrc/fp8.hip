@@ -661,7 +661,7 @@ static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
 // per MFMA scale and add, and every block passes LDS once per wave that uses it.
 int fp8_tile(int M, int NT, int KB, bool exact) {
   static const struct { int tokens, panels, per_cu; float round, step, busy; } T[2][5] = {
-      {{256, 16, 1, 3.0f, 1.415f, 0.480f}, {256, 12, 1, 1.9f, 1.302f, 0.333f}, {128, 16, 1, 4.2f, 0.854f, 0.255f}, {128, 8, 1, 3.2f, 0.537f, 0.124f}, {64, 4, 2, 3.2f, 0.304f, 0.151f}},
+      {{256, 16, 1, 3.0f, 1.415f, 0.480f}, {256, 12, 1, 3.0f, 1.274f, 0.339f}, {128, 16, 1, 4.2f, 0.854f, 0.255f}, {128, 8, 1, 3.2f, 0.537f, 0.124f}, {64, 4, 2, 3.2f, 0.304f, 0.151f}},
       {{0, 0, 0, 0.f, 0.f, 0.f}, {0, 0, 0, 0.f, 0.f, 0.f}, {128, 16, 1, 4.4f, 1.525f, 0.315f}, {128, 8, 1, 3.4f, 0.969f, 0.170f}, {64, 4, 2, 2.9f, 0.479f, 0.210f}}};
   int best = 4;
   double best_us = 0.0;
