@@ -76,15 +76,25 @@ __device__ __forceinline__ float block_scale(const float (&v)[8]) {
   float a = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a = fmaxf(a, fabsf(v[i]));
-  return fmaxf(row16_max(a), FP8_LEAST) * (1.0f / E4M3_MAX);
+  return fmaxf(row16_max(a), FP8_LEAST) / E4M3_MAX;
+}
+// The codes are those of the correctly rounded quotient v / scale: t = v * inv is off by less than two steps, v - t * scale is exact
+// in a multiply-add, and its share of the quotient added once rounds to the nearest (Markstein, for a correctly rounded inv).
+// The product alone took 1.5 times as many values for the other neighbour of a border (9.7e-7 of all, 6.5e-7 here).
+__device__ __forceinline__ float quotient(float v, float scale, float inv) {
+  const float t = v * inv;
+  return fmaf(fmaf(-t, scale, v), inv, t);
 }
 __device__ __forceinline__ uint2 to_e4m3(const float (&v)[8], float scale) {
-  const float inv = 1.0f / scale;                  // |v * inv| <= 448 up to two roundings, which round to 448
+  const float inv = 1.0f / scale;                  // the quotients reach 448 up to the scale's rounding, which rounds to 448
+  float t[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = quotient(v[i], scale, inv);
   int lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inv, v[1] * inv, lo, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inv, v[5] * inv, hi, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, hi, true);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[0], t[1], lo, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(t[2], t[3], lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(t[4], t[5], hi, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(t[6], t[7], hi, true);
   return make_uint2((unsigned)lo, (unsigned)hi);
 }
 
@@ -212,7 +222,7 @@ __global__ __launch_bounds__(256) void quant_weight_kernel(const bf16* __restric
   if (c == 0) top[r] = a;
   __syncthreads();
   a = row16_max(top[c]);
-  const float s = fmaxf(a, FP8_LEAST) * (1.0f / E4M3_MAX);
+  const float s = fmaxf(a, FP8_LEAST) / E4M3_MAX;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const int n = blockIdx.y * 128 + j * 16 + r;
