@@ -367,11 +367,13 @@ __global__ __launch_bounds__(SK_WAVES * 64, OCC) void fp8_skinny_kernel(Fp8Args 
   }
   u32x4 wq[D][RP][2], xq[D][MT][XL];
   float xs[D][MT], ws[RP], wn[RP];     // lane l of ws, wn: the panel's scale in stage l of this round, of the next one
+  // no scale where the wave has no block: the next one, of another wave or panel, may be a NaN, which the zeros there would become
   auto load_ws = [&](int u, int r, float (&to)[RP]) {
+    const unsigned mine = lane < min(D, ns - r * D) ? lane * 4u : SK_SKIP;
 #pragma unroll
     for (int p = 0; p < RP; ++p) {
       const unsigned at = (unsigned)min(u * RP + p, a.NT - 1) * (unsigned)a.KB + min(s0 + r * D, a.KB - 1);
-      to[p] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(pr, lane < D ? lane * 4u : SK_SKIP, at * 4u, 0));
+      to[p] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(pr, mine, at * 4u, 0));
     }
   };
   // stage s: block r * D + s of the wave's share of unit u.  What is not there is skipped by the lanes' offsets; the scalar ones
