@@ -265,18 +265,18 @@ int spec_dense_gemm(float* y_dev, void* z_dev, const void* x_dev, const void* w_
  * of an element is e4m3 * scale.  Weights have one per block of 128 x 128: scale[ceil(N/128)][ceil(K/128)].  A scale is
  * (largest magnitude of the block) / 448; blocks below 2^-100 take 2^-100 / 448.  A NaN stays a NaN of its own, an infinite
  * value makes its block NaN.  K (d) is a multiple of 16, N of 16; both at most SPEC_FP8_K_MAX, rows of the first two calls
- * at most SPEC_FP8_ROW_MAX.  All are asynchronous on `stream`, allocate nothing and can be captured. */
+ * at most SPEC_FP8_ROW_MAX, and there M * ceil(d / 512) is below 2^26.  All are asynchronous on `stream`, allocate nothing and can be captured. */
 enum { SPEC_F32 = 0, SPEC_BF16 = 1 };
 #define SPEC_FP8_ROW_MAX 32768
 #define SPEC_FP8_K_MAX 1048576
 
 /* Residual add, RMS norm and gain, rounded to e4m3: h[m] += delta[m] (delta may be NULL), in place and rounded to the type of
  * h; then y = h / sqrt(mean(h^2) + eps) * gain of what is stored, and its e4m3 values q[M][d] and scales.  h, delta: device,
- * SPEC_F32 or SPEC_BF16, row strides ldh, ldd >= d (elements; ldd also 0: one row for all); gain bf16 [d]; sums in fp32.  A
+ * SPEC_F32 or SPEC_BF16, row strides ldh, ldd >= d (elements; ldd also 0: one row for all); delta is h itself or shares no element with it; gain bf16 [d]; sums in fp32.  A
  * row's results do not depend on M.  q starts at a multiple of 8, the others at multiples of their elements. */
 int spec_add_norm_quant(void* h_dev, int h_type, long long ldh, const void* delta_dev, int delta_type, long long ldd,
                       const void* gain_dev, float eps, int M, int d, void* q_dev, float* scale_dev, void* stream);
-/* The e4m3 values q[M][K] and scales of rows as they are: what a projection reads that no norm precedes. */
+/* The e4m3 values q[M][K] and scales of rows as they are (ldx >= K, or 0): what a projection reads that no norm precedes. */
 int spec_quant_rows(const void* x_dev, int x_type, long long ldx, int M, int K, void* q_dev, float* scale_dev, void* stream);
 /* The same of a weight matrix W[N][K] (bf16 row-major, device), with its scales per block of 128 x 128. */
 int spec_quant_weight(const void* w_dev, int N, int K, void* q_dev, float* scale_dev, void* stream);

@@ -1443,6 +1443,8 @@ static bool off_element(const void* p, int type) { return off_by(p, type == SPEC
 static int check_fp8_rows(int M, int d) {
   if (M < 1 || d < 16 || d % 16 || d > SPEC_FP8_ROW_MAX)
     FAIL(SPEC_E_INVAL, "need M >= 1 and rows of 16 to %d columns, a multiple of 16", SPEC_FP8_ROW_MAX);
+  if ((size_t)M * ((d + 511) / 512) >= (1u << 26))          // a wave each; a launch has at most 2^32 - 1 threads
+    FAIL(SPEC_E_INVAL, "too many rows: M * ceil(d / 512) has to be below 2^26");
   return SPEC_OK;
 }
 extern "C" int spec_add_norm_quant(void* h, int h_type, long long ldh, const void* delta, int delta_type, long long ldd,

@@ -23,6 +23,8 @@ def _rows(x: torch.Tensor, name: str) -> int:
     """Row stride of a matrix of rows in fp32 or bf16."""
     if not (x.is_cuda and x.dtype in _TYPES and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1)):
         raise ValueError(f"{name}: rows in float32 or bfloat16 on a GPU, their elements neighbours, are wanted")
+    if x.shape[0] >> 31:                               # ctypes would keep the low 32 bits
+        raise ValueError(f"{name}: too many rows")
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
@@ -30,7 +32,8 @@ def add_norm_fp8(h: torch.Tensor, delta: Optional[torch.Tensor], gain: torch.Ten
                  eps: float) -> Tuple[torch.Tensor, torch.Tensor]:
     """h += delta in place (None: nothing is added), then (q, scale) of the RMS norm of h times gain.
 
-    h [M][d] and delta [M][d] fp32 or bf16, rows at any stride (delta's may be 0: the same row for all); gain bf16 [d].
+    h [M][d] and delta [M][d] fp32 or bf16, rows at any stride (delta's may be 0: the same row for all; it is h itself
+    or shares no element with it); gain bf16 [d].
     q e4m3 [M][d], scale fp32 [ceil(d / 128)][M]."""
     ldh, (M, d), dev = _rows(h, "h"), h.shape, h.get_device()
     if not (gain.dtype is torch.bfloat16 and gain.get_device() == dev and gain.shape == (d,) and gain.is_contiguous()):
@@ -76,6 +79,11 @@ class Fp8Weight:
     __slots__ = ("data", "scale", "N", "K", "interleaved")
 
     def __init__(self, data: torch.Tensor, scale: torch.Tensor, N: int, K: int, interleaved: bool):
+        _need(N > 0 and N % 16 == 0 and K > 0 and K % 16 == 0, "need N % 16 == 0 and K % 16 == 0")
+        _need(data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous() and
+              data.numel() == N // 16 * _blocks(K) * 2048, "data: 2048 bytes per panel of 16 rows and block of 128 are wanted")
+        _need(scale.dtype == torch.float32 and scale.is_contiguous() and scale.device == data.device and
+              tuple(scale.shape) == (N // 16, _blocks(K)), "scale: float32 [N / 16][ceil(K / 128)] is wanted")
         self.data, self.scale, self.N, self.K, self.interleaved = data, scale, N, K, interleaved
 
 
@@ -110,7 +118,7 @@ def gemm_fp8(x: torch.Tensor, x_scale: torch.Tensor, w: Fp8Weight, epilogue: int
     epilogue 0: returns y [M][N] in bfloat16 or float32; 2: z [M][N / 2] bf16 = silu(gate) * up of weights packed with
     interleave=True."""
     (M, K), dev, N = x.shape, x.get_device(), w.N
-    if not (x.is_cuda and x.dtype is E4M3 and x.is_contiguous() and K == w.K and w.data.get_device() == dev):
+    if not (x.is_cuda and x.dtype is E4M3 and x.is_contiguous() and not M >> 31 and K == w.K and w.data.get_device() == dev):
         raise ValueError("x: contiguous e4m3 rows of the weights' width on their device are wanted")
     if not (x_scale.dtype is torch.float32 and x_scale.is_contiguous() and x_scale.get_device() == dev and
             x_scale.shape == (_blocks(K), M)):

@@ -82,3 +82,9 @@ def test_python_calls_refuse_host_tensors_and_wrong_types(amd):
         amd.pack_weights_fp8([])
     with pytest.raises(ValueError):
         amd.pack_weights_fp8([(h.to(torch.float8_e4m3fn), torch.ones(1, 2))])
+
+
+@pytest.mark.parametrize("M,d", [(1 << 26, 16), (1 << 26, 512), (1 << 25, 528), (1 << 22, 8192), (1 << 20, 32768), (2 ** 31 - 1, 32768)])
+def test_rows_beyond_a_launch(amd, M, d):
+    assert _norm(amd.load_library(), M=M, d=d, ldh=d, ldd=d) == amd.SPEC_E_INVAL
+    assert amd.load_library().spec_quant_rows(P, 1, d, M, d, P, P, None) == amd.SPEC_E_INVAL
