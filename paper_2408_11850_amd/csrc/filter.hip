@@ -45,7 +45,7 @@ static_assert(FL_CHUNKS_MAX <= 128, "two chunks per lane");
 
 struct FilterInfo {              // of a row: borders by classes, masses relative to its largest weight
   int kbin, plo, phi, low, n_before;  // class of the k-th id; classes that top-p may end in; first that min-p leaves out; ids before kbin
-  double m_before_k, m_before_p, mass;
+  double m_before_k, m_before_p, mass;  // mass: that of the ids top-p counts, where no kbin says which
 };
 struct FilterEnd {
   u64 last;                      // order of the last kept id
@@ -417,9 +417,13 @@ __device__ __forceinline__ FilterInfo find_classes(const FilterArgs& a, float to
       const int at = __ffsll((long long)some) - 1;
       f.low = at * 4 + lane_t(k, at);
     }
-    // borders among ids that min-p leaves out anyway
-    if (f.kbin >= f.low) f.kbin = FL_BINS;
+    // Borders among ids that min-p leaves out anyway; but as long as top-p's counts, it takes its share of the mass of the first k
+    // ids, so the k-th is still looked for (not in the last class, whose ids have no units).
     if (f.plo >= f.low) f.plo = f.phi = FL_BINS;
+    if (f.kbin >= f.low && (f.plo == FL_BINS || f.kbin == FL_BINS - 1)) {
+      f.mass = f.m_before_k;
+      f.kbin = FL_BINS;
+    }
   }
   return f;
 }
