@@ -314,7 +314,7 @@ int spec_sample_row(const float* logits_dev, int vocab, float temperature, float
  *                              temperature and logit_scale, for the target to be truncated as the draft model is
  *   tok_out[n_rows]            the first id at which the sum of q passes u_dev[row] (below 0 and NaN as 0, from 1 on the last id)
  * each of them may be NULL, but not all; u_dev only matters for tok_out at a temperature.  q_out or masked_out may be the
- * logits (ld == vocab).  A row without a finite logit, or with a NaN or +inf, has no distribution: NaN and token -1 (at
+ * logits (ld == vocab); any other overlap of the results and the workspace, with each other or with what is read, is refused.  A row without a finite logit, or with a NaN or +inf, has no distribution: NaN and token -1 (at
  * temperature 0 a NaN counts as none, and a row without any logit above -inf gives id 0).  Borders and draws are decided in 64
  * bits, the results do not depend on the order in which anything runs.  temperature >= 0, logit_scale > 0, both finite,
  * top_k >= 0, top_p and min_p in [0, 1], n_rows <= 65535, vocab <= SPEC_SAMPLE_VOCAB_MAX.  work_dev: 16-byte aligned device

@@ -1534,6 +1534,17 @@ static int check_sample_rows(int n_rows, int vocab) {
     FAIL(SPEC_E_INVAL, "need 1 to 65535 rows of 1 to %d ids", SPEC_SAMPLE_VOCAB_MAX);
   return SPEC_OK;
 }
+static bool meet(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return na && nb && (x < y ? y - x < na : x - y < nb);
+}
+// whether any of n rows of `width` bytes, ld bytes apart, meets p
+static bool meets_rows(const void* rows, size_t ld, size_t n, size_t width, const void* p, size_t bytes) {
+  const uintptr_t x = (uintptr_t)rows, y = (uintptr_t)p;
+  if (!bytes || y < x) return bytes && x - y < bytes;
+  const size_t at = y - x, first = at < width ? 0 : (at - width) / ld + 1;      // the first row that ends behind p's first byte
+  return first < n && first <= (at + bytes - 1) / ld;
+}
 extern "C" size_t spec_sample_rows_workspace_bytes(int n_rows, int vocab) {
   return check_sample_rows(n_rows, vocab) ? 0 : filter_work_bytes(n_rows, vocab);
 }
@@ -1552,6 +1563,16 @@ extern "C" int spec_sample_rows(const float* logits, long long ld, int n_rows, i
   if ((q_out == logits || masked_out == logits) && ld != vocab) FAIL(SPEC_E_INVAL, "results in place need ld == vocab");
   if (off_by(logits, 4) || off_by(u, 4) || off_by(q_out, 4) || off_by(masked_out, 4) || off_by(tok_out, 4) || off_by(work, 16))
     FAIL(SPEC_E_INVAL, "misaligned operand");
+  const size_t row = (size_t)vocab * 4, n = n_rows;
+  const struct { const void* p; size_t bytes; } to[4] = {{q_out, q_out ? n * row : 0}, {masked_out, masked_out ? n * row : 0},
+                                                         {tok_out, tok_out ? n * 4 : 0}, {work, filter_work_bytes(n_rows, vocab)}};
+  for (int i = 0; i < 4; ++i) {
+    bool clash = to[i].p != logits && meets_rows(logits, (size_t)ld * 4, n, row, to[i].p, to[i].bytes);
+    clash |= i >= 2 && to[i].p == logits && to[i].bytes;
+    clash |= tok_out && s->temperature > 0.0f && meet(u, n * 4, to[i].p, to[i].bytes);
+    for (int j = 0; j < i; ++j) clash |= meet(to[j].p, to[j].bytes, to[i].p, to[i].bytes);
+    if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
+  }
   HIPCHK(launch_sample_rows(logits, (size_t)ld, n_rows, vocab, *s, u, q_out, masked_out, tok_out, work, (hipStream_t)stream));
   return SPEC_OK;
 }

@@ -48,7 +48,7 @@ def sample_rows(logits: torch.Tensor, u: Optional[torch.Tensor], temperature: fl
 def filter_rows(logits: torch.Tensor, temperature: float = 1.0, logit_scale: float = 1.0, top_k: int = 0, top_p: float = 1.0,
                 min_p: float = 0.0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The logits with -inf where sample_rows would keep no id: p_logits for accept_rows with the same temperature and
-    logit_scale.  out: contiguous [n][vocab], may be the logits."""
+    logit_scale.  out: contiguous [n][vocab], may be the logits, but not overlap them otherwise."""
     if out is None:
         out = torch.empty(logits.shape, dtype=torch.float32, device=logits.device)
     need(out.dtype == torch.float32 and out.is_contiguous() and out.device == logits.device and out.shape == logits.shape,
