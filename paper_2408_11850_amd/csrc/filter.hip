@@ -89,7 +89,8 @@ __device__ __forceinline__ float logit_of(u64 order) {
 // Bounds of the orders of logits up to / from a value that roundings have moved by less than 1e-6 of it.
 __device__ __forceinline__ u64 first_order(float x) { return order_of(x + (fabsf(x) * 1e-6f + 1e-44f), 0); }
 __device__ __forceinline__ u64 last_order(float x) { return order_of(x - (fabsf(x) * 1e-6f + 1e-44f), -1); }
-// exp(-d), d >= 0: 2^-n times the Taylor series of 2^f, |f| <= 1/2, to the 12th power (6e-15 of the value)
+// exp(-d), d >= 0: 2^-n times the Taylor series of 2^f, |f| <= 1/2, to the 12th power.  Against 60 digits off by up to 3e-16 of the
+// value below d = 1, and by 1.2e-16 d beyond, the rounding of y (1.1e-14 up to 100, 4.9e-14 up to 700); d itself has two roundings.
 __device__ __forceinline__ double weight(double d) {
   const double y = fmin(d, 1000.0) * 1.4426950408889634074, n = rint(y), t = (n - y) * 0.69314718055994530942;
   double p = 1.0 / 479001600.0;
