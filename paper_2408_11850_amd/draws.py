@@ -23,6 +23,8 @@ def _call(logits: torch.Tensor, u, sampling, want_q: bool, masked, want_tokens: 
             (logits.stride(1) == 1 or logits.shape[1] == 1)):
         raise ValueError("logits: rows in float32 on a GPU are wanted")
     n, V = logits.shape
+    if n >> 31 or V >> 31:                                               # ctypes would keep the low 32 bits
+        raise ValueError("logits: too many rows or ids")
     lib = load_library()
     work = logits.new_empty(lib.spec_sample_rows_workspace_bytes(n, V) or 16, dtype=torch.uint8)
     q = logits.new_empty((n, V)) if want_q else None
