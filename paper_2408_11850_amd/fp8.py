@@ -23,8 +23,8 @@ def _rows(x: torch.Tensor, name: str) -> int:
     """Row stride of a matrix of rows in fp32 or bf16."""
     if not (x.is_cuda and x.dtype in _TYPES and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1)):
         raise ValueError(f"{name}: rows in float32 or bfloat16 on a GPU, their elements neighbours, are wanted")
-    if x.shape[0] >> 31:                               # ctypes would keep the low 32 bits
-        raise ValueError(f"{name}: too many rows")
+    if x.shape[0] >> 31 or x.shape[1] >> 31:           # ctypes would keep the low 32 bits
+        raise ValueError(f"{name}: rows and columns below 2^31 are wanted")
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
@@ -66,6 +66,7 @@ def quant_weight_fp8(w: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     _need(w.is_cuda and w.dim() == 2 and w.dtype == torch.bfloat16 and w.is_contiguous(),
           "w: a contiguous bfloat16 matrix on a GPU is wanted")
     N, K = w.shape
+    _need(not (N >> 31 or K >> 31), "w: rows and columns below 2^31 are wanted")
     lib = load_library()
     q = torch.empty((N, K), dtype=E4M3, device=w.device)
     scale = torch.empty((_blocks(N), _blocks(K)), dtype=torch.float32, device=w.device)
@@ -80,6 +81,7 @@ class Fp8Weight:
 
     def __init__(self, data: torch.Tensor, scale: torch.Tensor, N: int, K: int, interleaved: bool):
         _need(N > 0 and N % 16 == 0 and K > 0 and K % 16 == 0, "need N % 16 == 0 and K % 16 == 0")
+        _need(not (N >> 31 or K >> 31), "need N and K below 2^31")
         _need(data.is_cuda and data.dtype == torch.uint8 and data.is_contiguous() and
               data.numel() == N // 16 * _blocks(K) * 2048, "data: 2048 bytes per panel of 16 rows and block of 128 are wanted")
         _need(scale.dtype == torch.float32 and scale.is_contiguous() and scale.device == data.device and
@@ -100,6 +102,7 @@ def pack_weights_fp8(mats: List[Tuple[torch.Tensor, torch.Tensor]], interleave: 
         _need(not interleave or q.shape == mats[0][0].shape, "only matrices of one shape can be interleaved")
     lib = load_library()
     N = sum(q.shape[0] for q, _ in mats)
+    _need(not (N >> 31 or K >> 31), "rows, of all matrices together, and columns below 2^31 are wanted")
     _need(all(lib.spec_packed_quant_bytes(q.shape[0], K) > 0 for q, _ in mats), "need N % 16 == 0 and K % 16 == 0")
     data = torch.empty(sum(lib.spec_packed_quant_bytes(q.shape[0], K) for q, _ in mats), dtype=torch.uint8, device=device)
     scale = torch.empty((N // 16, _blocks(K)), dtype=torch.float32, device=device)

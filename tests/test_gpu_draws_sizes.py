@@ -7,6 +7,13 @@ from tests.util import gpu_available
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs a GPU")]
 
 
+@pytest.fixture(autouse=True)
+def give_back():
+    """The large tensors do not stay in the allocator's cache."""
+    yield
+    torch.cuda.empty_cache()
+
+
 @pytest.mark.parametrize("n", [(1 << 32) + 1, 1 << 31])
 def test_rows(n):
     import paper_2408_11850_amd as amd
