@@ -25,6 +25,8 @@
 //   1 row of 32000, a top-k that goes by groups     groups 2.8, few 7.8
 //   64 rows of 128256, top-k 1000                   groups 10.3 (66 MB read and written), few 23.3
 //   8 rows of 128256, by classes                    bins 5.2, collect 8.6, resolve 2.7, finish 7.2
+#include <float.h>
+
 #include "spec_internal.h"
 
 #define FL_THREADS 512
@@ -86,9 +88,16 @@ __device__ __forceinline__ float logit_of(u64 order) {
   const unsigned key = ~(unsigned)(order >> 32);
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
-// Bounds of the orders of logits up to / from a value that roundings have moved by less than 1e-6 of it.
-__device__ __forceinline__ u64 first_order(float x) { return order_of(x + (fabsf(x) * 1e-6f + 1e-44f), 0); }
-__device__ __forceinline__ u64 last_order(float x) { return order_of(x - (fabsf(x) * 1e-6f + 1e-44f), -1); }
+// Bounds of the orders of logits up to / from a value that roundings have moved by less than 1e-6 of it; the edge of a class that is
+// wider than fp32 may have become infinite, which has no 1e-6.
+__device__ __forceinline__ u64 first_order(float x) {
+  x = fmaxf(x, -FLT_MAX);
+  return order_of(x + (fabsf(x) * 1e-6f + 1e-44f), 0);
+}
+__device__ __forceinline__ u64 last_order(float x) {
+  x = fminf(x, FLT_MAX);
+  return order_of(x - (fabsf(x) * 1e-6f + 1e-44f), -1);
+}
 // exp(-d), d >= 0: 2^-n times the Taylor series of 2^f, |f| <= 1/2, to the 12th power.  Against 60 digits off by up to 3e-16 of the
 // value below d = 1, and by 1.2e-16 d beyond, the rounding of y (1.1e-14 up to 100, 4.9e-14 up to 700); d itself has two roundings.
 __device__ __forceinline__ double weight(double d) {
