@@ -264,16 +264,19 @@ int spec_dense_gemm(float* y_dev, void* z_dev, const void* x_dev, const void* w_
  * scale per row and block of 128 columns (the last one may be short), stored block by block: scale[ceil(K/128)][M]; the value
  * of an element is e4m3 * scale.  Weights have one per block of 128 x 128: scale[ceil(N/128)][ceil(K/128)].  A scale is
  * (largest magnitude of the block) / 448; blocks below 2^-100 take 2^-100 / 448.  A NaN stays a NaN of its own, an infinite
- * value makes its block NaN.  K (d) is a multiple of 16, N of 16; both at most SPEC_FP8_K_MAX, rows of the first two calls
- * at most SPEC_FP8_ROW_MAX, and there M * ceil(d / 512) is below 2^26.  All are asynchronous on `stream`, allocate nothing and can be captured. */
+ * value makes its block NaN (behind a norm: see there).  K (d) is a multiple of 16, N of 16; both at most SPEC_FP8_K_MAX, rows of
+ * the first two calls at most SPEC_FP8_ROW_MAX, and there M * ceil(d / 512) is below 2^26.  All are asynchronous on `stream`,
+ * allocate nothing and can be captured. */
 enum { SPEC_F32 = 0, SPEC_BF16 = 1 };
 #define SPEC_FP8_ROW_MAX 32768
 #define SPEC_FP8_K_MAX 1048576
 
 /* Residual add, RMS norm and gain, rounded to e4m3: h[m] += delta[m] (delta may be NULL), in place and rounded to the type of
  * h; then y = h / sqrt(mean(h^2) + eps) * gain of what is stored, and its e4m3 values q[M][d] and scales.  h, delta: device,
- * SPEC_F32 or SPEC_BF16, row strides ldh, ldd >= d (elements; ldd also 0: one row for all); delta is h itself or shares no element with it; gain bf16 [d]; sums in fp32.  A
- * row's results do not depend on M.  q starts at a multiple of 8, the others at multiples of their elements. */
+ * SPEC_F32 or SPEC_BF16, row strides ldh, ldd >= d (elements; ldd also 0: one row for all); delta is h itself or shares no element
+ * with it; gain bf16 [d]; sums in fp32.  A row with a NaN becomes NaN; one with an infinite value, or whose squares add up beyond
+ * fp32, becomes 0 where it is finite and NaN where it is not.  A row's results do not depend on M.  q starts at a multiple of 8, the
+ * others at multiples of their elements. */
 int spec_add_norm_quant(void* h_dev, int h_type, long long ldh, const void* delta_dev, int delta_type, long long ldd,
                       const void* gain_dev, float eps, int M, int d, void* q_dev, float* scale_dev, void* stream);
 /* The e4m3 values q[M][K] and scales of rows as they are (ldx >= K, or 0): what a projection reads that no norm precedes. */
@@ -290,7 +293,10 @@ size_t spec_packed_quant_bytes(int N, int K);
 /* y = x W^T of e4m3 rows and packed e4m3 weights, any M >= 1; sums in fp32.  epilogue 0: out[M][N] of out_type, SPEC_F32 or
  * SPEC_BF16; 2: out[M][N/2], SPEC_BF16, = silu(gate) * up of interleaved panels (N % 32 == 0).  (There is no epilogue 1:
  * spec_add_norm_quant adds what follows to the residual stream.)  fp32 results are sums of exact products; from 33 rows on
- * bf16 ones come from 8-bit matrix instructions, which cost them 1.5e-5 before the rounding and take half the time.
+ * bf16 ones come from 8-bit matrix instructions, which take half the time and leave small terms out beside large ones: before the
+ * rounding 1.5e-5 of the result in the 2-norm for normal operands, more where some columns are far above the others, and never more
+ * than 2^-10 of the sum of a result's magnitudes.  Where large products cancel, that shows; fp32 results do not have it.  The
+ * scales of a row and a weight block are multiplied in fp32: products of them beyond its range give infinities and NaN.
  * x and the packed weights start at 16-byte addresses, out at one of 16 (SPEC_F32) or 8.  Up to 32 rows, a row's results do
  * not depend on M. */
 int spec_gemm_quant(void* out_dev, int out_type, const void* x_dev, const float* x_scale_dev, const void* w_packed_dev,
@@ -314,11 +320,14 @@ int spec_sample_row(const float* logits_dev, int vocab, float temperature, float
  *                              temperature and logit_scale, for the target to be truncated as the draft model is
  *   tok_out[n_rows]            the first id at which the sum of q passes u_dev[row] (below 0 and NaN as 0, from 1 on the last id)
  * each of them may be NULL, but not all; u_dev only matters for tok_out at a temperature.  q_out or masked_out may be the
- * logits (ld == vocab); any other overlap of the results and the workspace, with each other or with what is read, is refused.  A row without a finite logit, or with a NaN or +inf, has no distribution: NaN and token -1 (at
- * temperature 0 a NaN counts as none, and a row without any logit above -inf gives id 0).  Borders and draws are decided in 64
- * bits, the results do not depend on the order in which anything runs.  temperature >= 0, logit_scale > 0, both finite,
- * top_k >= 0, top_p and min_p in [0, 1], n_rows <= 65535, vocab <= SPEC_SAMPLE_VOCAB_MAX.  work_dev: 16-byte aligned device
- * memory of spec_sample_rows_workspace_bytes(n_rows, vocab), for this call alone until it has run; nothing in it need be set.
+ * logits (ld == vocab); any other overlap of the results and the workspace, with each other or with what is read, is refused.  A
+ * row without a finite logit, or with a NaN or +inf, has no distribution: NaN and token -1 (at temperature 0 a NaN counts as none,
+ * and a row without any logit above -inf gives id 0).  Borders and draws are decided in 64 bits, in sums to which an id adds a
+ * multiple of 2^-43 of the largest weight (of the row, in the last step of a draw that of 2048 to 8192 neighbours), so what is below
+ * 2^-44 of it is passed over even by a uniform of 0; the results do not depend on the order in which anything runs.
+ * temperature >= 0, logit_scale > 0, both finite, top_k >= 0, top_p and min_p in [0, 1], n_rows <= 65535, vocab <=
+ * SPEC_SAMPLE_VOCAB_MAX.  work_dev: 16-byte aligned device memory of spec_sample_rows_workspace_bytes(n_rows, vocab) (for a row up to
+ * 64 KiB and 4 KiB per 2048 ids, whatever the settings), for this call alone until it has run; nothing in it need be set.
  * Allocates nothing, can be captured; asynchronous on `stream`. */
 typedef struct {
   float temperature, logit_scale;
