@@ -1134,8 +1134,13 @@ static hipError_t launch_filter(FilterArgs a, int rows, hipStream_t st) {
   if (!a.greedy && a.top_k && a.top_k <= FL_FEW) {
     const int clear = a.q != a.logits && a.masked != a.logits;
     filter_groups_kernel<Q><<<grid, block, 0, st>>>(a, clear);
-    // 16 waves where a row has many groups to read: 64 rows of 128256 ids, top-k 1000, 25.3 -> 23.1 us; 32000 ids take 7.6 with 8
-    if (a.V > 65536) filter_few_kernel<16><<<rows, 1024, 0, st>>>(a, clear);
+    // 16 waves where many ids are compared digit by digit, or where the row is long: their barriers cost more than they share as long
+    // as few ids count, but take less than the whole row does that is read again and again if the k-th group lies far below (us,
+    // 8 | 16 waves):
+    //   32000 ids     k 300 16.2 | 16.9    500 19.1 | 18.2    1000 23.4 | 21.2    k 50 at temperature 0.1 188 | 136
+    //   128256        k 50  11.1 | 11.8    500 20.7 | 19.6    1000 25.8 | 23.4                            655 | 462
+    //   160000        k 50  12.8 | 12.0   (8 waves' registers hold the groups of 131072)
+    if (a.top_k > 384 || a.V > 65536) filter_few_kernel<16><<<rows, 1024, 0, st>>>(a, clear);
     else filter_few_kernel<8><<<rows, 512, 0, st>>>(a, clear);
     if (!clear) filter_finish_kernel<Q><<<grid, block, 0, st>>>(a, FINISH_WRITE);
     return hipGetLastError();

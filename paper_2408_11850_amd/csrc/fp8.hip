@@ -686,6 +686,10 @@ static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
 //   64 x 4096 x 4096       43 |  38 |  30 | 20.4 | 13.6     1023 x 12288 x 4096   66 |  61 |  74 |  79 | 108
 //   256 x 12288 x 4096     60 |  55 |  38 | 26.2 | 32.2     1023 x 8192 x 8192   107 | 101 |  79 |  91 | 139
 //   512 x 8192 x 8192     107 | 100 |  64 | 49.5 | 74.6     4095 x 8192 x 8192   248 | 292 | 293 | 346 | 501
+// and of few blocks, where the fixed part counts:
+//   288 x 1024 x 128     10.2 | 8.4 | 6.7 |  4.7 |  3.1     898 x 4448 x 304    13.5 | 11.4 |  9.6 | 10.2 | 10.7
+//   377 x 19616 x 416    16.7 | 14.4 | 12.2 | 14.1 | 17.9   2339 x 26896 x 384  58.9 | 63.9 | 63.0 | 76.1 | 96.0
+// Off by more: 519 x 32448 x 22352 takes 256 x 192, 605, where 128 x 256 takes 547.
 // 256 x 256 runs at 2.3 to 2.4 PFLOP/s (zeros instead of data: 3.0, so the chip's power is a part of what bounds it); 4 vector instructions
 // per MFMA scale and add, and every block passes LDS once per wave that uses it.
 int fp8_tile(int M, int NT, int KB, bool exact) {
