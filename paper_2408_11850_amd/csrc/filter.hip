@@ -22,9 +22,12 @@
 // `finish` writes the distribution or the truncated logits and draws inside the chunk that the draw falls into.
 //
 // Few rows are bound by launches that depend on each other, many by the row's one workgroup (kernels alone, us):
-//   1 row of 32000, a top-k that goes by groups     groups 2.8, few 7.8
-//   64 rows of 128256, top-k 1000                   groups 10.3 (66 MB read and written), few 23.3
-//   8 rows of 128256, by classes                    bins 5.2, collect 8.6, resolve 2.7, finish 7.2
+//   1 row of 32000, a top-k that goes by groups     groups 2.9, few 7.9
+//   64 rows of 128256, top-k 1000                   groups 10.9 (66 MB read and written), few 22.8
+//   8 rows of 128256, by classes                    bins 5.2, collect 8.1, resolve 3.0, finish 7.1
+// Classes end 31.9 below the largest z.  Where fewer than k groups (ids) lie that near, or a border's class has more ids than a list
+// holds, the row's one workgroup reads the row again in every pass (whole calls): 32000 ids, top-k 50, temperature 0.1 138 (0.25 and
+// up: 10), 128256 ids 324; one level of 128256 ids, or 640 above -inf and top-k 1000, 1650.
 #include <float.h>
 
 #include "spec_internal.h"
@@ -1135,8 +1138,8 @@ static hipError_t launch_filter(FilterArgs a, int rows, hipStream_t st) {
     const int clear = a.q != a.logits && a.masked != a.logits;
     filter_groups_kernel<Q><<<grid, block, 0, st>>>(a, clear);
     // 16 waves where many ids are compared digit by digit, or where the row is long: their barriers cost more than they share as long
-    // as few ids count, but take less than the whole row does that is read again and again if the k-th group lies far below (us,
-    // 8 | 16 waves):
+    // as few ids count, but take less than the whole row does that is read again and again if the k-th group lies far below (us
+    // with top-p 0.9375, 8 | 16 waves):
     //   32000 ids     k 300 16.2 | 16.9    500 19.1 | 18.2    1000 23.4 | 21.2    k 50 at temperature 0.1 188 | 136
     //   128256        k 50  11.1 | 11.8    500 20.7 | 19.6    1000 25.8 | 23.4                            655 | 462
     //   160000        k 50  12.8 | 12.0   (8 waves' registers hold the groups of 131072)

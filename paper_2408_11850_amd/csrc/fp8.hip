@@ -116,7 +116,7 @@ __device__ __forceinline__ uint2 to_e4m3(const float (&v)[8], float scale) {
 // A row belongs to `wpr` waves of a workgroup; a chunk is the 512 columns a wave takes at a time, at most G per wave.  The sum of
 // squares is formed per chunk and over the chunks in ascending order, so a row's bits do not depend on how it is dealt out.
 // Everything stays in registers between one read and one write, so HBM bounds it: 4096 x 8192 bf16 and a bf16 delta, 236 MB, 47 us
-// (5.0 TB/s, as a copy), 1023 x 4096 fp32 11.3 us; one row of 8192 takes 3.5, of which the launch is most.
+// (5.0 TB/s, as a copy), 1023 x 4096 fp32 11.1 us; one row of 8192 takes 3.6, of which the launch is most.
 #define ROWS_CHUNK 512
 #define ROWS_WAVES_MAX 16
 template <int XT, int DT, bool NORM, int G>
@@ -689,7 +689,8 @@ static hipError_t launch_skinny(const Fp8Args& a, hipStream_t st) {
 // and of few blocks, where the fixed part counts:
 //   288 x 1024 x 128     10.2 | 8.4 | 6.7 |  4.7 |  3.1     898 x 4448 x 304    13.5 | 11.4 |  9.6 | 10.2 | 10.7
 //   377 x 19616 x 416    16.7 | 14.4 | 12.2 | 14.1 | 17.9   2339 x 26896 x 384  58.9 | 63.9 | 63.0 | 76.1 | 96.0
-// Off by more: 519 x 32448 x 22352 takes 256 x 192, 605, where 128 x 256 takes 547.
+// Off by more: 519 x 32448 x 22352 takes 256 x 192, 605, where 128 x 256 takes 547; 151 x 19200 x 512 128 x 256, 11.1, where 64 x 64
+// takes 9.6.
 // 256 x 256 runs at 2.3 to 2.4 PFLOP/s (zeros instead of data: 3.0, so the chip's power is a part of what bounds it); 4 vector instructions
 // per MFMA scale and add, and every block passes LDS once per wave that uses it.
 int fp8_tile(int M, int NT, int KB, bool exact) {
