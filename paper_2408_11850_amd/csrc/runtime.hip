@@ -1,6 +1,7 @@
 // Host runtime of the speculative-decoding library: contexts, the paged KV allocator, the
 // forward pass as a chain of kernel launches, the draft-token ring with its q-row cache, the
 // accept step's bookkeeping and the three decoding loops (paper Section 2 and Algorithms 1, 2).
+#include <algorithm>
 #include <chrono>
 #include <cstdarg>
 #include <cstdio>
@@ -1563,11 +1564,11 @@ extern "C" int spec_sample_rows(const float* logits, long long ld, int n_rows, i
   if ((q_out == logits || masked_out == logits) && ld != vocab) FAIL(SPEC_E_INVAL, "results in place need ld == vocab");
   if (off_by(logits, 4) || off_by(u, 4) || off_by(q_out, 4) || off_by(masked_out, 4) || off_by(tok_out, 4) || off_by(work, 16))
     FAIL(SPEC_E_INVAL, "misaligned operand");
-  const size_t row = (size_t)vocab * 4, n = n_rows;
+  const size_t row = (size_t)vocab * 4, n = n_rows, apart = (size_t)std::min(ld, 1ll << 56) * 4;       // beyond any address, and fits
   const struct { const void* p; size_t bytes; } to[4] = {{q_out, q_out ? n * row : 0}, {masked_out, masked_out ? n * row : 0},
                                                          {tok_out, tok_out ? n * 4 : 0}, {work, filter_work_bytes(n_rows, vocab)}};
   for (int i = 0; i < 4; ++i) {
-    bool clash = to[i].p != logits && meets_rows(logits, (size_t)ld * 4, n, row, to[i].p, to[i].bytes);
+    bool clash = to[i].p != logits && meets_rows(logits, apart, n, row, to[i].p, to[i].bytes);
     clash |= i >= 2 && to[i].p == logits && to[i].bytes;
     clash |= tok_out && s->temperature > 0.0f && meet(u, n * 4, to[i].p, to[i].bytes);
     for (int j = 0; j < i; ++j) clash |= meet(to[j].p, to[j].bytes, to[i].p, to[i].bytes);

@@ -76,3 +76,12 @@ def test_neighbours_and_gaps(amd):
     with pytest.raises(amd.SpecError):
         amd.filter_rows(own[:N * V].view(N, V), out=own[7:].view(N, V))
     assert torch.equal(own[:N * V].view(N, V), x)
+
+
+@pytest.mark.parametrize("ld", [1 << 40, 1 << 61, 1 << 62, (1 << 63) - 1])
+def test_far_rows(amd, ld):
+    """Strides whose bytes do not fit 64 bits: the first row is looked at all the same."""
+    lib = amd.load_library()
+    for change in (dict(q=AT["logits"] + ROW - 4), dict(work=AT["logits"]), dict(masked=AT["logits"] - 4)):
+        assert _call(lib, amd, {**AT, **change, "ld": ld}) == amd.SPEC_E_INVAL
+        assert b"overlap" in lib.spec_last_error()
