@@ -302,6 +302,68 @@ size_t spec_packed_quant_bytes(int N, int K);
 int spec_gemm_quant(void* out_dev, int out_type, const void* x_dev, const float* x_scale_dev, const void* w_packed_dev,
                     const float* w_scale_dev, int M, int N, int K, int epilogue, void* stream);
 
+/* ---- attention over a paged 8-bit cache ------------------------------------------------------
+ * Keys and values of n_seqs sequences in e4m3, in pages of 64 entries that a table deals out, with a scale for the keys and one for
+ * the values of every page and head.  A scale is a power of two, 2^e with -100 <= e <= 112: the least for which the largest
+ * magnitude of the page and head is at most 448 * 2^e.  While a page fills it only grows, and the codes that are there move to it
+ * (exact, but for codes that become denormal).  len[s] counts the entries of sequence s; the rows of a call are its LAST entries,
+ * so lengths are raised before spec_append_quant and stay for the calls that read what it stored.
+ * Rows of all sequences stand one behind the other: those of sequence s are row_start[s] .. row_start[s + 1] - 1 (device, n_seqs + 1
+ * rising numbers; NULL: n_rows / n_seqs each).  Rows behind the last sequence stay as they are.  Row j of M stands for entry len - M + j
+ * and sees the entries up to it; with a window > 0 only the last `window` of them and the first `sinks` entries.
+ * All numbers on the device are looked at there: a sequence whose length is beyond its table (64 * max_pages) stores nothing and its
+ * rows become NaN; so do rows that see an entry of a page id that is none of 0 .. n_pages - 1 (pages that no row sees, as behind a
+ * window, may have any id); rows in front of entry 0 see nothing: 0, and -inf as the logarithm of their sum.
+ * n_heads query heads share n_kv_heads evenly; head_dim is 64 or 128; n_rows * n_heads <= 2^26, n_seqs <= 65535,
+ * n_seqs * n_kv_heads <= 2^20.  Every call is asynchronous on `stream`, allocates nothing and can be captured; its results do not
+ * depend on the order in which anything runs.  What a call writes must not overlap what it reads. */
+#define SPEC_CACHE_HEADS_MAX 4096
+#define SPEC_CACHE_PAGES_MAX (1 << 24)
+typedef struct {
+  void* k;              /* e4m3 [n_pages][n_kv_heads][64][head_dim], 16-byte aligned */
+  void* v;              /* e4m3 [n_pages][n_kv_heads][head_dim][64]: entries of an element are neighbours */
+  float* scale;         /* [n_pages][n_kv_heads][2]: of the keys, of the values; 8-byte aligned */
+  const int32_t* table; /* [n_seqs][table_ld]: page of entries 64 i .. 64 i + 63 of a sequence */
+  int32_t* len;         /* [n_seqs] */
+  int n_pages, n_kv_heads, head_dim, n_seqs;
+  int max_pages;        /* columns of the table in use */
+  int table_ld;         /* its row stride */
+} spec_quant_cache;
+
+/* Store rows as the last entries of their sequences: k, v [n_rows][n_kv_heads][head_dim] of `type` (SPEC_F32 or SPEC_BF16; row
+ * strides ldk, ldv in elements, or 0: one row for all).  With theta > 0 k and q are rotated first: pairs (i, i + head_dim / 2) by position *
+ * theta^(-2 i / head_dim), the position being position[s] + j (device), or the entry's number where `position` is NULL.  q
+ * [n_rows][n_heads][head_dim] of the same type (NULL: none) goes, rotated, to q_out (bf16, contiguous; may be q itself).
+ * A token with a NaN, an infinite value or one from 2^120 on in a head's key or value gets a NaN key and the value 0 there: rows
+ * that see it become NaN, others do not.  The pages that new entries fall into belong to one sequence each. */
+int spec_append_quant(const spec_quant_cache* cache, const void* k_dev, long long ldk, const void* v_dev, long long ldv, int type,
+                      const int32_t* row_start_dev, int n_rows, const void* q_dev, long long ldq, int n_heads, float theta,
+                      const int32_t* position_dev, void* q_out_dev, void* stream);
+/* out[n_rows][n_heads][head_dim] (bf16) = softmax(scale * q k) v over the entries that a row sees; q bf16, rows ldq elements apart
+ * (a multiple of 8, rows at 16-byte addresses; 0: one row for all).  lse[n_rows][n_heads] (NULL: not wanted): natural logarithm of the sum of
+ * exp(scale * q k).  Sums and statistics in fp32, weights rounded to bf16 for the product with the values.
+ * work_dev: 16-byte aligned device memory of spec_attend_quant_workspace_bytes (the same arguments; 0: NULL will do), for this call alone
+ * until it has run. */
+int spec_attend_quant(const spec_quant_cache* cache, const void* q_dev, long long ldq, const int32_t* row_start_dev, int n_rows,
+                      int n_heads, float scale, int window, int sinks, void* out_dev, float* lse_dev, void* work_dev, void* stream);
+size_t spec_attend_quant_workspace_bytes(const spec_quant_cache* cache, const int32_t* row_start_dev, int n_rows, int n_heads,
+                                         int window, int sinks);
+/* The attention weight that entries get from the rows of a call: weight[s][h][entry] += sum over the rows that see it and the
+ * query heads of KV head h of exp(scale * q k - lse), q, scale, window, sinks and lse as in (and from) spec_attend_quant.  Entries of the
+ * rows themselves start from 0, so nothing has to be cleared; what lies behind the last entry stays as it is.  weight: fp32
+ * [n_seqs][n_kv_heads][ldw], ldw >= 64 * max_pages. */
+int spec_weigh_quant(const spec_quant_cache* cache, const void* q_dev, long long ldq, const float* lse_dev, const int32_t* row_start_dev,
+                     int n_rows, int n_heads, float scale, int window, int sinks, float* weight_dev, long long ldw, void* stream);
+/* Keep `budget` entries of every sequence and head: the first `sinks`, the last `recent`, and between them those of the largest
+ * weight (of equal ones the first; NaN counts as the least), in their order; all where there are no more than budget.  They go to the pages of `to`
+ * (same heads and sequences, its own table; it may share the pools, but no page of its table may be one that `cache` still reads), with
+ * scales of their own; to->len is set, to_weight[n_seqs][n_kv_heads][ldt >= budget] gets their weights and kept[n_seqs][n_kv_heads][budget]
+ * their numbers, -1 behind the last.  Heads keep different entries, so only the last `recent` ones stand for the same tokens in all of them.
+ * Entries of a page that is none get NaN keys; a sequence whose length is beyond its table keeps nothing and its new length is
+ * beyond any table. */
+int spec_evict_quant(const spec_quant_cache* cache, const float* weight_dev, long long ldw, const spec_quant_cache* to, int budget,
+                     int sinks, int recent, int32_t* kept_dev, float* to_weight_dev, long long ldt, void* stream);
+
 /* Streaming-read probe: sums `bytes` bytes of device memory with 16-byte loads; used to
  * measure the achievable HBM read ceiling next to the nominal peak.  out_dev: 4 bytes. */
 int spec_read_probe(const void* src_dev, size_t bytes, void* out_dev, void* stream);

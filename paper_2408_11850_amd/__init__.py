@@ -57,6 +57,12 @@ class Sampling(C.Structure):
                 ("min_p", C.c_float)]
 
 
+class QuantCacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("scale", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p),
+                ("n_pages", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("n_seqs", C.c_int),
+                ("max_pages", C.c_int), ("table_ld", C.c_int)]
+
+
 # name -> (restype, argtypes); every symbol include/spec.h declares
 _P = C.c_void_p
 _PI = C.POINTER(C.c_int)
@@ -99,6 +105,12 @@ SIGNATURES = {
     "spec_pack_quant": (C.c_int, [_P, _P, _P, _P, C.c_int, C.c_int, C.c_int, C.c_int, _P]),
     "spec_packed_quant_bytes": (C.c_size_t, [C.c_int, C.c_int]),
     "spec_gemm_quant": (C.c_int, [_P, C.c_int, _P, _P, _P, _P, C.c_int, C.c_int, C.c_int, C.c_int, _P]),
+    "spec_append_quant": (C.c_int, [_P, _P, C.c_longlong, _P, C.c_longlong, C.c_int, _P, C.c_int, _P, C.c_longlong, C.c_int, C.c_float,
+                                    _P, _P, _P]),
+    "spec_attend_quant": (C.c_int, [_P, _P, C.c_longlong, _P, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, _P, _P, _P, _P]),
+    "spec_attend_quant_workspace_bytes": (C.c_size_t, [_P, _P, C.c_int, C.c_int, C.c_int, C.c_int]),
+    "spec_weigh_quant": (C.c_int, [_P, _P, C.c_longlong, _P, _P, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, _P, C.c_longlong, _P]),
+    "spec_evict_quant": (C.c_int, [_P, _P, C.c_longlong, _P, C.c_int, C.c_int, C.c_int, _P, _P, C.c_longlong, _P]),
     "spec_read_probe": (C.c_int, [_P, C.c_size_t, _P, _P]),
     "spec_sample_row": (C.c_int, [_P, C.c_int, C.c_float, C.c_float, C.c_float, _P, _P, _P]),
     "spec_sample_rows": (C.c_int, [_P, C.c_longlong, C.c_int, C.c_int, C.POINTER(Sampling), _P, _P, _P, _P, _P, _P]),
@@ -147,3 +159,4 @@ def check(rc: int) -> int:
 from .binding import SpecContext, pack_model, gemm, dense_gemm, sample_row, accept_rows, accept_rows_static, read_probe  # noqa: E402,F401
 from .draws import filter_rows, sample_rows  # noqa: E402,F401
 from .fp8 import Fp8Weight, add_norm_fp8, gemm_fp8, pack_weights_fp8, quant_fp8, quant_weight_fp8  # noqa: E402,F401
+from .cache import Fp8Cache, append_fp8, attend_fp8, evict_fp8, weigh_fp8  # noqa: E402,F401

@@ -1514,6 +1514,194 @@ extern "C" int spec_gemm_quant(void* out, int out_type, const void* x, const flo
   return SPEC_OK;
 }
 
+// ---- attention over a paged 8-bit cache
+static bool meet(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return na && nb && (x < y ? y - x < na : x - y < nb);
+}
+// whether any of n rows of `width` bytes, ld bytes apart, meets p
+static bool meets_rows(const void* rows, size_t ld, size_t n, size_t width, const void* p, size_t bytes) {
+  const uintptr_t x = (uintptr_t)rows, y = (uintptr_t)p;
+  if (!bytes || y < x) return bytes && x - y < bytes;
+  const size_t at = y - x, first = at < width ? 0 : (at - width) / ld + 1;      // the first row that ends behind p's first byte
+  return first < n && first <= (at + bytes - 1) / ld;
+}
+struct Region {
+  const void* p;
+  size_t bytes;
+};
+// whether any of n rows of `row` elements, ld elements apart (0: the same one), meets p
+static bool meets_strided(const void* rows, long long ld, long long row, size_t element, size_t n, const void* p, size_t bytes) {
+  const size_t apart = (size_t)std::min(ld ? ld : row, 1ll << 56) * element;    // beyond any address, and fits
+  return meets_rows(rows, apart, ld ? n : 1, row * element, p, bytes);
+}
+
+static int check_quant_cache(const spec_quant_cache* c, QuantCache* o) {
+  if (!c || !c->k || !c->v || !c->scale || !c->table || !c->len) FAIL(SPEC_E_INVAL, "null pointer");
+  if (c->head_dim != 64 && c->head_dim != 128) FAIL(SPEC_E_INVAL, "head_dim must be 64 or 128");
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > SPEC_CACHE_HEADS_MAX || c->n_seqs < 1 || c->n_seqs > 65535 ||
+      (size_t)c->n_seqs * c->n_kv_heads > (1u << 20))
+    FAIL(SPEC_E_INVAL, "need pages, 1 to %d heads, 1 to 65535 sequences and at most 2^20 of their heads", SPEC_CACHE_HEADS_MAX);
+  if (c->max_pages < 1 || c->max_pages > SPEC_CACHE_PAGES_MAX || c->table_ld < c->max_pages)
+    FAIL(SPEC_E_INVAL, "need 1 to %d pages a sequence and a table at least as wide", SPEC_CACHE_PAGES_MAX);
+  if (off_by(c->k, 16) || off_by(c->v, 16) || off_by(c->scale, 8) || off_by(c->table, 4) || off_by(c->len, 4))
+    FAIL(SPEC_E_INVAL, "misaligned cache");
+  *o = {(uint8_t*)c->k, (uint8_t*)c->v, c->scale, c->table, c->len, c->n_pages, c->n_kv_heads, c->head_dim, c->n_seqs, c->max_pages, c->table_ld};
+  return SPEC_OK;
+}
+static int check_cache_rows(const QuantCache& c, const int32_t* row_start, int n_rows, int n_heads) {
+  if (n_heads < 1 || n_heads > SPEC_CACHE_HEADS_MAX || n_heads % c.n_kv_heads)
+    FAIL(SPEC_E_INVAL, "query heads must be a multiple of the cache's, at most %d", SPEC_CACHE_HEADS_MAX);
+  if (n_rows < 1 || (size_t)n_rows * n_heads > (1u << 26)) FAIL(SPEC_E_INVAL, "need 1 <= n_rows and at most 2^26 rows of heads");
+  if (!row_start && n_rows % c.n_seqs) FAIL(SPEC_E_INVAL, "without row_start every sequence has as many rows");
+  if (off_by(row_start, 4)) FAIL(SPEC_E_INVAL, "misaligned row_start");
+  return SPEC_OK;
+}
+// q of attention: 16-byte loads; a window that hides nothing is none
+static int check_cache_q(const QuantCache& c, const void* q, long long ldq, int n_heads, float scale, int* window, int* sinks) {
+  if (!q) FAIL(SPEC_E_INVAL, "null pointer");
+  if ((ldq && ldq < (long long)n_heads * c.head_dim) || ldq % 8 || off_by(q, 16))
+    FAIL(SPEC_E_INVAL, "rows of q start at multiples of 16 bytes and do not overlap");
+  if (!(scale > 0.0f) || scale == INFINITY) FAIL(SPEC_E_INVAL, "scale must be positive and finite");
+  if (*window < 0 || *sinks < 0) FAIL(SPEC_E_INVAL, "window and sinks must not be negative");
+  if (*window >= c.max_pages * SPEC_PAGE_TOKENS) *window = 0;
+  *sinks = *window ? std::min(*sinks, c.max_pages * SPEC_PAGE_TOKENS) : 0;
+  return SPEC_OK;
+}
+static void cache_regions(const QuantCache& c, Region (&r)[5]) {
+  const size_t blocks = (size_t)c.n_pages * c.n_kv_heads, pool = blocks * SPEC_PAGE_TOKENS * c.head_dim;
+  r[0] = {c.k, pool}, r[1] = {c.v, pool}, r[2] = {c.scale, blocks * 8};
+  r[3] = {c.table, ((size_t)(c.n_seqs - 1) * c.table_ld + c.max_pages) * 4}, r[4] = {c.len, (size_t)c.n_seqs * 4};
+}
+static bool meets_cache(const QuantCache& c, const void* p, size_t bytes) {
+  Region r[5];
+  cache_regions(c, r);
+  for (const Region& x : r)
+    if (meet(x.p, x.bytes, p, bytes)) return true;
+  return false;
+}
+extern "C" int spec_append_quant(const spec_quant_cache* cache, const void* k, long long ldk, const void* v, long long ldv, int type,
+                                 const int32_t* row_start, int n_rows, const void* q, long long ldq, int n_heads, float theta,
+                                 const int32_t* position, void* q_out, void* stream) {
+  QuantCache c;
+  int rc = check_quant_cache(cache, &c);
+  if (rc) return rc;
+  if (!k || !v || !q != !q_out) FAIL(SPEC_E_INVAL, "null pointer");
+  if (!fp8_type(type)) FAIL(SPEC_E_INVAL, "types are SPEC_F32 and SPEC_BF16");
+  if (!q) n_heads = c.n_kv_heads;
+  rc = check_cache_rows(c, row_start, n_rows, n_heads);
+  if (rc) return rc;
+  const long long wide = (long long)c.n_kv_heads * c.head_dim, wide_q = (long long)n_heads * c.head_dim;
+  if ((ldk && ldk < wide) || (ldv && ldv < wide) || (q && ldq && ldq < wide_q)) FAIL(SPEC_E_INVAL, "row stride below the row");
+  if (theta != 0.0f && (!(theta >= 1.0f) || theta == INFINITY)) FAIL(SPEC_E_INVAL, "theta must be 0 (no rotation) or finite and at least 1");
+  if (off_element(k, type) || off_element(v, type) || (q && off_element(q, type)) || off_by(q_out, 16) || off_by(position, 4))
+    FAIL(SPEC_E_INVAL, "misaligned operand");
+  const size_t el = type == SPEC_F32 ? 4 : 2, n = n_rows, out = q ? n * wide_q * 2 : 0;
+  Region pools[5];
+  cache_regions(c, pools);
+  bool clash = meets_cache(c, q_out, out) || meet(row_start, row_start ? (size_t)(c.n_seqs + 1) * 4 : 0, q_out, out) ||
+               meet(position, position ? (size_t)c.n_seqs * 4 : 0, q_out, out);
+  const struct { const void* p; long long ld, row; } in[3] = {{k, ldk, wide}, {v, ldv, wide}, {q, ldq, wide_q}};
+  for (int i = 0; i < (q ? 3 : 2); ++i) {
+    auto meets = [&](const void* p, size_t bytes) { return meets_strided(in[i].p, in[i].ld, in[i].row, el, n, p, bytes); };
+    if (!(i == 2 && q == q_out && type == SPEC_BF16 && ldq == wide_q)) clash |= meets(q_out, out);
+    for (int j = 0; j < 3; ++j) clash |= meets(pools[j].p, pools[j].bytes);
+  }
+  if (clash) FAIL(SPEC_E_INVAL, "results must not overlap each other or what is read");
+  AppendArgs a = {row_start, position, n_rows, n_heads, k, v, q, (size_t)ldk, (size_t)ldv, (size_t)ldq, (bf16*)q_out, theta,
+                  theta > 0.0f ? std::log2((double)theta) : 0.0};
+  HIPCHK(launch_append_quant(c, a, type, (hipStream_t)stream));
+  return SPEC_OK;
+}
+extern "C" size_t spec_attend_quant_workspace_bytes(const spec_quant_cache* cache, const int32_t* row_start, int n_rows, int n_heads,
+                                                    int window, int sinks) {
+  QuantCache c;
+  if (check_quant_cache(cache, &c) || check_cache_rows(c, row_start, n_rows, n_heads) || window < 0 || sinks < 0) return 0;
+  (void)check_cache_q(c, c.k, (long long)n_heads * c.head_dim, n_heads, 1.0f, &window, &sinks);
+  return attend_quant_work_bytes(c, row_start != nullptr, n_rows, n_heads, window, sinks);
+}
+extern "C" int spec_attend_quant(const spec_quant_cache* cache, const void* q, long long ldq, const int32_t* row_start, int n_rows,
+                                 int n_heads, float scale, int window, int sinks, void* out, float* lse, void* work, void* stream) {
+  QuantCache c;
+  int rc = check_quant_cache(cache, &c);
+  if (rc) return rc;
+  rc = check_cache_rows(c, row_start, n_rows, n_heads);
+  if (rc) return rc;
+  rc = check_cache_q(c, q, ldq, n_heads, scale, &window, &sinks);
+  if (rc) return rc;
+  if (!out) FAIL(SPEC_E_INVAL, "null pointer");
+  if (off_by(out, 16) || off_by(lse, 4) || off_by(work, 16)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  const size_t need = attend_quant_work_bytes(c, row_start != nullptr, n_rows, n_heads, window, sinks), n = n_rows;
+  if (need && !work) FAIL(SPEC_E_INVAL, "these rows need a workspace");
+  const Region to[3] = {{out, n * n_heads * c.head_dim * 2}, {lse, lse ? n * n_heads * 4 : 0}, {work, need}};
+  for (int i = 0; i < 3; ++i) {
+    bool clash = meets_cache(c, to[i].p, to[i].bytes) || meet(row_start, row_start ? (size_t)(c.n_seqs + 1) * 4 : 0, to[i].p, to[i].bytes) ||
+                 meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, to[i].p, to[i].bytes);
+    for (int j = 0; j < i; ++j) clash |= meet(to[j].p, to[j].bytes, to[i].p, to[i].bytes);
+    if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
+  }
+  AttendArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, (bf16*)out, lse,
+                  0, 0, 0, nullptr, nullptr};
+  HIPCHK(launch_attend_quant(c, a, work, (hipStream_t)stream));
+  return SPEC_OK;
+}
+extern "C" int spec_weigh_quant(const spec_quant_cache* cache, const void* q, long long ldq, const float* lse, const int32_t* row_start,
+                                int n_rows, int n_heads, float scale, int window, int sinks, float* weight, long long ldw, void* stream) {
+  QuantCache c;
+  int rc = check_quant_cache(cache, &c);
+  if (rc) return rc;
+  rc = check_cache_rows(c, row_start, n_rows, n_heads);
+  if (rc) return rc;
+  rc = check_cache_q(c, q, ldq, n_heads, scale, &window, &sinks);
+  if (rc) return rc;
+  if (!lse || !weight) FAIL(SPEC_E_INVAL, "null pointer");
+  if (off_by(lse, 4) || off_by(weight, 4)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  if (ldw < (long long)c.max_pages * SPEC_PAGE_TOKENS || ldw > 1ll << 40) FAIL(SPEC_E_INVAL, "a row of weights holds every entry of a sequence");
+  const size_t n = n_rows, bytes = (size_t)c.n_seqs * c.n_kv_heads * (size_t)ldw * 4;
+  if (meets_cache(c, weight, bytes) || meet(row_start, row_start ? (size_t)(c.n_seqs + 1) * 4 : 0, weight, bytes) ||
+      meet(lse, n * n_heads * 4, weight, bytes) || meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, weight, bytes))
+    FAIL(SPEC_E_INVAL, "results must not overlap what is read");
+  WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, lse, weight, (size_t)ldw, 0};
+  HIPCHK(launch_weigh_quant(c, a, (hipStream_t)stream));
+  return SPEC_OK;
+}
+extern "C" int spec_evict_quant(const spec_quant_cache* cache, const float* weight, long long ldw, const spec_quant_cache* to, int budget,
+                                int sinks, int recent, int32_t* kept, float* to_weight, long long ldt, void* stream) {
+  QuantCache c, o;
+  int rc = check_quant_cache(cache, &c);
+  if (rc) return rc;
+  rc = check_quant_cache(to, &o);
+  if (rc) return rc;
+  if (!weight || !kept || !to_weight) FAIL(SPEC_E_INVAL, "null pointer");
+  if (c.n_kv_heads != o.n_kv_heads || c.head_dim != o.head_dim || c.n_seqs != o.n_seqs) FAIL(SPEC_E_INVAL, "two caches of other heads or sequences");
+  if (budget < 1 || budget > o.max_pages * SPEC_PAGE_TOKENS) FAIL(SPEC_E_INVAL, "budget must be at least 1 and fit the new table");
+  if (sinks < 0 || recent < 0 || (long long)sinks + recent > budget) FAIL(SPEC_E_INVAL, "need 0 <= sinks, 0 <= recent and their sum at most budget");
+  if (off_by(weight, 4) || off_by(kept, 4) || off_by(to_weight, 4)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  const size_t heads = (size_t)c.n_seqs * c.n_kv_heads;
+  if (ldw < (long long)c.max_pages * SPEC_PAGE_TOKENS || ldw > 1ll << 40 || ldt < budget || ldt > 1ll << 40)
+    FAIL(SPEC_E_INVAL, "a row of weights holds every entry of a sequence");
+  Region in[5], out[5];
+  cache_regions(c, in);
+  cache_regions(o, out);
+  // the pages may be of one pool; tables, lengths and weights are not
+  const Region w[3] = {{weight, heads * (size_t)ldw * 4}, in[3], in[4]}, r[4] = {{kept, heads * budget * 4}, {to_weight, heads * (size_t)ldt * 4}, out[4], out[3]};
+  bool clash = false;
+  for (int i = 0; i < 4; ++i) {
+    for (const Region& x : w) clash |= i < 3 && meet(r[i].p, r[i].bytes, x.p, x.bytes);
+    for (int j = 0; j < i; ++j) clash |= meet(r[i].p, r[i].bytes, r[j].p, r[j].bytes);
+    for (int j = 0; j < 3; ++j) clash |= meet(r[i].p, r[i].bytes, in[j].p, in[j].bytes) || meet(r[i].p, r[i].bytes, out[j].p, out[j].bytes);
+  }
+  for (int j = 0; j < 3; ++j) {
+    for (const Region& x : w) clash |= meet(out[j].p, out[j].bytes, x.p, x.bytes);
+    const bool same = out[j].p == in[j].p;
+    for (int i = 0; i < 3; ++i) clash |= !(same && i == j) && meet(out[j].p, out[j].bytes, in[i].p, in[i].bytes);
+  }
+  if (clash) FAIL(SPEC_E_INVAL, "results must not overlap each other or what is read");
+  EvictArgs a = {weight, (size_t)ldw, budget, sinks, recent, to->len, to_weight, (size_t)ldt, kept};
+  HIPCHK(launch_evict_quant(c, o, a, (hipStream_t)stream));
+  return SPEC_OK;
+}
+
 extern "C" int spec_read_probe(const void* src, size_t bytes, void* out, void* stream) {
   if (!src || !out || bytes < 16) FAIL(SPEC_E_INVAL, "bad argument");
   HIPCHK(launch_read_probe(src, bytes, out, (hipStream_t)stream));
@@ -1534,17 +1722,6 @@ static int check_sample_rows(int n_rows, int vocab) {
   if (n_rows < 1 || n_rows > 65535 || vocab < 1 || vocab > SPEC_SAMPLE_VOCAB_MAX)
     FAIL(SPEC_E_INVAL, "need 1 to 65535 rows of 1 to %d ids", SPEC_SAMPLE_VOCAB_MAX);
   return SPEC_OK;
-}
-static bool meet(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return na && nb && (x < y ? y - x < na : x - y < nb);
-}
-// whether any of n rows of `width` bytes, ld bytes apart, meets p
-static bool meets_rows(const void* rows, size_t ld, size_t n, size_t width, const void* p, size_t bytes) {
-  const uintptr_t x = (uintptr_t)rows, y = (uintptr_t)p;
-  if (!bytes || y < x) return bytes && x - y < bytes;
-  const size_t at = y - x, first = at < width ? 0 : (at - width) / ld + 1;      // the first row that ends behind p's first byte
-  return first < n && first <= (at + bytes - 1) / ld;
 }
 extern "C" size_t spec_sample_rows_workspace_bytes(int n_rows, int vocab) {
   return check_sample_rows(n_rows, vocab) ? 0 : filter_work_bytes(n_rows, vocab);

@@ -206,6 +206,62 @@ hipError_t launch_gemm_fp8(const uint8_t* x, const float* xs, const void* w, con
 // 1 = 256 x 192 (both bf16 only), 2 = 128 x 256, 3 = 128 x 128, 4 = 64 x 64
 int fp8_tile(int M, int NT, int KB, bool exact);
 
+// attention over a paged 8-bit cache (cache.hip); members as in spec.h's spec_quant_cache
+struct QuantCache {
+  uint8_t *k, *v;
+  float* scale;
+  const int *table, *len;
+  int n_pages, n_kv_heads, head_dim, n_seqs, max_pages, table_ld;
+};
+struct AppendArgs {
+  const int *rows, *position;
+  int n_rows, n_heads;
+  const void *k, *v, *q;      // q may be null
+  size_t ldk, ldv, ldq;
+  bf16* q_out;
+  float theta;                // 0: nothing is rotated
+  double log2_theta;
+};
+struct AttendArgs {
+  const int* rows;
+  int n_rows, n_heads;
+  const bf16* q;
+  size_t ldq;
+  float scale_log2e;
+  int window, sinks;
+  bf16* out;
+  float* lse;                 // may be null
+  int G, splits, row_waves;   // set by the launch ...
+  float* part;                // ... parts [splits][n_rows][n_heads][head_dim] and their maxima and sums
+  float2* part_ml;
+};
+struct WeighArgs {
+  const int* rows;
+  int n_rows, n_heads;
+  const bf16* q;
+  size_t ldq;
+  float scale_log2e;
+  int window, sinks;
+  const float* lse;
+  float* weight;
+  size_t ldw;
+  int G;                      // set by the launch
+};
+struct EvictArgs {
+  const float* weight;
+  size_t ldw;
+  int budget, sinks, recent;
+  int* to_len;
+  float* to_weight;
+  size_t ldt;
+  int* kept;
+};
+hipError_t launch_append_quant(const QuantCache& c, const AppendArgs& a, int type, hipStream_t st);
+size_t attend_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks);
+hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hipStream_t st);
+hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, hipStream_t st);
+hipError_t launch_evict_quant(const QuantCache& c, const QuantCache& to, const EvictArgs& a, hipStream_t st);
+
 // sampling / acceptance
 struct AcceptArgs {
   int kind;                 // SPEC_ACCEPT_*
