@@ -351,9 +351,12 @@ size_t spec_attend_quant_workspace_bytes(const spec_quant_cache* cache, const in
 /* The attention weight that entries get from the rows of a call: weight[s][h][entry] += sum over the rows that see it and the
  * query heads of KV head h of exp(scale * q k - lse), q, scale, window, sinks and lse as in (and from) spec_attend_quant.  Entries of the
  * rows themselves start from 0, so nothing has to be cleared; what lies behind the last entry stays as it is.  weight: fp32
- * [n_seqs][n_kv_heads][ldw], ldw >= 64 * max_pages. */
+ * [n_seqs][n_kv_heads][ldw], ldw >= 64 * max_pages.  work_dev as for spec_attend_quant, of spec_weigh_quant_workspace_bytes. */
 int spec_weigh_quant(const spec_quant_cache* cache, const void* q_dev, long long ldq, const float* lse_dev, const int32_t* row_start_dev,
-                     int n_rows, int n_heads, float scale, int window, int sinks, float* weight_dev, long long ldw, void* stream);
+                     int n_rows, int n_heads, float scale, int window, int sinks, float* weight_dev, long long ldw, void* work_dev,
+                     void* stream);
+size_t spec_weigh_quant_workspace_bytes(const spec_quant_cache* cache, const int32_t* row_start_dev, int n_rows, int n_heads, int window,
+                                        int sinks);
 /* Keep `budget` entries of every sequence and head: the first `sinks`, the last `recent`, and between them those of the largest
  * weight (of equal ones the first; NaN counts as the least), in their order; all where there are no more than budget.  They go to the pages of `to`
  * (same heads and sequences, its own table; it may share the pools, but no page of its table may be one that `cache` still reads), with

@@ -109,7 +109,9 @@ SIGNATURES = {
                                     _P, _P, _P]),
     "spec_attend_quant": (C.c_int, [_P, _P, C.c_longlong, _P, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, _P, _P, _P, _P]),
     "spec_attend_quant_workspace_bytes": (C.c_size_t, [_P, _P, C.c_int, C.c_int, C.c_int, C.c_int]),
-    "spec_weigh_quant": (C.c_int, [_P, _P, C.c_longlong, _P, _P, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, _P, C.c_longlong, _P]),
+    "spec_weigh_quant": (C.c_int, [_P, _P, C.c_longlong, _P, _P, C.c_int, C.c_int, C.c_float, C.c_int, C.c_int, _P, C.c_longlong, _P,
+                                   _P]),
+    "spec_weigh_quant_workspace_bytes": (C.c_size_t, [_P, _P, C.c_int, C.c_int, C.c_int, C.c_int]),
     "spec_evict_quant": (C.c_int, [_P, _P, C.c_longlong, _P, C.c_int, C.c_int, C.c_int, _P, _P, C.c_longlong, _P]),
     "spec_read_probe": (C.c_int, [_P, C.c_size_t, _P, _P]),
     "spec_sample_row": (C.c_int, [_P, C.c_int, C.c_float, C.c_float, C.c_float, _P, _P, _P]),

@@ -144,9 +144,13 @@ def weigh_fp8(cache: Fp8Cache, q: torch.Tensor, lse: torch.Tensor, weight: torch
         raise ValueError("q: bfloat16 is wanted")
     if not (lse.dtype is torch.float32 and lse.shape == (n, heads) and lse.is_contiguous() and lse.get_device() == cache.device):
         raise ValueError("lse: contiguous float32 [n][query heads] on the device of q is wanted")
-    ldw = cache._weights(weight, cache.capacity, "weight")
-    call_on(cache.device, load_library().spec_weigh_quant, cache.ref, q.data_ptr(), ldq, lse.data_ptr(), cache._starts(rows), n, heads,
-            d ** -0.5 if scale is None else scale, _int32(window, "window"), _int32(sinks, "sinks"), weight.data_ptr(), ldw)
+    ldw, start = cache._weights(weight, cache.capacity, "weight"), cache._starts(rows)
+    _int32(window, "window"), _int32(sinks, "sinks")
+    lib = load_library()
+    size = lib.spec_weigh_quant_workspace_bytes(cache.ref, start, n, heads, window, sinks)
+    work = q.new_empty(size, dtype=torch.uint8) if size else None
+    call_on(cache.device, lib.spec_weigh_quant, cache.ref, q.data_ptr(), ldq, lse.data_ptr(), start, n, heads,
+            d ** -0.5 if scale is None else scale, window, sinks, weight.data_ptr(), ldw, work.data_ptr() if size else None)
     return weight
 
 

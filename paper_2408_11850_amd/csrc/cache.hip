@@ -21,6 +21,8 @@ typedef __attribute__((ext_vector_type(8), aligned(2))) unsigned short bf16x8a;
 #define LEAST_EXP (-100)            // scales are 2^e, e >= this
 #define FINITE_MAX 0x1p120f         // keys and values from here on count as infinite: their scales would leave fp32's range
 #define NONE (-3.0e38f)             // running maximum of a row that has seen nothing; scores below it cannot be told from it
+#define LAG 8.f                     // a row's reference stays until a score is so far above it: weights reach 2^8, which changes no bit of a ratio
+#define FAR 0x1p20f                 // references from here on: see where it is used
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
 
@@ -48,43 +50,75 @@ __device__ __forceinline__ unsigned moved4(unsigned w, float by) {
 }
 __device__ __forceinline__ float move_by(int from, int to) { return power(max(from - to, -126)); }
 
+// a * b - c with both roundings
+__device__ __forceinline__ float difference(float a, float b, float c) {
+#pragma clang fp contract(off)
+  const float p = a * b;
+  return p - c;
+}
+
+// over a wave, the same bits in every lane
+template <int CTRL>
+__device__ __forceinline__ float rotated(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float row_max(float v) {
+  v = fmaxf(v, rotated<0x128>(v));
+  v = fmaxf(v, rotated<0x124>(v));
+  v = fmaxf(v, rotated<0x122>(v));
+  return fmaxf(v, rotated<0x121>(v));
+}
+__device__ __forceinline__ float row_sum(float v) {
+  v += rotated<0x128>(v);
+  v += rotated<0x124>(v);
+  v += rotated<0x122>(v);
+  return v + rotated<0x121>(v);
+}
+__device__ __forceinline__ float wave_max(float v) { return groups_max(row_max(v)); }
+__device__ __forceinline__ float wave_sum(float v) { return groups_sum(row_sum(v)); }
+
 // ---- which rows a workgroup works on --------------------------------------------------------------------------------------
 struct Span {
   int s;          // sequence, or -1: none
   int t;          // which of its tiles
   int row, M;     // its first row and their number
+  int len;        // what the cache says of its length
 };
-// Tile `id` of all sequences' tiles one behind the other; tiles(M) of a sequence with M rows.  Called by whole waves.
+// sums of a value over the lanes up to one's own
+__device__ __forceinline__ int lanes_upto(int v) {
+  const int lane = threadIdx.x & 63;
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);            // one, two, four and eight lanes down in a row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  const int a = __builtin_amdgcn_readlane(v, 15), b = __builtin_amdgcn_readlane(v, 31), c = __builtin_amdgcn_readlane(v, 47);
+  return v + (lane >= 16 ? a : 0) + (lane >= 32 ? b : 0) + (lane >= 48 ? c : 0);
+}
+// Tile `id` of all sequences' tiles one behind the other; tiles(M) of a sequence with M rows.  Called by whole waves, the same in all lanes.
 template <class Tiles>
 __device__ __forceinline__ Span find_span(const QuantCache& c, const int* rows, int n_rows, int id, Tiles tiles) {
   if (!rows) {
     const int M = n_rows / c.n_seqs, per = tiles(M), s = id / per;
-    return s < c.n_seqs ? Span{s, id - s * per, s * M, M} : Span{-1, 0, 0, 0};
+    return s < c.n_seqs ? Span{s, id - s * per, s * M, M, c.len[s]} : Span{-1, 0, 0, 0, 0};
   }
-  const int lane = threadIdx.x & 63;
   int before = 0;
   for (int base = 0; base < c.n_seqs; base += 64) {
-    const int s = base + lane;
-    int first = 0, M = 0;
+    const int s = base + (int)(threadIdx.x & 63);
+    int first = 0, M = 0, len = 0;
     if (s < c.n_seqs) {                       // whatever the numbers are, the rows are rows of the call
       first = min(max(rows[s], 0), n_rows);
       M = min(max(rows[s + 1], first), n_rows) - first;
+      len = c.len[s];
     }
-    const int mine = M > 0 ? tiles(M) : 0;
-    int upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      upto += lane >= d ? o : 0;
-    }
-    const int all = __shfl(upto, 63);
+    const int mine = M > 0 ? tiles(M) : 0, upto = lanes_upto(mine), all = __builtin_amdgcn_readlane(upto, 63);
     if (id - before < all) {
       const int at = __ffsll((long long)__ballot(upto > id - before)) - 1;
-      return Span{base + at, id - before - __shfl(upto - mine, at), __shfl(first, at), __shfl(M, at)};
+      return Span{base + at, id - before - __builtin_amdgcn_readlane(upto - mine, at), __builtin_amdgcn_readlane(first, at),
+                  __builtin_amdgcn_readlane(M, at), __builtin_amdgcn_readlane(len, at)};
     }
     before += all;
   }
-  return Span{-1, 0, 0, 0};
+  return Span{-1, 0, 0, 0, 0};
 }
 
 // Pages that rows at the entries lo .. hi see: the first `a` (with a window: those of the sinks), then from `b` on.
@@ -101,6 +135,38 @@ __device__ __forceinline__ Seen seen_pages(int lo, int hi, int window, int sinks
   }
   return Seen{a, b, a + hi / PAGE - b + 1};
 }
+
+// Ids and scales of the pages that a wave goes over, 64 at a time: a lane holds those of a page, so that none of them is waited for
+// on the way to a page's codes.
+struct PageList {
+  const QuantCache& c;
+  const int* table;
+  Seen seen;
+  int h, step, first;     // the wave's pages are first, first + step, ... of `seen`
+  int base, id;
+  float ks, vs;
+  __device__ __forceinline__ PageList(const QuantCache& c, int s, const Seen& seen, int h, int first, int step)
+      : c(c), table(c.table + (size_t)s * c.table_ld), seen(seen), h(h), step(step), first(first), base(-64), id(0), ks(0.f), vs(0.f) {}
+  __device__ __forceinline__ void fetch(int from) {
+    base = from;
+    const int i = first + (from + (int)(threadIdx.x & 63)) * step;
+    id = i < seen.n ? table[seen.page(i)] : -1;
+    const bool there = (unsigned)id < (unsigned)c.n_pages;
+    const float2 x = *reinterpret_cast<const float2*>(c.scale + ((size_t)(there ? id : 0) * c.n_kv_heads + h) * 2);
+    id = there ? id : -1;
+    ks = x.x, vs = x.y;
+  }
+  // waits for what was fetched: no wait in the loop around, where codes are on their way
+  __device__ __forceinline__ void settle() { asm volatile("" : "+v"(id), "+v"(ks), "+v"(vs)); }
+  __device__ __forceinline__ int first_id() const { return __builtin_amdgcn_readlane(id, 0); }
+  // page i of the wave: its id, -1 if it is none of the cache, and its scales
+  __device__ __forceinline__ int get(int i, float* k, float* v) {
+    if (i >= base + 64) fetch(i), settle();
+    *k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), i - base));
+    *v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), i - base));
+    return __builtin_amdgcn_readlane(id, i - base);
+  }
+};
 
 // ---- append ---------------------------------------------------------------------------------------------------------------
 // A workgroup takes the entries of a call that fall into one page: keys and values of a KV head, or eight query heads.  The
@@ -133,7 +199,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(QuantCache c, Ap
   __shared__ float tops[APPEND_THREADS / 64][2];
   const Span sp = find_span(c, a.rows, a.n_rows, blockIdx.x, [](int M) { return (M + 2 * PAGE - 2) / PAGE; });
   if (sp.s < 0) return;
-  const int len = min(max(c.len[sp.s], 0), INT_MAX / 2), first = len - sp.M, capacity = c.max_pages * PAGE;
+  const int len = min(max(sp.len, 0), INT_MAX / 2), first = len - sp.M, capacity = c.max_pages * PAGE;
   const int page0 = ((first >> 6) + sp.t) * PAGE;                    // first may be negative
   const int lo = max(first, page0), hi = min(len, page0 + PAGE);     // the entries of this page
   if (lo >= hi) return;
@@ -235,8 +301,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void append_kernel(QuantCache c, Ap
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor(top[i], d));
+    top[i] = wave_max(top[i]);
     if ((tid & 63) == 0) tops[tid >> 6][i] = top[i];
   }
   __syncthreads();
@@ -320,33 +385,21 @@ hipError_t launch_append_quant(const QuantCache& c, const AppendArgs& a, int typ
 // and 16 neighbouring bytes of a value's row its partner.  16 neighbouring bytes of a key likewise: the contraction over d takes
 // them in that order on both sides.
 template <int DH>
-struct PageData {
-  u32x4 k[4][DH / 64], v[DH / 16];
-  float ks, vs;
-  bool there;
-};
-
-template <int DH>
-__device__ __forceinline__ void load_keys(const QuantCache& c, PageData<DH>& p, int page, int h, int lane) {
+__device__ __forceinline__ void load_keys(const QuantCache& c, u32x4 (&k)[4][DH / 64], int page, int h, int lane) {
   const int r = lane & 15, g = lane >> 4;
-  p.there = (unsigned)page < (unsigned)c.n_pages;
-  const size_t at = (size_t)(p.there ? page : 0) * c.n_kv_heads + h;
-  const uint8_t* k = c.k + at * PAGE * DH + (16 * (r >> 2) + (r & 3)) * DH + g * 16;
+  const uint8_t* p = c.k + ((size_t)max(page, 0) * c.n_kv_heads + h) * PAGE * DH + (16 * (r >> 2) + (r & 3)) * DH + g * 16;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int f = 0; f < DH / 64; ++f) p.k[t][f] = *reinterpret_cast<const u32x4*>(k + 4 * t * DH + f * 64);
-  p.ks = p.there ? c.scale[at * 2] : __uint_as_float(0x7fc00000u);       // no such page: whoever sees it becomes NaN
+    for (int f = 0; f < DH / 64; ++f) k[t][f] = *reinterpret_cast<const u32x4*>(p + 4 * t * DH + f * 64);
 }
 template <int DH>
-__device__ __forceinline__ void load_values(const QuantCache& c, PageData<DH>& p, int page, int h, int lane) {
-  const bool there = (unsigned)page < (unsigned)c.n_pages;
-  const size_t at = (size_t)(there ? page : 0) * c.n_kv_heads + h;
-  const uint8_t* v = c.v + at * PAGE * DH + (lane & 15) * PAGE + (lane >> 4) * 16;
+__device__ __forceinline__ void load_values(const QuantCache& c, u32x4 (&v)[DH / 16], int page, int h, int lane) {
+  const uint8_t* p = c.v + ((size_t)max(page, 0) * c.n_kv_heads + h) * PAGE * DH + (lane & 15) * PAGE + (lane >> 4) * 16;
 #pragma unroll
-  for (int d = 0; d < DH / 16; ++d) p.v[d] = *reinterpret_cast<const u32x4*>(v + d * 16 * PAGE);
-  p.vs = c.scale[at * 2 + 1];
+  for (int d = 0; d < DH / 16; ++d) v[d] = *reinterpret_cast<const u32x4*>(p + d * 16 * PAGE);
 }
+#define NAN32 __uint_as_float(0x7fc00000u)
 
 #define FEW_WAVES 4
 template <int DH, int RT>
@@ -362,7 +415,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
   sp.s = __builtin_amdgcn_readfirstlane(sp.s);
   if (sp.s < 0) return;
   sp.t = __builtin_amdgcn_readfirstlane(sp.t), sp.row = __builtin_amdgcn_readfirstlane(sp.row), sp.M = __builtin_amdgcn_readfirstlane(sp.M);
-  const int capacity = c.max_pages * PAGE, given = c.len[sp.s];
+  const int capacity = c.max_pages * PAGE, given = __builtin_amdgcn_readfirstlane(sp.len);
   const bool beyond = given > capacity;              // nothing is read; the rows become NaN
   const int len = max(given, 0), first = len - sp.M, R = sp.M * G;
   const int phases = FEW_WAVES / a.row_waves, rw = w % a.row_waves, phase = w / a.row_waves;
@@ -400,20 +453,23 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const int* table = c.table + (size_t)sp.s * c.table_ld;
-  PageData<DH> p;
-  int i = i0 + phase;
-  if (i < i1) {
-    const int id = table[seen.page(i)];
-    load_keys<DH>(c, p, id, h, lane);
-    load_values<DH>(c, p, id, h, lane);
+  PageList pages(c, sp.s, seen, h, i0 + phase, phases);
+  const int mine = max(0, (i1 - i0 - phase + phases - 1) / phases);           // pages of this wave
+  u32x4 kd[4][DH / 64], vd[DT];
+  float ks = 0.f, vs = 0.f;
+  int id = -1;
+  if (mine > 0) {
+    pages.fetch(0);                            // the first codes are asked for behind the scales, and waited for with them
+    load_keys<DH>(c, kd, pages.first_id(), h, lane);
+    load_values<DH>(c, vd, pages.first_id(), h, lane);
+    pages.settle();
+    id = pages.get(0, &ks, &vs);
   }
-  for (; i < i1; i += phases) {
-    const int e0 = seen.page(i) * PAGE;
-    const bool more = i + phases < i1;
-    const int next = more ? table[seen.page(i + phases)] : 0;
-    const float by = p.ks * a.scale_log2e;
-    const bool there = p.there;
+  for (int i = 0; i < mine; ++i) {
+    const int e0 = seen.page(i0 + phase + i * phases) * PAGE;
+    const bool there = id >= 0, more = i + 1 < mine;
+    const float by = there ? ks * a.scale_log2e : NAN32, vscale = there ? vs : 0.f;     // no such page: whoever sees it becomes NaN
+    if (more) id = pages.get(i + 1, &ks, &vs);
     f32x4 s[RT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -421,13 +477,26 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
       for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        const bf16x8 kf = to_bf16x8(p.k[t][j >> 1][(j & 1) * 2], p.k[t][j >> 1][(j & 1) * 2 + 1], 1.f);
+        const bf16x8 kf = to_bf16x8(kd[t][j >> 1][(j & 1) * 2], kd[t][j >> 1][(j & 1) * 2 + 1], 1.f);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][j], s[rt][t], 0, 0, 0);
       }
     }
-    if (more) load_keys<DH>(c, p, next, h, lane);
-    const bool all = e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks);
+    if (more) load_keys<DH>(c, kd, id, h, lane);
+    if (!(e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks))) {
+      const int from = e0 + 16 * g;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const int low = a.window ? pos[rt] - a.window : INT_MIN;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int e = from + 4 * t + x;
+            s[rt][t][x] = (e <= pos[rt]) & ((e > low) | (e < a.sinks)) ? s[rt][t][x] : -INFINITY;
+          }
+      }
+    }
     bf16x8 pf[RT][2];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -435,33 +504,36 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float v = s[rt][t][x] * by;
-          if (!all) {
-            const int e = e0 + 16 * g + 4 * t + x;
-            const bool see = e <= pos[rt] && (!a.window || e > pos[rt] - a.window || e < a.sinks);
-            v = see ? v : -INFINITY;
-          }
-          s[rt][t][x] = v;
-          mx = fmaxf(mx, v);
-        }
-      const float m_new = fmaxf(m[rt], groups_max(mx));
-      const float corr = __builtin_amdgcn_exp2f(m[rt] - m_new);
+        for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[rt][t][x]);
+      mx = groups_max(mx) * by;
+      if (__any(mx > m[rt] + LAG)) {             // maxima settle after a few pages
+        asm volatile("" ::: "memory");           // and what is to do then stays here
+        const float m_new = fmaxf(m[rt], mx), corr = __builtin_amdgcn_exp2f(m[rt] - m_new);
+        m[rt] = m_new;
+        l[rt] *= corr;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[rt][d] *= corr;
+      }
+      // the product with the scale in one rounding with the difference, unless its own rounding, left in the largest score, would count
+      float mul = by, less = m[rt];
+      if (__any(fabsf(less) > FAR)) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) s[rt][t][x] = difference(s[rt][t][x], by, less);
+        mul = 1.f, less = 0.f;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const float v = __builtin_amdgcn_exp2f(s[rt][t][x] - m_new);
+          const float v = __builtin_amdgcn_exp2f(fmaf(s[rt][t][x], mul, -less));
           sum += v;
           pf[rt][t >> 1][(t & 1) * 4 + x] = (__bf16)v;
         }
-      l[rt] = l[rt] * corr + sum;
-      m[rt] = m_new;
-      if (!__all(corr == 1.f)) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[rt][d] *= corr;
-      }
+      l[rt] += sum;
     }
     // entries behind the last one, or of no page, may hold anything: 0 times a NaN would be one
     const int live = there ? min(len - e0, PAGE) - 16 * g : 0;
@@ -471,19 +543,18 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
         const int n = live - 4 * x;
         const unsigned keep = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << n * 8) - 1;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) p.v[d][x] &= keep;
+        for (int d = 0; d < DT; ++d) vd[d][x] &= keep;
       }
     }
-    const float vs = there ? p.vs : 0.f;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const bf16x8 vf = to_bf16x8(p.v[d][x * 2], p.v[d][x * 2 + 1], vs);
+        const bf16x8 vf = to_bf16x8(vd[d][x * 2], vd[d][x * 2 + 1], vscale);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) o[rt][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt][x], o[rt][d], 0, 0, 0);
       }
-    if (more) load_values<DH>(c, p, next, h, lane);
+    if (more) load_values<DH>(c, vd, id, h, lane);
   }
   // the waves of a row tile together
 #pragma unroll
@@ -538,27 +609,265 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
   }
 }
 
-// Parts of a row's attention together; a lane has 4 elements, 64 * 4 / DH rows share a wave.
+// Many rows: a workgroup of 8 waves has 256 rows of a KV head, a wave 32 of them, and a page is converted to bf16 once for all, on its
+// way to LDS.  S^T = K Q^T and O^T += V^T P^T, 32 x 32 x 16: row 8 b + 4 c + i of a key tile is entry 16 (b / 2) + 8 c + 4 (b % 2) + i, so that
+// again a lane's scores are the operand it gives, here against eight neighbouring entries of a value's row.  Scores of the next page
+// are formed while the softmax of the present one runs: keys are in LDS one page ahead of values.
+#define MANY_WAVES 8
+#define MANY_ROWS (MANY_WAVES * 32)
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
 template <int DH>
-__global__ __launch_bounds__(256) void attend_merge_kernel(QuantCache c, AttendArgs a) {
-  constexpr int LANES = DH / 4;
-  const size_t all = (size_t)a.n_rows * a.n_heads, at = (size_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (at >= all) return;
-  const int row = (int)(at / a.n_heads);
-  // rows behind the last sequence have no parts and stay as they are; a row in front of the first entry sees nothing
-  if (a.rows && (row >= a.rows[c.n_seqs] || row < a.rows[0])) return;
-  float top = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[s * all + at].x);
-  const bool empty = top == -INFINITY;
-  float sum = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  const int lane = threadIdx.x % LANES;
-  for (int s = 0; s < a.splits; ++s) {
-    const float2 ml = a.part_ml[s * all + at];
-    const float f = __builtin_amdgcn_exp2f(ml.x - top);
-    sum += ml.y * f;
-    if (ml.y != 0.f) o += *reinterpret_cast<const f32x4*>(a.part + (s * all + at) * DH + lane * 4) * f;
+__global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCache c, AttendArgs a) {
+  constexpr int KS = DH / 16, DT = DH / 32;
+  constexpr int KB = 65, VB = 66;              // 16-byte units of an operand block: 64, and what keeps the writes of 8 lanes apart
+  constexpr bool BOTH = DH == 128;             // a thread brings 16 bytes of the keys and of the values; with 64 either
+  __shared__ u32x4 ksh[2][2 * KS * KB], vsh[2][DT * 4 * VB];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
+  const unsigned parts = c.n_kv_heads * a.splits, part = blockIdx.x % parts;
+  const int h = part % c.n_kv_heads, split = part / c.n_kv_heads, G = a.G;
+  Span sp = find_span(c, a.rows, a.n_rows, gridDim.x / parts - 1 - blockIdx.x / parts, [&](int M) { return (M * G + MANY_ROWS - 1) / MANY_ROWS; });
+  sp.s = __builtin_amdgcn_readfirstlane(sp.s);
+  if (sp.s < 0) return;
+  sp.t = __builtin_amdgcn_readfirstlane(sp.t), sp.row = __builtin_amdgcn_readfirstlane(sp.row), sp.M = __builtin_amdgcn_readfirstlane(sp.M);
+  const int given = __builtin_amdgcn_readfirstlane(sp.len);
+  const bool beyond = given > c.max_pages * PAGE;
+  const int len = max(given, 0), first = len - sp.M, R = sp.M * G;
+  const int wg0 = sp.t * MANY_ROWS, wg_last = min(wg0 + MANY_ROWS, R) - 1, r0 = wg0 + w * 32, r_last = min(r0 + 32, R) - 1;
+  const Seen seen = seen_pages(first + wg0 / G, beyond ? -1 : first + wg_last / G, a.window, a.sinks);
+  const int per = (seen.n + a.splits - 1) / a.splits, i0 = split * per, n = min(i0 + per, seen.n) - i0;
+  const int see_all = first + r0 / G, low_all = a.window ? first + max(r_last, 0) / G - a.window + 1 : 0;
+
+  const int r = r0 + r32;
+  const bool valid = r < R;
+  const int tok = valid ? r / G : 0, hq = h * G + (valid ? r % G : 0), pos = valid ? first + tok : -1;
+  const size_t row_at = (size_t)(sp.row + tok) * a.n_heads + hq;
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int j = 0; j < KS; ++j)
+    qf[j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(a.q + (size_t)(sp.row + tok) * a.ldq + (size_t)hq * DH + half * 8 + j * 16));
+  float m = NONE, l = 0.f;
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = f32x16{};
+
+  // what this thread brings of a page, and where it goes
+  const bool has_k = BOTH || tid < 256, has_v = BOTH || tid >= 256;
+  const int kt = tid / KS % 64, kj = tid % KS, ku = kt & 31;
+  const int kto = ((kt >> 5) * KS + kj) * KB + 8 * (2 * (ku >> 4) + ((ku >> 2) & 1)) + 4 * ((ku >> 3) & 1) + (ku & 3);
+  const int vd = tid / 4 % DH, vj = tid & 3, vto = ((vd >> 5) * 4 + vj) * VB + (vd & 31);
+  PageList pages(c, sp.s, seen, h, i0, 1);
+  struct Raw {
+    u32x4 k, v;
+    float ks, vs;
+    int id;
+  };
+  // keys are asked for first, the values of the same page a step later
+  auto load_k = [&](Raw& p, int i) {
+    p.id = pages.get(i, &p.ks, &p.vs);
+    if (has_k) p.k = *reinterpret_cast<const u32x4*>(c.k + ((size_t)max(p.id, 0) * c.n_kv_heads + h) * PAGE * DH + kt * DH + kj * 16);
+  };
+  auto load_v = [&](Raw& p) {
+    if (has_v) p.v = *reinterpret_cast<const u32x4*>(c.v + ((size_t)max(p.id, 0) * c.n_kv_heads + h) * PAGE * DH + vd * PAGE + vj * 16);
+  };
+  auto put_keys = [&](const Raw& p, int to) {
+    if (!has_k) return;
+    u32x4 lo, hi;
+    if (p.id >= 0) {
+      lo = __builtin_bit_cast(u32x4, to_bf16x8(p.k[0], p.k[1], p.ks));
+      hi = __builtin_bit_cast(u32x4, to_bf16x8(p.k[2], p.k[3], p.ks));
+    } else lo = hi = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};      // no such page: whoever sees it becomes NaN
+    ksh[to][kto] = lo;
+    ksh[to][kto + 32] = hi;
+  };
+  auto put_values = [&](Raw& p, int i, int to) {
+    if (!has_v) return;
+    const int e0 = seen.page(i0 + i) * PAGE;
+    if (p.id < 0 || e0 + PAGE > len) {         // entries behind the last one, or of no page, may hold anything: 0 times a NaN would be one
+      const int live = p.id >= 0 ? min(len - e0, PAGE) - 16 * vj : 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int k = live - 4 * x;
+        p.v[x] &= k >= 4 ? 0xffffffffu : k <= 0 ? 0u : (1u << k * 8) - 1;
+      }
+    }
+    const float scale = p.id >= 0 ? p.vs : 0.f;
+    vsh[to][vto] = __builtin_bit_cast(u32x4, to_bf16x8(p.v[0], p.v[1], scale));
+    vsh[to][vto + 32] = __builtin_bit_cast(u32x4, to_bf16x8(p.v[2], p.v[3], scale));
+  };
+  auto scores = [&](f32x16 (&s)[2], int from) {
+    s[0] = f32x16{}, s[1] = f32x16{};
+#pragma unroll
+    for (int j = 0; j < KS; ++j)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ksh[from][(t * KS + j) * KB + lane]), qf[j], s[t], 0, 0, 0);
+  };
+  Raw rk = {}, rv = {};                        // of the page whose keys go to LDS next, and of the one before it
+  const int low = a.window ? pos - a.window : INT_MIN;
+  auto step = [&](f32x16 (&s)[2], f32x16 (&ahead)[2], int i) {
+    __syncthreads();                           // keys of page i + 1 and values of page i are there, their other places free
+    if (i + 2 < n) put_keys(rk, i & 1);
+    if (i + 1 < n) put_values(rv, i + 1, (i + 1) & 1);
+    rv = rk;
+    if (i + 2 < n) load_v(rv);
+    if (i + 3 < n) load_k(rk, i + 3);
+    const int e0 = seen.page(i0 + i) * PAGE;
+    if (!(e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks))) {
+      const int mine = e0 + 8 * half;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int e = mine + 32 * t + 16 * (x >> 3) + (x & 7);
+          s[t][x] = (e <= pos) & ((e > low) | (e < a.sinks)) ? s[t][x] : -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s[t][x]);
+    auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])) * a.scale_log2e;
+    if (__any(mx > m + LAG)) {                 // maxima settle after a few pages
+      asm volatile("" ::: "memory");           // and what is to do then stays here
+      const float m_new = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
+    }
+    // the product with the scale in one rounding with the difference, unless its own rounding, left in the largest score, would count
+    float by = a.scale_log2e, less = m;
+    if (__any(fabsf(m) > FAR)) {
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s[t][x] = difference(s[t][x], a.scale_log2e, m);
+      by = 1.f, less = 0.f;
+    }
+    scores(ahead, (i + 1) & 1);                // behind the last page: of nothing, for nobody
+    bf16x8 pf[4];
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const float v = __builtin_amdgcn_exp2f(fmaf(s[t][x], by, -less));
+        sum += v;
+        pf[t * 2 + (x >> 3)][x & 7] = (__bf16)v;
+      }
+    l += sum;
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vsh[i & 1][(d * 4 + y) * VB + lane]), pf[y], o[d], 0, 0, 0);
+    // operands are asked for six products ahead; the softmax goes between the products of the next scores
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int j = 0; j < 2 * KS; ++j) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 112 / (2 * KS), 0);
+    }
+#pragma unroll
+    for (int j = 0; j < 4 * DT; ++j) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+  };
+  if (n > 0) {
+    f32x16 s0[2], s1[2];
+    load_k(rv, 0);
+    load_v(rv);
+    if (n > 1) load_k(rk, 1);
+    put_keys(rv, 0);
+    put_values(rv, 0, 0);
+    if (n > 1) put_keys(rk, 1);
+    rv = rk;
+    if (n > 1) load_v(rv);
+    if (n > 2) load_k(rk, 2);
+    __syncthreads();
+    scores(s0, 0);
+    for (int i = 0; i < n; i += 2) {
+      step(s0, s1, i);
+      if (i + 1 < n) step(s1, s0, i + 1);
+    }
   }
+  auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(other[0]) + __uint_as_float(other[1]);
+  if (!valid) return;
+  if (beyond) l = __uint_as_float(0x7fc00000u);
+  if (a.splits == 1) {
+    const bool empty = pos < 0;
+    const float inv = empty ? 0.f : 1.f / l;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        bf16 b[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) b[y] = __float2bfloat16(o[d][x * 4 + y] * inv);
+        *reinterpret_cast<uint2*>(a.out + row_at * DH + d * 32 + x * 8 + half * 4) = *reinterpret_cast<const uint2*>(b);
+      }
+    if (a.lse && half == 0) a.lse[row_at] = empty ? -INFINITY : (m + __log2f(l)) * LN2;
+  } else {
+    const size_t at = (size_t)split * a.n_rows * a.n_heads + row_at;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<f32x4*>(a.part + at * DH + d * 32 + x * 8 + half * 4) = f32x4{o[d][x * 4], o[d][x * 4 + 1], o[d][x * 4 + 2], o[d][x * 4 + 3]};
+    if (half == 0) a.part_ml[at] = make_float2(pos < 0 ? -INFINITY : m, l);
+  }
+}
+
+// Parts of a row's attention together.  WAVES waves have a row and head: a lane the maximum and sum of a part (there are at most 64), then
+// 4 elements of some of the parts, the first eight of them asked for beside the sums.
+#define MERGE_WAVES 4
+#define MERGE_PARTS 64
+template <int DH, int WAVES>
+__global__ __launch_bounds__(MERGE_WAVES * 64) void attend_merge_kernel(QuantCache c, AttendArgs a) {
+  constexpr int LANES = DH / 4, WAYS = 64 / LANES * WAVES, AHEAD = 8;
+  __shared__ f32x4 osh[MERGE_WAVES][LANES];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, way = w % WAVES * (64 / LANES) + lane / LANES;
+  const size_t all = (size_t)a.n_rows * a.n_heads, at = (size_t)blockIdx.x * (MERGE_WAVES / WAVES) + w / WAVES;
+  if (at >= all) return;                                                        // WAVES == 4: the whole workgroup
+  const int row = (int)(at / a.n_heads);
+  if (a.rows && (row >= a.rows[c.n_seqs] || row < a.rows[0])) return;         // rows of no sequence have no parts and stay as they are
+  const float2 ml = lane < a.splits ? a.part_ml[lane * all + at] : make_float2(-INFINITY, 0.f);
+  const float* from = a.part + at * DH + (lane % LANES) * 4;
+  f32x4 ahead[AHEAD];
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) {
+    const int s = way + x * WAYS;
+    ahead[x] = s < a.splits ? *reinterpret_cast<const f32x4*>(from + s * all * DH) : f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float top = wave_max(ml.x);
+  const bool empty = top == -INFINITY;                                          // in every part: the row sees nothing
+  const float f = empty || lane >= a.splits ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+  const float sum = wave_sum(ml.y * f);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int x = 0; x < AHEAD; ++x) o += ahead[x] * __shfl(f, (way + x * WAYS) & 63);
+  if (AHEAD * WAYS < MERGE_PARTS)
+#pragma unroll 8
+    for (int s = way + AHEAD * WAYS; s < a.splits; s += WAYS) o += *reinterpret_cast<const f32x4*>(from + s * all * DH) * __shfl(f, s);
+#pragma unroll
+  for (int d = LANES; d < 64; d <<= 1)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) o[x] += __shfl_xor(o[x], d);
+  if (WAVES > 1) {
+    if (lane < LANES) osh[w][lane] = o;
+    __syncthreads();
+    if (w % WAVES) return;
+#pragma unroll
+    for (int x = 1; x < WAVES; ++x) o += osh[w + x][lane % LANES];
+  }
+  if (lane >= LANES) return;
   const float inv = empty ? 0.f : 1.f / sum;
   bf16 b[4];
 #pragma unroll
@@ -568,82 +877,245 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(QuantCache c, AttendA
 }
 
 // ---- attention weight of the entries ------------------------------------------------------------------------------------------
-// w[entry] = sum over the rows and heads of a group of exp(score - lse).  A wave holds the 64 keys of a page as operands and goes
-// over row tiles of 16; a lane's scores belong to one row, so sums over rows stay in registers until the end.
+// w[entry] = sum over the rows and heads of a group of exp(score - lse).
+struct Rows {
+  int row, M, len, first, R;
+  bool none;
+};
+__device__ __forceinline__ Rows rows_of(const QuantCache& c, const int* rows, int n_rows, int s, int G) {
+  Rows r;
+  r.M = n_rows / c.n_seqs, r.row = s * r.M;
+  if (rows) {
+    r.row = min(max(rows[s], 0), n_rows);
+    r.M = min(max(rows[s + 1], r.row), n_rows) - r.row;
+  }
+  const int given = c.len[s];
+  r.len = max(given, 0), r.first = r.len - r.M, r.R = r.M * G;
+  r.none = r.M == 0 || given > c.max_pages * PAGE || given <= 0;
+  return r;
+}
+
+// Few rows: their queries stay in registers, up to RT tiles of 16 at a time, and a wave goes over pages.  S^T = K Q^T as in the attention:
+// a lane's scores belong to one row, so that sums over the rows of a tile are sums over 16 lanes, once per page.
 #define WEIGH_WAVES 4
-template <int DH, bool SHARE>
-__global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_kernel(QuantCache c, WeighArgs a) {
+template <int DH, int RT>
+__global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCache c, WeighArgs a) {
   constexpr int KS = DH / 32;
-  __shared__ float wsh[WEIGH_WAVES][PAGE];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.y, s = blockIdx.z, G = a.G;
-  int row = s * (a.n_rows / c.n_seqs), M = a.n_rows / c.n_seqs;
-  if (a.rows) {
-    row = min(max(a.rows[s], 0), a.n_rows);
-    M = min(max(a.rows[s + 1], row), a.n_rows) - row;
-  }
-  const int len = max(c.len[s], 0), first = len - M, R = M * G;
-  if (M == 0 || len > c.max_pages * PAGE) return;
+  const Rows rs = rows_of(c, a.rows, a.n_rows, s, G);
+  if (rs.none) return;
+  const int first = rs.first, len = rs.len;
   const Seen seen = seen_pages(first, len - 1, a.window, a.sinks);
-  const int i = SHARE ? blockIdx.x : blockIdx.x * WEIGH_WAVES + w;
-  if (i >= seen.n) return;                                     // SHARE: the whole workgroup
-  const int page = seen.page(i), e0 = page * PAGE;
-  PageData<DH> p;
-  load_keys<DH>(c, p, c.table[(size_t)s * c.table_ld + page], h, lane);
-  bf16x8 kf[4][KS];
+  const int from = blockIdx.x * WEIGH_WAVES + w, step = gridDim.x * WEIGH_WAVES;
+  const int mine = (seen.n - from + step - 1) / step;
+  if (mine <= 0) return;
+  float* to = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw;
+  for (int r0 = 0; r0 < rs.R; r0 += 16 * RT) {                // once, unless the rows are far more than those of other sequences
+    bf16x8 qf[RT][KS];
+    float lse[RT];
+    int pos[RT];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+    for (int rt = 0; rt < RT; ++rt) {
+      const int r = r0 + rt * 16 + r16;
+      const bool valid = r < rs.R;
+      const int tok = valid ? r / G : 0, hq = h * G + (valid ? r % G : 0);
+      pos[rt] = valid ? first + tok : -1;
+      lse[rt] = valid ? a.lse[(size_t)(rs.row + tok) * a.n_heads + hq] * LOG2E : 0.f;
+      const bf16* q = a.q + (size_t)(rs.row + tok) * a.ldq + (size_t)hq * DH + g * 16;
 #pragma unroll
-    for (int j = 0; j < KS; ++j) kf[t][j] = to_bf16x8(p.k[t][j >> 1][(j & 1) * 2], p.k[t][j >> 1][(j & 1) * 2 + 1], 1.f);
-  const float by = p.ks * a.scale_log2e;
-  f32x4 sum[4];
+      for (int j = 0; j < KS; ++j) qf[rt][j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + (j >> 1) * 64 + (j & 1) * 8));
+    }
+    const int see_all = first + r0 / G, low_all = a.window ? first + min(r0 + 16 * RT, rs.R) / G - a.window + 1 : 0;
+    PageList pages(c, s, seen, h, from, step);
+    u32x4 kd[4][DH / 64];
+    float ks, vs;
+    pages.fetch(0);
+    load_keys<DH>(c, kd, pages.first_id(), h, lane);
+    pages.settle();
+    int id = pages.get(0, &ks, &vs);
+    for (int i = 0; i < mine; ++i) {
+      const int e0 = seen.page(from + i * step) * PAGE;
+      const float by = id >= 0 ? ks * a.scale_log2e : NAN32;   // no such page: whoever sees it becomes NaN
+      u32x4 now[4][DH / 64];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // the first row that sees the page's first entry
-  const int tile0 = max(0, e0 - first) * G / 16, tiles = (R + 15) / 16;
-  for (int tile = tile0 + (SHARE ? w : 0); tile < tiles; tile += SHARE ? WEIGH_WAVES : 1) {
-    const int r = tile * 16 + r16;
-    const bool valid = r < R;
-    const int tok = valid ? r / G : 0, hq = h * G + (valid ? r % G : 0);
-    const int pos = valid ? first + tok : -1;
-    const bf16* q = a.q + (size_t)(row + tok) * a.ldq + (size_t)hq * DH + g * 16;
-    const float lse = valid ? a.lse[(size_t)(row + tok) * a.n_heads + hq] * LOG2E : 0.f;
-    bf16x8 qf[KS];
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int j = 0; j < KS; ++j) qf[j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + (j >> 1) * 64 + (j & 1) * 8));
+        for (int f = 0; f < DH / 64; ++f) now[t][f] = kd[t][f];
+      if (i + 1 < mine) {
+        id = pages.get(i + 1, &ks, &vs);
+        load_keys<DH>(c, kd, id, h, lane);
+      }
+      const bool all = e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks) && r0 + 16 * RT <= rs.R;
+      f32x4 sum[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < 4; ++t) {
+        f32x4 x[RT];
 #pragma unroll
-      for (int j = 0; j < KS; ++j) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][j], qf[j], x, 0, 0, 0);
+        for (int rt = 0; rt < RT; ++rt) x[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        const int e = e0 + 16 * g + 4 * t + y;
-        const bool see = e <= pos && (!a.window || e > pos - a.window || e < a.sinks);
-        sum[t][y] += see ? __builtin_amdgcn_exp2f(fmaf(x[y], by, -lse)) : 0.f;
+        for (int j = 0; j < KS; ++j) {
+          const bf16x8 kf = to_bf16x8(now[t][j >> 1][(j & 1) * 2], now[t][j >> 1][(j & 1) * 2 + 1], 1.f);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) x[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][j], x[rt], 0, 0, 0);
+        }
+        sum[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const int low = a.window ? pos[rt] - a.window : INT_MIN;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            float v = __builtin_amdgcn_exp2f(difference(x[rt][y], by, lse[rt]));
+            if (!all) {
+              const int e = e0 + 16 * g + 4 * t + y;
+              v = (e <= pos[rt]) & ((e > low) | (e < a.sinks)) ? v : 0.f;
+            }
+            sum[t][y] += v;
+          }
+        }
+      }
+      float v = 0.f;                                          // lane 16 g + 4 t + y: that entry of the page
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const float x = row_sum(sum[t][y]);
+          v = r16 == 4 * t + y ? x : v;
+        }
+      const int e = e0 + lane;
+      if (e < len) to[e] = e < first || r0 ? to[e] + v : v;    // an entry of these rows begins here
+    }
+  }
+}
+
+// Many rows: a wave keeps the 64 keys of a page as operands and the workgroup goes over tiles of 32 rows, whose queries, logarithms and
+// entries pass through LDS.  S = Q K^T, 32 x 32 x 16: a lane's scores belong to one entry.  The tiles that see a group of pages are dealt to
+// `slices` workgroups; sums of slices are added in their order.
+template <int DH>
+__global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCache c, WeighArgs a) {
+  constexpr int KS = DH / 16, QB = 66, CH = DH / 8, LOADS = 32 * CH / (WEIGH_WAVES * 64);
+  __shared__ u32x4 qsh[2][KS * QB];
+  __shared__ __align__(16) float lsh[2][32];
+  __shared__ __align__(16) int psh[2][32];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
+  const int h = blockIdx.y, s = blockIdx.z, G = a.G, group = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+  const Rows rs = rows_of(c, a.rows, a.n_rows, s, G);
+  if (rs.none) return;
+  const int first = rs.first, len = rs.len, R = rs.R;
+  const Seen seen = seen_pages(first, len - 1, a.window, a.sinks);
+  const int i = group * WEIGH_WAVES + w;
+  if (group * WEIGH_WAVES >= seen.n) return;
+  const bool has = i < seen.n;
+  const int page = seen.page(min(i, seen.n - 1)), e0 = page * PAGE;
+  const int id = c.table[(size_t)s * c.table_ld + page];
+  const bool there = (unsigned)id < (unsigned)c.n_pages;
+  const size_t block = (size_t)(there ? id : 0) * c.n_kv_heads + h;
+  bf16x8 kf[2][KS];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int j = 0; j < KS; j += 2) {                          // 16 bytes of a key are two operands: d in that order on both sides
+      const u32x4 x = *reinterpret_cast<const u32x4*>(c.k + block * PAGE * DH + (t * 32 + r32) * DH + j * 16 + half * 16);
+      kf[t][j] = to_bf16x8(x[0], x[1], 1.f);
+      kf[t][j + 1] = to_bf16x8(x[2], x[3], 1.f);
+    }
+  const float by = there ? c.scale[block * 2] * a.scale_log2e : NAN32;             // no such page: whoever sees it becomes NaN
+  // tiles with rows that see any of the group's pages
+  const int lo_e = seen.page(group * WEIGH_WAVES) * PAGE, hi_e = seen.page(min(group * WEIGH_WAVES + WEIGH_WAVES, seen.n) - 1) * PAGE + PAGE - 1;
+  const int tiles = (R + 31) / 32, tile0 = max(0, lo_e - first) * G / 32;
+  int tile1 = tiles;
+  if (a.window && lo_e >= a.sinks && hi_e + a.window - first < rs.M) tile1 = min(tiles, max(0, hi_e + a.window - first) * G / 32 + 1);
+  const int all_tiles = max(0, tile1 - tile0), t0 = tile0 + (int)((long long)slice * all_tiles / a.slices), t1 = tile0 + (int)((long long)(slice + 1) * all_tiles / a.slices);
+  u32x4 raw[LOADS];
+  float lse = 0.f;
+  int pos = -1;
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int at = x * WEIGH_WAVES * 64 + tid, r = min(tile * 32 + at / CH, R - 1), tok = r / G;
+      raw[x] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(rs.row + tok) * a.ldq + (size_t)(h * G + r % G) * DH + at % CH * 8);
+    }
+    if (tid < 32) {
+      const int r = tile * 32 + tid, tok = min(r, R - 1) / G;
+      lse = a.lse[(size_t)(rs.row + tok) * a.n_heads + h * G + min(r, R - 1) % G] * LOG2E;
+      pos = r < R ? first + tok : -1;
+    }
+  };
+  auto put = [&](int to) {
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      // 8 elements: 32 j + 16 c + 8 b are those of step 2 j + b in the lanes of half c
+      const int at = x * WEIGH_WAVES * 64 + tid, r = at / CH, ch = at % CH;
+      qsh[to][(ch / 4 * 2 + (ch & 1)) * QB + (ch >> 1 & 1) * 33 + r] = raw[x];
+    }
+    if (tid < 32) lsh[to][tid] = lse, psh[to][tid] = pos;
+  };
+  float sum[2] = {0.f, 0.f};
+  if (t0 < t1) load(t0), put(0);
+  for (int tile = t0; tile < t1; ++tile) {
+    const int at = (tile - t0) & 1;
+    __syncthreads();                                           // this tile is there, and nobody reads the other place
+    if (tile + 1 < t1) load(tile + 1);
+    f32x16 x[2];
+    x[0] = f32x16{}, x[1] = f32x16{};
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+      const bf16x8 qf = __builtin_bit_cast(bf16x8, qsh[at][j * QB + half * 33 + r32]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[t][j], x[t], 0, 0, 0);
+    }
+    const int p_lo = first + tile * 32 / G, p_hi = first + min(tile * 32 + 31, R - 1) / G;
+    const bool all = e0 + PAGE - 1 <= p_lo && (!a.window || e0 > p_hi - a.window || e0 + PAGE <= a.sinks) && tile * 32 + 32 <= R;
+    if (!all) {
+#pragma unroll
+      for (int y = 0; y < 16; ++y) {
+        const int p = psh[at][8 * (y >> 2) + 4 * half + (y & 3)], low = a.window ? p - a.window : INT_MIN;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int e = e0 + t * 32 + r32;
+          x[t][y] = (e <= p) & ((e > low) | (e < a.sinks)) ? x[t][y] : -INFINITY;
+        }
       }
     }
-  }
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
+    for (int y = 0; y < 16; ++y) {
+      const float l = lsh[at][8 * (y >> 2) + 4 * half + (y & 3)];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-      float v = sum[t][y];
-#pragma unroll
-      for (int d = 1; d < 16; d <<= 1) v += __shfl_xor(v, d);
-      if (r16 == 0) wsh[w][16 * g + 4 * t + y] = v;
+      for (int t = 0; t < 2; ++t) sum[t] += __builtin_amdgcn_exp2f(fmaf(x[t][y], by, -l));
     }
-  if (SHARE) {
-    __syncthreads();
-    if (w) return;
+    if (tile + 1 < t1) put(at ^ 1);
   }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    auto o = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[t]), __float_as_uint(sum[t]), false, false);
+    sum[t] = __uint_as_float(o[0]) + __uint_as_float(o[1]);
+  }
+  const float v = half ? sum[1] : sum[0];
   const int e = e0 + lane;
-  if (e >= len) return;
-  float v = wsh[w][lane];
-  if (SHARE)
-    for (int x = 1; x < WEIGH_WAVES; ++x) v += wsh[x][lane];
-  float* to = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw + e;
-  *to = e < first ? *to + v : v;                               // an entry of these rows begins here
+  if (!has || e >= len) return;
+  const size_t line = (size_t)s * c.n_kv_heads + h;
+  if (a.slices == 1) {
+    float* to = a.weight + line * a.ldw + e;
+    *to = e < first ? *to + v : v;                             // an entry of these rows begins here
+  } else a.part[((size_t)slice * c.n_seqs * c.n_kv_heads + line) * c.max_pages * PAGE + e] = v;
+}
+
+__global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs a) {
+  const int h = blockIdx.y, s = blockIdx.z;
+  const Rows rs = rows_of(c, a.rows, a.n_rows, s, a.G);
+  if (rs.none) return;
+  const Seen seen = seen_pages(rs.first, rs.len - 1, a.window, a.sinks);
+  const int i = blockIdx.x * 4 + threadIdx.x / PAGE;
+  if (i >= seen.n) return;
+  const int e = seen.page(i) * PAGE + threadIdx.x % PAGE;
+  if (e >= rs.len) return;
+  const size_t line = (size_t)s * c.n_kv_heads + h, all = (size_t)c.n_seqs * c.n_kv_heads * c.max_pages * PAGE;
+  const float* p = a.part + line * c.max_pages * PAGE + e;
+  float* to = a.weight + line * a.ldw + e;
+  float v = e < rs.first ? *to : 0.f;                          // an entry of these rows begins here
+#pragma unroll 8
+  for (int x = 0; x < a.slices; ++x) v += p[x * all];
+  *to = v;
 }
 
 // ---- eviction -----------------------------------------------------------------------------------------------------------------
@@ -810,8 +1282,7 @@ __global__ __launch_bounds__(GATHER_THREADS) void evict_gather_kernel(QuantCache
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor(top[i], d));
+    top[i] = wave_max(top[i]);
     if (lane == 0) tops[w][i] = top[i];
   }
   __syncthreads();
@@ -862,6 +1333,7 @@ static long long most_tiles(const QuantCache& c, bool ragged, int n_rows, int G,
   return (long long)c.n_seqs * (((long long)(n_rows / c.n_seqs) * G + tile - 1) / tile);
 }
 struct AttendPlan {
+  bool many;
   int row_tiles;    // of 16 rows per wave
   int row_waves;    // waves of a workgroup that have rows of their own; the others take other pages of theirs
   int splits;
@@ -869,14 +1341,23 @@ struct AttendPlan {
 };
 static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   AttendPlan p;
-  const int G = n_heads / c.n_kv_heads, rows = (n_rows / c.n_seqs + 1) * G;
+  const int G = n_heads / c.n_kv_heads;
+  const long long rows = (long long)((n_rows + c.n_seqs - 1) / c.n_seqs) * G;      // of a sequence, in the mean
+  p.many = rows > 160;
+  if (p.many) {
+    p.tiles = most_tiles(c, ragged, n_rows, G, MANY_ROWS);
+    const int pages = most_pages(c, (MANY_ROWS + G - 1) / G, window, sinks);
+    const long long groups = p.tiles * c.n_kv_heads;
+    p.splits = (int)max(1ll, min(min(spec_num_cu() / groups, (long long)pages / 8), (long long)MERGE_PARTS));
+    return p;
+  }
   p.row_tiles = rows > 16 ? 2 : 1;
   p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
   const int tile = 16 * p.row_tiles * p.row_waves;
   p.tiles = most_tiles(c, ragged, n_rows, G, tile);
   const int pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
-  const long long groups = p.tiles * c.n_kv_heads, want = 4ll * spec_num_cu();
-  p.splits = (int)max(1ll, min(min((want + groups - 1) / groups, (long long)((pages + phases - 1) / phases)), 64ll));
+  const long long groups = p.tiles * c.n_kv_heads, want = 2ll * spec_num_cu();
+  p.splits = (int)max(1ll, min(min((want + groups - 1) / groups, (long long)((pages + phases - 1) / phases)), (long long)MERGE_PARTS));
   return p;
 }
 size_t attend_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
@@ -894,7 +1375,11 @@ hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hi
   const size_t all = (size_t)a.n_rows * a.n_heads;
   a.part = (float*)work;
   a.part_ml = (float2*)(a.part + (size_t)p.splits * all * c.head_dim);
-  if (c.head_dim == 128) {
+  if (p.many) {
+    const unsigned groups = (unsigned)(p.tiles * c.n_kv_heads * p.splits);
+    if (c.head_dim == 128) attend_many_kernel<128><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
+    else attend_many_kernel<64><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
+  } else if (c.head_dim == 128) {
     if (p.row_tiles == 1) launch_few<128, 1>(c, a, p.tiles, st);
     else launch_few<128, 2>(c, a, p.tiles, st);
   } else {
@@ -903,24 +1388,61 @@ hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hi
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  const size_t per = 256 / (c.head_dim / 4);
-  if (c.head_dim == 128) attend_merge_kernel<128><<<(unsigned)((all + per - 1) / per), 256, 0, st>>>(c, a);
-  else attend_merge_kernel<64><<<(unsigned)((all + per - 1) / per), 256, 0, st>>>(c, a);
+  const bool wide = p.splits > 16 && all <= (1u << 16);
+  const unsigned groups = wide ? (unsigned)all : (unsigned)((all + MERGE_WAVES - 1) / MERGE_WAVES);
+  if (c.head_dim == 128) {
+    if (wide) attend_merge_kernel<128, 4><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
+    else attend_merge_kernel<128, 1><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
+  } else {
+    if (wide) attend_merge_kernel<64, 4><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
+    else attend_merge_kernel<64, 1><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
+  }
   return hipGetLastError();
 }
-hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, hipStream_t st) {
-  a.G = a.n_heads / c.n_kv_heads;
-  const long long rows = (long long)(a.n_rows / c.n_seqs + 1) * a.G;
-  const int pages = a.rows || !a.window ? c.max_pages : most_pages(c, a.n_rows / c.n_seqs, a.window, a.sinks);
-  if (rows > 64) {
-    const dim3 grid(pages, c.n_kv_heads, c.n_seqs);
-    if (c.head_dim == 128) weigh_kernel<128, true><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
-    else weigh_kernel<64, true><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
-  } else {
-    const dim3 grid((pages + WEIGH_WAVES - 1) / WEIGH_WAVES, c.n_kv_heads, c.n_seqs);
-    if (c.head_dim == 128) weigh_kernel<128, false><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
-    else weigh_kernel<64, false><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
+struct WeighPlan {
+  int row_tiles;    // of 16 rows, in registers; 0: many rows
+  int pages;        // most that are seen
+  int groups;       // workgroups in x, over the slices' number
+  int slices;
+};
+static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
+  WeighPlan p;
+  const int G = n_heads / c.n_kv_heads, M = (n_rows + c.n_seqs - 1) / c.n_seqs;
+  const long long rows = (long long)M * G, lines = (long long)c.n_seqs * c.n_kv_heads;
+  p.pages = most_pages(c, ragged ? n_rows : M, window, sinks);
+  const int fours = (p.pages + WEIGH_WAVES - 1) / WEIGH_WAVES;
+  p.slices = 1;
+  if (rows <= 64) {
+    p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    p.groups = (int)max(1ll, min((long long)fours, (3ll * spec_num_cu() + lines - 1) / lines));
+    return p;
   }
+  p.row_tiles = 0;
+  p.groups = fours;
+  p.slices = (int)max(1ll, min(min(4ll * spec_num_cu() / (lines * fours), (rows + 255) / 256), 64ll));
+  return p;
+}
+size_t weigh_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
+  const WeighPlan p = weigh_plan(c, ragged, n_rows, n_heads, window, sinks);
+  return p.slices == 1 ? 0 : (size_t)p.slices * c.n_seqs * c.n_kv_heads * c.max_pages * PAGE * sizeof(float);
+}
+template <int DH>
+static void launch_weigh(const QuantCache& c, const WeighArgs& a, const WeighPlan& p, hipStream_t st) {
+  const dim3 grid(p.groups * p.slices, c.n_kv_heads, c.n_seqs);
+  if (p.row_tiles == 1) weigh_few_kernel<DH, 1><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
+  else if (p.row_tiles == 2) weigh_few_kernel<DH, 2><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
+  else if (p.row_tiles == 4) weigh_few_kernel<DH, 4><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
+  else weigh_many_kernel<DH><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
+}
+hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, void* work, hipStream_t st) {
+  const WeighPlan p = weigh_plan(c, a.rows != nullptr, a.n_rows, a.n_heads, a.window, a.sinks);
+  a.G = a.n_heads / c.n_kv_heads;
+  a.slices = p.slices, a.part = (float*)work;
+  if (c.head_dim == 128) launch_weigh<128>(c, a, p, st);
+  else launch_weigh<64>(c, a, p, st);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.slices == 1) return e;
+  weigh_add_kernel<<<dim3((p.pages + 3) / 4, c.n_kv_heads, c.n_seqs), 256, 0, st>>>(c, a);
   return hipGetLastError();
 }
 hipError_t launch_evict_quant(const QuantCache& c, const QuantCache& to, const EvictArgs& a, hipStream_t st) {

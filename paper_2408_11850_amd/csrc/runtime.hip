@@ -1613,12 +1613,21 @@ extern "C" int spec_append_quant(const spec_quant_cache* cache, const void* k, l
   HIPCHK(launch_append_quant(c, a, type, (hipStream_t)stream));
   return SPEC_OK;
 }
+// which of two workspaces' sizes, 0 for what the call would refuse
+static size_t cache_work_bytes(const spec_quant_cache* cache, const int32_t* row_start, int n_rows, int n_heads, int window, int sinks,
+                               size_t (*bytes)(const QuantCache&, bool, int, int, int, int)) {
+  QuantCache c;
+  if (check_quant_cache(cache, &c) || check_cache_rows(c, row_start, n_rows, n_heads)) return 0;
+  if (check_cache_q(c, c.k, (long long)n_heads * c.head_dim, n_heads, 1.0f, &window, &sinks)) return 0;
+  return bytes(c, row_start != nullptr, n_rows, n_heads, window, sinks);
+}
 extern "C" size_t spec_attend_quant_workspace_bytes(const spec_quant_cache* cache, const int32_t* row_start, int n_rows, int n_heads,
                                                     int window, int sinks) {
-  QuantCache c;
-  if (check_quant_cache(cache, &c) || check_cache_rows(c, row_start, n_rows, n_heads) || window < 0 || sinks < 0) return 0;
-  (void)check_cache_q(c, c.k, (long long)n_heads * c.head_dim, n_heads, 1.0f, &window, &sinks);
-  return attend_quant_work_bytes(c, row_start != nullptr, n_rows, n_heads, window, sinks);
+  return cache_work_bytes(cache, row_start, n_rows, n_heads, window, sinks, attend_quant_work_bytes);
+}
+extern "C" size_t spec_weigh_quant_workspace_bytes(const spec_quant_cache* cache, const int32_t* row_start, int n_rows, int n_heads,
+                                                   int window, int sinks) {
+  return cache_work_bytes(cache, row_start, n_rows, n_heads, window, sinks, weigh_quant_work_bytes);
 }
 extern "C" int spec_attend_quant(const spec_quant_cache* cache, const void* q, long long ldq, const int32_t* row_start, int n_rows,
                                  int n_heads, float scale, int window, int sinks, void* out, float* lse, void* work, void* stream) {
@@ -1646,7 +1655,8 @@ extern "C" int spec_attend_quant(const spec_quant_cache* cache, const void* q, l
   return SPEC_OK;
 }
 extern "C" int spec_weigh_quant(const spec_quant_cache* cache, const void* q, long long ldq, const float* lse, const int32_t* row_start,
-                                int n_rows, int n_heads, float scale, int window, int sinks, float* weight, long long ldw, void* stream) {
+                                int n_rows, int n_heads, float scale, int window, int sinks, float* weight, long long ldw, void* work,
+                                void* stream) {
   QuantCache c;
   int rc = check_quant_cache(cache, &c);
   if (rc) return rc;
@@ -1657,12 +1667,18 @@ extern "C" int spec_weigh_quant(const spec_quant_cache* cache, const void* q, lo
   if (!lse || !weight) FAIL(SPEC_E_INVAL, "null pointer");
   if (off_by(lse, 4) || off_by(weight, 4)) FAIL(SPEC_E_INVAL, "misaligned operand");
   if (ldw < (long long)c.max_pages * SPEC_PAGE_TOKENS || ldw > 1ll << 40) FAIL(SPEC_E_INVAL, "a row of weights holds every entry of a sequence");
-  const size_t n = n_rows, bytes = (size_t)c.n_seqs * c.n_kv_heads * (size_t)ldw * 4;
-  if (meets_cache(c, weight, bytes) || meet(row_start, row_start ? (size_t)(c.n_seqs + 1) * 4 : 0, weight, bytes) ||
-      meet(lse, n * n_heads * 4, weight, bytes) || meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, weight, bytes))
-    FAIL(SPEC_E_INVAL, "results must not overlap what is read");
-  WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, lse, weight, (size_t)ldw, 0};
-  HIPCHK(launch_weigh_quant(c, a, (hipStream_t)stream));
+  if (off_by(work, 16)) FAIL(SPEC_E_INVAL, "misaligned operand");
+  const size_t n = n_rows, need = weigh_quant_work_bytes(c, row_start != nullptr, n_rows, n_heads, window, sinks);
+  if (need && !work) FAIL(SPEC_E_INVAL, "these rows need a workspace");
+  const Region to[2] = {{weight, (size_t)c.n_seqs * c.n_kv_heads * (size_t)ldw * 4}, {work, need}};
+  bool clash = meet(to[0].p, to[0].bytes, to[1].p, to[1].bytes);
+  for (const Region& r : to)
+    clash |= meets_cache(c, r.p, r.bytes) || meet(row_start, row_start ? (size_t)(c.n_seqs + 1) * 4 : 0, r.p, r.bytes) ||
+             meet(lse, n * n_heads * 4, r.p, r.bytes) || meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, r.p, r.bytes);
+  if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
+  WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, lse, weight, (size_t)ldw,
+                 0, 0, nullptr};
+  HIPCHK(launch_weigh_quant(c, a, work, (hipStream_t)stream));
   return SPEC_OK;
 }
 extern "C" int spec_evict_quant(const spec_quant_cache* cache, const float* weight, long long ldw, const spec_quant_cache* to, int budget,

@@ -245,7 +245,8 @@ struct WeighArgs {
   const float* lse;
   float* weight;
   size_t ldw;
-  int G;                      // set by the launch
+  int G, slices;              // set by the launch ...
+  float* part;                // ... sums of slices [slices][n_seqs][n_kv_heads][64 max_pages]
 };
 struct EvictArgs {
   const float* weight;
@@ -259,7 +260,8 @@ struct EvictArgs {
 hipError_t launch_append_quant(const QuantCache& c, const AppendArgs& a, int type, hipStream_t st);
 size_t attend_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks);
 hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hipStream_t st);
-hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, hipStream_t st);
+size_t weigh_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks);
+hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, void* work, hipStream_t st);
 hipError_t launch_evict_quant(const QuantCache& c, const QuantCache& to, const EvictArgs& a, hipStream_t st);
 
 // sampling / acceptance
