@@ -158,7 +158,7 @@ struct PageList {
   }
   // waits for what was fetched: no wait in the loop around, where codes are on their way
   __device__ __forceinline__ void settle() { asm volatile("" : "+v"(id), "+v"(ks), "+v"(vs)); }
-  __device__ __forceinline__ int first_id() const { return __builtin_amdgcn_readlane(id, 0); }
+  __device__ __forceinline__ int first_id(int i = 0) const { return __builtin_amdgcn_readlane(id, i); }
   // page i of the wave: its id, -1 if it is none of the cache, and its scales
   __device__ __forceinline__ int get(int i, float* k, float* v) {
     if (i >= base + 64) fetch(i), settle();
@@ -401,49 +401,124 @@ __device__ __forceinline__ void load_values(const QuantCache& c, u32x4 (&v)[DH /
 }
 #define NAN32 __uint_as_float(0x7fc00000u)
 
+// the first n of 16 bytes, 0 behind them
+__device__ __forceinline__ u32x4 first_bytes(u32x4 v, int n) {
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int k = n - 4 * x;
+    v[x] &= k >= 4 ? 0xffffffffu : k <= 0 ? 0u : (1u << k * 8) - 1;
+  }
+  return v;
+}
+// A page's scores s (times `by` to the base 2; of the entries from `from` on) into weights pf, their sum l and reference m; o follows m.
+// all: every row sees the whole page, else up to pos, above low or below sinks.
+template <int DH>
+__device__ __forceinline__ void softmax_step(f32x4 (&s)[4], f32x4 (&o)[DH / 16], float& m, float& l, bf16x8 (&pf)[2], float by, bool all,
+                                             int from, int pos, int low, int sinks) {
+  if (!all) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int e = from + 4 * t + x;
+        s[t][x] = (e <= pos) & ((e > low) | (e < sinks)) ? s[t][x] : -INFINITY;
+      }
+  }
+  float mx = -INFINITY;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[t][x]);
+  mx = groups_max(mx) * by;
+  if (__any(mx > m + LAG)) {                       // maxima settle after a few pages
+    asm volatile("" ::: "memory");                 // and what is to do then stays here
+    const float m_new = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    l *= corr;
+#pragma unroll
+    for (int d = 0; d < DH / 16; ++d) o[d] *= corr;
+  }
+  // the product with the scale in one rounding with the difference, unless its own rounding, left in the largest score, would count
+  float mul = by, less = m;
+  if (__any(fabsf(less) > FAR)) {
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[t][x] = difference(s[t][x], by, less);
+    mul = 1.f, less = 0.f;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float v = __builtin_amdgcn_exp2f(fmaf(s[t][x], mul, -less));
+      sum += v;
+      pf[t >> 1][(t & 1) * 4 + x] = (__bf16)v;
+    }
+  l += sum;
+}
+// a row's result, or its part: 4 elements of every 16 in this lane
+template <int DH>
+__device__ __forceinline__ void store_rows(const AttendArgs& a, const f32x4 (&o)[DH / 16], float m, float l, int pos, int split, size_t row_at, int g) {
+  if (a.splits == 1) {
+    const bool empty = pos < 0;
+    const float inv = empty ? 0.f : 1.f / l;
+#pragma unroll
+    for (int d = 0; d < DH / 16; ++d) {
+      bf16 b[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) b[x] = __float2bfloat16(o[d][x] * inv);
+      *reinterpret_cast<uint2*>(a.out + row_at * DH + d * 16 + g * 4) = *reinterpret_cast<const uint2*>(b);
+    }
+    if (a.lse && g == 0) a.lse[row_at] = empty ? -INFINITY : (m + __log2f(l)) * LN2;
+  } else {
+    const size_t at = (size_t)split * a.n_rows * a.n_heads + row_at;
+#pragma unroll
+    for (int d = 0; d < DH / 16; ++d) *reinterpret_cast<f32x4*>(a.part + at * DH + d * 16 + g * 4) = o[d];
+    if (g == 0) a.part_ml[at] = make_float2(pos < 0 ? -INFINITY : m, l);       // -inf: the row sees nothing
+  }
+}
+
+// Few rows of a KV head: the codes go to registers as operands, RT tiles of 16 rows share them in a wave.  The waves of a workgroup have
+// row_waves sets of rows and take pages in turn.
 #define FEW_WAVES 4
 template <int DH, int RT>
-__global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCache c, AttendArgs a) {
+__global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_kernel(QuantCache c, AttendArgs a) {
   constexpr int KS = DH / 32, DT = DH / 16;
   __shared__ f32x4 osh[FEW_WAVES - 1][RT][DT][64];
   __shared__ float2 mlsh[FEW_WAVES][RT][16];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   const unsigned parts = c.n_kv_heads * a.splits, part = blockIdx.x % parts;
-  const int h = part % c.n_kv_heads, split = part / c.n_kv_heads;
-  const int G = a.G, tile_rows = 16 * RT * a.row_waves;
+  const int h = part % c.n_kv_heads, split = part / c.n_kv_heads, G = a.G, tile_rows = 16 * RT * a.row_waves;
   Span sp = find_span(c, a.rows, a.n_rows, blockIdx.x / parts, [&](int M) { return (M * G + tile_rows - 1) / tile_rows; });
   sp.s = __builtin_amdgcn_readfirstlane(sp.s);
   if (sp.s < 0) return;
   sp.t = __builtin_amdgcn_readfirstlane(sp.t), sp.row = __builtin_amdgcn_readfirstlane(sp.row), sp.M = __builtin_amdgcn_readfirstlane(sp.M);
-  const int capacity = c.max_pages * PAGE, given = __builtin_amdgcn_readfirstlane(sp.len);
-  const bool beyond = given > capacity;              // nothing is read; the rows become NaN
+  const int given = __builtin_amdgcn_readfirstlane(sp.len);
+  const bool beyond = given > c.max_pages * PAGE;    // nothing is read; the rows become NaN
   const int len = max(given, 0), first = len - sp.M, R = sp.M * G;
   const int phases = FEW_WAVES / a.row_waves, rw = w % a.row_waves, phase = w / a.row_waves;
-  const int wg0 = sp.t * tile_rows, wg_last = min(wg0 + tile_rows, R) - 1;
-  const int r0 = wg0 + rw * 16 * RT, r_last = min(r0 + 16 * RT, R) - 1;      // r_last < r0: a wave without rows
+  const int wg0 = sp.t * tile_rows, wg_last = min(wg0 + tile_rows, R) - 1, r0 = wg0 + rw * 16 * RT, r_last = min(r0 + 16 * RT, R) - 1;
   const Seen seen = seen_pages(first + wg0 / G, beyond ? -1 : first + wg_last / G, a.window, a.sinks);
-  const int per = (seen.n + a.splits - 1) / a.splits, i0 = split * per, i1 = min(i0 + per, seen.n);
-  const int see_all = first + r0 / G;                                         // entries up to here are seen by all of the wave's rows
-  const int low_all = a.window ? first + max(r_last, 0) / G - a.window + 1 : 0;
+  const int per = (seen.n + a.splits - 1) / a.splits, i0 = split * per + phase;
+  const int n = r0 < R ? max(0, (min(split * per + per, seen.n) - i0 + phases - 1) / phases) : 0;         // pages of this wave
+  const int see_all = first + r0 / G, low_all = a.window ? first + max(r_last, 0) / G - a.window + 1 : 0;
 
   int pos[RT];
-  bool valid[RT];
-  size_t row_at[RT];                                                          // (row, head), counted through
+  size_t row_at[RT];                                 // (row, head), counted through
   bf16x8 qf[RT][KS];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int r = r0 + rt * 16 + r16;
-    valid[rt] = r < R;
-    const int tok = valid[rt] ? r / G : 0, hq = h * G + (valid[rt] ? r % G : 0);
-    pos[rt] = valid[rt] ? first + tok : -1;
+    const bool valid = r < R;
+    const int tok = valid ? r / G : 0, hq = h * G + (valid ? r % G : 0);
+    pos[rt] = valid ? first + tok : -1;
     row_at[rt] = (size_t)(sp.row + tok) * a.n_heads + hq;
-    const bf16* q = a.q + (size_t)(sp.row + tok) * a.ldq + (size_t)hq * DH + g * 16;
 #pragma unroll
-    for (int j = 0; j < KS; ++j) {
-      u32x4 x = {0u, 0u, 0u, 0u};
-      if (valid[rt]) x = *reinterpret_cast<const u32x4*>(q + (j >> 1) * 64 + (j & 1) * 8);
-      qf[rt][j] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int j = 0; j < KS; ++j)
+      qf[rt][j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(a.q + (size_t)(sp.row + tok) * a.ldq + (size_t)hq * DH + g * 16 + (j >> 1) * 64 + (j & 1) * 8));
   }
   float m[RT], l[RT];
   f32x4 o[RT][DT];
@@ -453,21 +528,20 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  PageList pages(c, sp.s, seen, h, i0 + phase, phases);
-  const int mine = max(0, (i1 - i0 - phase + phases - 1) / phases);           // pages of this wave
+  PageList pages(c, sp.s, seen, h, i0, phases);
   u32x4 kd[4][DH / 64], vd[DT];
   float ks = 0.f, vs = 0.f;
   int id = -1;
-  if (mine > 0) {
-    pages.fetch(0);                            // the first codes are asked for behind the scales, and waited for with them
+  if (n > 0) {
+    pages.fetch(0);                                  // the first codes are asked for behind the scales, and waited for with them
     load_keys<DH>(c, kd, pages.first_id(), h, lane);
     load_values<DH>(c, vd, pages.first_id(), h, lane);
     pages.settle();
     id = pages.get(0, &ks, &vs);
   }
-  for (int i = 0; i < mine; ++i) {
-    const int e0 = seen.page(i0 + phase + i * phases) * PAGE;
-    const bool there = id >= 0, more = i + 1 < mine;
+  for (int i = 0; i < n; ++i) {
+    const int e0 = seen.page(i0 + i * phases) * PAGE;
+    const bool there = id >= 0, more = i + 1 < n;
     const float by = there ? ks * a.scale_log2e : NAN32, vscale = there ? vs : 0.f;     // no such page: whoever sees it becomes NaN
     if (more) id = pages.get(i + 1, &ks, &vs);
     f32x4 s[RT][4];
@@ -483,68 +557,16 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
       }
     }
     if (more) load_keys<DH>(c, kd, id, h, lane);
-    if (!(e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks))) {
-      const int from = e0 + 16 * g;
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const int low = a.window ? pos[rt] - a.window : INT_MIN;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int e = from + 4 * t + x;
-            s[rt][t][x] = (e <= pos[rt]) & ((e > low) | (e < a.sinks)) ? s[rt][t][x] : -INFINITY;
-          }
-      }
-    }
+    const bool all = e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks);
     bf16x8 pf[RT][2];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float mx = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) mx = fmaxf(mx, s[rt][t][x]);
-      mx = groups_max(mx) * by;
-      if (__any(mx > m[rt] + LAG)) {             // maxima settle after a few pages
-        asm volatile("" ::: "memory");           // and what is to do then stays here
-        const float m_new = fmaxf(m[rt], mx), corr = __builtin_amdgcn_exp2f(m[rt] - m_new);
-        m[rt] = m_new;
-        l[rt] *= corr;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[rt][d] *= corr;
-      }
-      // the product with the scale in one rounding with the difference, unless its own rounding, left in the largest score, would count
-      float mul = by, less = m[rt];
-      if (__any(fabsf(less) > FAR)) {
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) s[rt][t][x] = difference(s[rt][t][x], by, less);
-        mul = 1.f, less = 0.f;
-      }
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float v = __builtin_amdgcn_exp2f(fmaf(s[rt][t][x], mul, -less));
-          sum += v;
-          pf[rt][t >> 1][(t & 1) * 4 + x] = (__bf16)v;
-        }
-      l[rt] += sum;
-    }
+    for (int rt = 0; rt < RT; ++rt)
+      softmax_step<DH>(s[rt], o[rt], m[rt], l[rt], pf[rt], by, all, e0 + 16 * g, pos[rt], a.window ? pos[rt] - a.window : INT_MIN, a.sinks);
     // entries behind the last one, or of no page, may hold anything: 0 times a NaN would be one
-    const int live = there ? min(len - e0, PAGE) - 16 * g : 0;
     if (!there || e0 + PAGE > len) {
+      const int live = there ? min(len - e0, PAGE) - 16 * g : 0;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int n = live - 4 * x;
-        const unsigned keep = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << n * 8) - 1;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) vd[d][x] &= keep;
-      }
+      for (int d = 0; d < DT; ++d) vd[d] = first_bytes(vd[d], live);
     }
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -556,7 +578,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
       }
     if (more) load_values<DH>(c, vd, id, h, lane);
   }
-  // the waves of a row tile together
+  // the waves of a set of rows together
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     l[rt] = groups_sum(l[rt]);
@@ -565,18 +587,14 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
   __syncthreads();
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    float top = NONE;
-    for (int x = 0; x < phases; ++x) top = fmaxf(top, mlsh[x * a.row_waves + rw][rt][r16].x);
+    float top = NONE, sum = 0.f;
+    for (int x = rw; x < FEW_WAVES; x += a.row_waves) top = fmaxf(top, mlsh[x][rt][r16].x);
+    for (int x = rw; x < FEW_WAVES; x += a.row_waves) sum += mlsh[x][rt][r16].y * __builtin_amdgcn_exp2f(mlsh[x][rt][r16].x - top);
     const float f = __builtin_amdgcn_exp2f(m[rt] - top);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       o[rt][d] *= f;
       if (phase) osh[w - a.row_waves][rt][d][lane] = o[rt][d];
-    }
-    float sum = 0.f;
-    for (int x = 0; x < phases; ++x) {
-      const float2 ml = mlsh[x * a.row_waves + rw][rt][r16];
-      sum += ml.y * __builtin_amdgcn_exp2f(ml.x - top);
     }
     m[rt] = top, l[rt] = sum;
   }
@@ -584,28 +602,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 2) void attend_few_kernel(QuantCach
   if (phase) return;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    for (int x = 1; x < phases; ++x)
+    for (int x = rw; x < FEW_WAVES - a.row_waves; x += a.row_waves)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[rt][d] += osh[(x - 1) * a.row_waves + rw][rt][d][lane];
-    if (!valid[rt]) continue;
-    if (beyond) l[rt] = __uint_as_float(0x7fc00000u);
-    if (a.splits == 1) {
-      const bool empty = pos[rt] < 0;
-      const float inv = empty ? 0.f : 1.f / l[rt];
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        bf16 b[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) b[x] = __float2bfloat16(o[rt][d][x] * inv);
-        *reinterpret_cast<uint2*>(a.out + row_at[rt] * DH + d * 16 + g * 4) = *reinterpret_cast<const uint2*>(b);
-      }
-      if (a.lse && g == 0) a.lse[row_at[rt]] = empty ? -INFINITY : (m[rt] + __log2f(l[rt])) * LN2;
-    } else {
-      const size_t at = (size_t)split * a.n_rows * a.n_heads + row_at[rt];
-#pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(a.part + at * DH + d * 16 + g * 4) = o[rt][d];
-      if (g == 0) a.part_ml[at] = make_float2(pos[rt] < 0 ? -INFINITY : m[rt], l[rt]);      // -inf: the row sees nothing
-    }
+      for (int d = 0; d < DT; ++d) o[rt][d] += osh[x][rt][d][lane];
+    if (r0 + rt * 16 + r16 < R) store_rows<DH>(a, o[rt], m[rt], beyond ? NAN32 : l[rt], pos[rt], split, row_at[rt], g);
   }
 }
 
@@ -684,12 +684,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
     if (!has_v) return;
     const int e0 = seen.page(i0 + i) * PAGE;
     if (p.id < 0 || e0 + PAGE > len) {         // entries behind the last one, or of no page, may hold anything: 0 times a NaN would be one
-      const int live = p.id >= 0 ? min(len - e0, PAGE) - 16 * vj : 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int k = live - 4 * x;
-        p.v[x] &= k >= 4 ? 0xffffffffu : k <= 0 ? 0u : (1u << k * 8) - 1;
-      }
+      p.v = first_bytes(p.v, p.id >= 0 ? min(len - e0, PAGE) - 16 * vj : 0);
     }
     const float scale = p.id >= 0 ? p.vs : 0.f;
     vsh[to][vto] = __builtin_bit_cast(u32x4, to_bf16x8(p.v[0], p.v[1], scale));
@@ -1119,10 +1114,12 @@ __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs 
 }
 
 // ---- eviction -----------------------------------------------------------------------------------------------------------------
-// One workgroup per sequence and head finds the weight of the last entry that is kept, eight bits of an ordered key at a time, and
-// lists the entries that are kept in their order; then a workgroup per page of 64 of them moves their codes.
+// One workgroup per sequence and head finds the weight of the last entry that is kept, 11 bits of an ordered key at a time (the first
+// ones are sign, exponent and two more, so that few entries of a wave meet in a counter), and lists the entries that are kept in their
+// order; then a workgroup per page of 64 of them moves their codes.  A wave has a stretch of entries, in registers where that is up to 1024.
 #define SELECT_THREADS 1024
 #define SELECT_WAVES (SELECT_THREADS / 64)
+#define SELECT_KEYS 16
 
 // larger weights have larger keys, equal ones the same; a NaN counts as the least
 __device__ __forceinline__ unsigned weight_key(float w) {
@@ -1131,10 +1128,10 @@ __device__ __forceinline__ unsigned weight_key(float w) {
 }
 
 __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(QuantCache c, EvictArgs a) {
-  __shared__ int hist[256];
+  __shared__ int hist[2048];
   __shared__ int found[2];
   __shared__ int counts[SELECT_WAVES][2];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = blockIdx.x, s = blockIdx.y;
   const int given = c.len[s], len = given > c.max_pages * PAGE ? 0 : max(given, 0);
   const float* weight = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw;
@@ -1149,75 +1146,86 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(QuantCache
   }
   const int lo = a.sinks, hi = len - a.recent;                  // between them by weight
   int want = a.budget - a.sinks - a.recent;                     // so many of them, fewer than there are
-  unsigned key = 0, mask = 0;                                   // the bits of the last kept key that are known
-  if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int i = lo + tid; i < hi; i += SELECT_THREADS) {
-        const unsigned k = weight_key(weight[i]);
-        if ((k & mask) == key) atomicAdd(&hist[k >> shift & 255u], 1);
-      }
-      __syncthreads();
-      if (w == 0) {                                             // 4 digits a lane, from the largest down
-        int four[4], mine = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) four[j] = hist[255 - (lane * 4 + j)], mine += four[j];
-        int upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-          const int o = __shfl_up(upto, d);
-          upto += lane >= d ? o : 0;
-        }
-        int before = upto - mine;
-        if (before < want && upto >= want) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (before < want && before + four[j] >= want) found[0] = 255 - (lane * 4 + j), found[1] = want - before;
-            before += four[j];
-          }
-        }
-      }
-      __syncthreads();
-      key |= (unsigned)found[0] << shift;
-      mask |= 255u << shift;
-      want = found[1];                                          // so many of those with this digit
-      __syncthreads();
-    }
-  } else key = 0xffffffffu;                                     // above every key (a NaN's bits do not reach it)
-  // every wave has a stretch of entries; larger keys are kept, and the first `want` equal ones
   const int stretch = ((hi - lo + SELECT_WAVES - 1) / SELECT_WAVES + 63) / 64 * 64;
   const int from = lo + w * stretch, to = min(from + stretch, hi);
-  int more = 0, equal = 0;
-  for (int i = from; i < to; i += 64) {
-    const unsigned k = i + lane < to ? weight_key(weight[i + lane]) : 0u;
-    more += __popcll(__ballot(i + lane < to && k > key));
-    equal += __popcll(__ballot(i + lane < to && k == key));
+  const bool fits = stretch <= 64 * SELECT_KEYS;
+  unsigned keys[SELECT_KEYS];
+  if (fits) {
+    float v[SELECT_KEYS];
+#pragma unroll
+    for (int x = 0; x < SELECT_KEYS; ++x) {
+      const int i = from + x * 64 + lane;
+      v[x] = i < to ? weight[i] : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < SELECT_KEYS; ++x) keys[x] = weight_key(v[x]);
   }
+  // f(entry, key, whether there is one) for the wave's entries, 64 at a time in their order
+  auto each = [&](auto f) {
+    if (fits) {
+#pragma unroll
+      for (int x = 0; x < SELECT_KEYS; ++x) {
+        const int i = from + x * 64 + lane;
+        if (from + x * 64 < to) f(i, keys[x], i < to);
+      }
+    } else {
+      for (int i = from + lane; i - lane < to; i += 64) f(i, i < to ? weight_key(weight[i]) : 0u, i < to);
+    }
+  };
+  unsigned key = 0, mask = 0;                                   // the bits of the last kept key that are known
+  if (want > 0) {
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const unsigned bits = pass == 2 ? 1023u : 2047u;
+      hist[tid] = hist[tid + SELECT_THREADS] = 0;
+      __syncthreads();
+      each([&](int, unsigned k, bool in) {
+        if (in && (k & mask) == key) atomicAdd(&hist[k >> shift & bits], 1);
+      });
+      __syncthreads();
+      const int first = hist[2047 - 2 * tid], second = hist[2046 - 2 * tid];       // from the largest digit down
+      const int upto = lanes_upto(first + second);
+      if (lane == 63) counts[w][0] = upto;
+      __syncthreads();
+      const int waves = lanes_upto(counts[lane % SELECT_WAVES][0]);             // of the waves up to lane's in the first row of lanes
+      const int before = upto - first - second + (w ? __builtin_amdgcn_readlane(waves, max(w - 1, 0)) : 0);
+      if (before < want && before + first >= want) found[0] = 2047 - 2 * tid, found[1] = want - before;
+      else if (before + first < want && before + first + second >= want) found[0] = 2046 - 2 * tid, found[1] = want - before - first;
+      __syncthreads();
+      key |= (unsigned)found[0] << shift;
+      mask |= bits << shift;
+      want = found[1];                                          // so many of those with this digit
+    }
+  } else key = 0xffffffffu;                                     // above every key (a NaN's bits do not reach it)
+  // larger keys are kept, and the first `want` equal ones
+  int more = 0, equal = 0;
+  each([&](int, unsigned k, bool in) {
+    more += __popcll(__ballot(in && k > key));
+    equal += __popcll(__ballot(in && k == key));
+  });
+  __syncthreads();                                              // counts have been read
   if (lane == 0) counts[w][0] = more, counts[w][1] = equal;
   __syncthreads();
   int at = a.sinks, equals = 0;                                 // places and equal ones in front of this wave
-  for (int x = 0; x < w; ++x) {
-    const int take = min(counts[x][1], max(want - equals, 0));
-    at += counts[x][0] + take;
-    equals += counts[x][1];
+  {
+    const int m = lanes_upto(counts[lane % SELECT_WAVES][0]), e = lanes_upto(counts[lane % SELECT_WAVES][1]);
+    equals = w ? __builtin_amdgcn_readlane(e, max(w - 1, 0)) : 0;
+    at += (w ? __builtin_amdgcn_readlane(m, max(w - 1, 0)) : 0) + min(equals, max(want, 0));
   }
   const unsigned long long below = (1ull << lane) - 1;
-  for (int i = from; i < to; i += 64) {
-    const bool in = i + lane < to;
-    const float v = in ? weight[i + lane] : 0.f;
-    const unsigned k = weight_key(v);
+  each([&](int i, unsigned k, bool in) {
     const unsigned long long eq = __ballot(in && k == key);
     const bool keep = in && (k > key || (k == key && equals + __popcll(eq & below) < want));
     const unsigned long long all = __ballot(keep);
     if (keep) {
       const int to_at = at + __popcll(all & below);
-      kept[to_at] = i + lane;
-      to_weight[to_at] = v;
+      kept[to_at] = i;
+      to_weight[to_at] = weight[i];
     }
     at += __popcll(all);
     equals += __popcll(eq);
-  }
+  });
   for (int i = tid; i < a.sinks; i += SELECT_THREADS) kept[i] = i, to_weight[i] = weight[i];
   for (int i = tid; i < a.recent; i += SELECT_THREADS) kept[a.budget - a.recent + i] = hi + i, to_weight[a.budget - a.recent + i] = weight[hi + i];
 }
@@ -1333,8 +1341,7 @@ static long long most_tiles(const QuantCache& c, bool ragged, int n_rows, int G,
   return (long long)c.n_seqs * (((long long)(n_rows / c.n_seqs) * G + tile - 1) / tile);
 }
 struct AttendPlan {
-  bool many;
-  int row_tiles;    // of 16 rows per wave
+  int row_tiles;    // of 16 rows in a wave; 0: many rows
   int row_waves;    // waves of a workgroup that have rows of their own; the others take other pages of theirs
   int splits;
   long long tiles;
@@ -1343,30 +1350,26 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
   AttendPlan p;
   const int G = n_heads / c.n_kv_heads;
   const long long rows = (long long)((n_rows + c.n_seqs - 1) / c.n_seqs) * G;      // of a sequence, in the mean
-  p.many = rows > 160;
-  if (p.many) {
-    p.tiles = most_tiles(c, ragged, n_rows, G, MANY_ROWS);
-    const int pages = most_pages(c, (MANY_ROWS + G - 1) / G, window, sinks);
-    const long long groups = p.tiles * c.n_kv_heads;
-    p.splits = (int)max(1ll, min(min(spec_num_cu() / groups, (long long)pages / 8), (long long)MERGE_PARTS));
-    return p;
-  }
-  p.row_tiles = rows > 16 ? 2 : 1;
+  p.row_tiles = rows > 160 ? 0 : rows > 16 ? 2 : 1;
   p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
-  const int tile = 16 * p.row_tiles * p.row_waves;
+  const int tile = p.row_tiles ? 16 * p.row_tiles * p.row_waves : MANY_ROWS;
   p.tiles = most_tiles(c, ragged, n_rows, G, tile);
-  const int pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
-  const long long groups = p.tiles * c.n_kv_heads, want = 2ll * spec_num_cu();
-  p.splits = (int)max(1ll, min(min((want + groups - 1) / groups, (long long)((pages + phases - 1) / phases)), (long long)MERGE_PARTS));
+  const long long groups = p.tiles * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
+  const long long most = p.row_tiles ? (pages + phases - 1) / phases : pages / 8;
+  const long long want = p.row_tiles ? (2ll * spec_num_cu() + groups - 1) / groups : spec_num_cu() / groups;
+  p.splits = (int)max(1ll, min(min(want, most), (long long)MERGE_PARTS));
   return p;
 }
 size_t attend_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   const AttendPlan p = attend_plan(c, ragged, n_rows, n_heads, window, sinks);
   return p.splits == 1 ? 0 : (size_t)p.splits * n_rows * n_heads * (c.head_dim + 2) * sizeof(float);
 }
-template <int DH, int RT>
-static void launch_few(const QuantCache& c, const AttendArgs& a, long long tiles, hipStream_t st) {
-  attend_few_kernel<DH, RT><<<(unsigned)(tiles * c.n_kv_heads * a.splits), FEW_WAVES * 64, 0, st>>>(c, a);
+template <int DH>
+static void launch_attend(const QuantCache& c, const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+  const unsigned groups = (unsigned)(p.tiles * c.n_kv_heads * p.splits);
+  if (p.row_tiles == 1) attend_few_kernel<DH, 1><<<groups, FEW_WAVES * 64, 0, st>>>(c, a);
+  else if (p.row_tiles == 2) attend_few_kernel<DH, 2><<<groups, FEW_WAVES * 64, 0, st>>>(c, a);
+  else attend_many_kernel<DH><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
 }
 hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hipStream_t st) {
   const AttendPlan p = attend_plan(c, a.rows != nullptr, a.n_rows, a.n_heads, a.window, a.sinks);
@@ -1375,17 +1378,8 @@ hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hi
   const size_t all = (size_t)a.n_rows * a.n_heads;
   a.part = (float*)work;
   a.part_ml = (float2*)(a.part + (size_t)p.splits * all * c.head_dim);
-  if (p.many) {
-    const unsigned groups = (unsigned)(p.tiles * c.n_kv_heads * p.splits);
-    if (c.head_dim == 128) attend_many_kernel<128><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
-    else attend_many_kernel<64><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
-  } else if (c.head_dim == 128) {
-    if (p.row_tiles == 1) launch_few<128, 1>(c, a, p.tiles, st);
-    else launch_few<128, 2>(c, a, p.tiles, st);
-  } else {
-    if (p.row_tiles == 1) launch_few<64, 1>(c, a, p.tiles, st);
-    else launch_few<64, 2>(c, a, p.tiles, st);
-  }
+  if (c.head_dim == 128) launch_attend<128>(c, a, p, st);
+  else launch_attend<64>(c, a, p, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const bool wide = p.splits > 16 && all <= (1u << 16);
