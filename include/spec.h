@@ -315,10 +315,10 @@ int spec_gemm_quant(void* out_dev, int out_type, const void* x_dev, const float*
  * rows become NaN; so do rows that see an entry of a page id that is none of 0 .. n_pages - 1 (pages that no row sees, as behind a
  * window, may have any id); rows in front of entry 0 see nothing: 0, and -inf as the logarithm of their sum.
  * n_heads query heads share n_kv_heads evenly; head_dim is 64 or 128; n_rows * n_heads <= 2^26, n_seqs <= 65535,
- * n_seqs * n_kv_heads <= 2^20.  Every call is asynchronous on `stream`, allocates nothing and can be captured; its results do not
+ * n_seqs * n_kv_heads <= 2^20, max_pages * n_kv_heads <= 2^24.  Every call is asynchronous on `stream`, allocates nothing and can be captured; its results do not
  * depend on the order in which anything runs.  What a call writes must not overlap what it reads. */
 #define SPEC_CACHE_HEADS_MAX 4096
-#define SPEC_CACHE_PAGES_MAX (1 << 24)
+#define SPEC_CACHE_PAGES_MAX (1 << 20)
 typedef struct {
   void* k;              /* e4m3 [n_pages][n_kv_heads][64][head_dim], 16-byte aligned */
   void* v;              /* e4m3 [n_pages][n_kv_heads][head_dim][64]: entries of an element are neighbours */

@@ -11,6 +11,8 @@
 // own, len - M + j, and of those, with a window, the last `window` and the first `sinks`.
 #include <limits.h>
 
+#include <type_traits>
+
 #include "spec_internal.h"
 
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
@@ -983,17 +985,18 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
   }
 }
 
-// Many rows: a wave keeps the 64 keys of a page as operands and the workgroup goes over tiles of 32 rows, whose queries, logarithms and
+// Many rows: a wave keeps the 64 keys of a page as operands and the workgroup goes over tiles of 64 rows, whose queries, logarithms and
 // entries pass through LDS.  S = Q K^T, 32 x 32 x 16: a lane's scores belong to one entry.  The tiles that see a group of pages are dealt to
 // `slices` workgroups; sums of slices are added in their order.
 template <int DH>
 __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCache c, WeighArgs a) {
-  constexpr int KS = DH / 16, QB = 66, CH = DH / 8, LOADS = 32 * CH / (WEIGH_WAVES * 64);
-  __shared__ u32x4 qsh[2][KS * QB];
-  __shared__ __align__(16) float lsh[2][32];
-  __shared__ __align__(16) int psh[2][32];
+  constexpr int KS = DH / 16, QB = 66, CH = DH / 8, LOADS = 64 * CH / (WEIGH_WAVES * 64);
+  __shared__ u32x4 qsh[2][2 * KS * QB];
+  __shared__ __align__(16) float lsh[2][64];
+  __shared__ __align__(16) int psh[2][64];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
-  const int h = blockIdx.y, s = blockIdx.z, G = a.G, group = blockIdx.x / a.slices, slice = blockIdx.x % a.slices;
+  // pages that most rows see first
+  const int h = blockIdx.x % c.n_kv_heads, s = blockIdx.y, G = a.G, group = blockIdx.x / c.n_kv_heads / a.slices, slice = blockIdx.x / c.n_kv_heads % a.slices;
   const Rows rs = rows_of(c, a.rows, a.n_rows, s, G);
   if (rs.none) return;
   const int first = rs.first, len = rs.len, R = rs.R;
@@ -1017,23 +1020,38 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   const float by = there ? c.scale[block * 2] * a.scale_log2e : NAN32;             // no such page: whoever sees it becomes NaN
   // tiles with rows that see any of the group's pages
   const int lo_e = seen.page(group * WEIGH_WAVES) * PAGE, hi_e = seen.page(min(group * WEIGH_WAVES + WEIGH_WAVES, seen.n) - 1) * PAGE + PAGE - 1;
-  const int tiles = (R + 31) / 32, tile0 = max(0, lo_e - first) * G / 32;
+  const int tiles = (R + 63) / 64, tile0 = max(0, lo_e - first) * G / 64;
   int tile1 = tiles;
-  if (a.window && lo_e >= a.sinks && hi_e + a.window - first < rs.M) tile1 = min(tiles, max(0, hi_e + a.window - first) * G / 32 + 1);
+  if (a.window && lo_e >= a.sinks && hi_e + a.window - first < rs.M) tile1 = min(tiles, max(0, hi_e + a.window - first) * G / 64 + 1);
   const int all_tiles = max(0, tile1 - tile0), t0 = tile0 + (int)((long long)slice * all_tiles / a.slices), t1 = tile0 + (int)((long long)(slice + 1) * all_tiles / a.slices);
+  auto token = [&](int r) { return (int)((unsigned long long)(unsigned)r * a.by_group >> 38); };      // r / G
+  // rows that see all of this wave's page
+  const int see_from = max(0, e0 + PAGE - 1 - first) * G;
+  const int see_to = a.window && e0 + PAGE > a.sinks ? (int)min((long long)R, max(0ll, (long long)e0 + a.window - first) * G) : R;
   u32x4 raw[LOADS];
+  const bf16* from[LOADS];
   float lse = 0.f;
   int pos = -1;
+  // where a tile's rows stand: 64 rows further on where they are whole tokens, else worked out anew
+  const bool whole = 64 % G == 0;
+  const size_t on = (size_t)(64 / min(G, 64)) * a.ldq;
   auto load = [&](int tile) {
+    if (whole && tile > t0 && tile * 64 + 64 <= R) {
 #pragma unroll
-    for (int x = 0; x < LOADS; ++x) {
-      const int at = x * WEIGH_WAVES * 64 + tid, r = min(tile * 32 + at / CH, R - 1), tok = r / G;
-      raw[x] = *reinterpret_cast<const u32x4*>(a.q + (size_t)(rs.row + tok) * a.ldq + (size_t)(h * G + r % G) * DH + at % CH * 8);
+      for (int x = 0; x < LOADS; ++x) from[x] += on;
+    } else {
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        const int at = x * WEIGH_WAVES * 64 + tid, r = min(tile * 64 + at / CH, R - 1), tok = token(r);
+        from[x] = a.q + (size_t)(rs.row + tok) * a.ldq + (size_t)(h * G + r - tok * G) * DH + at % CH * 8;
+      }
     }
-    if (tid < 32) {
-      const int r = tile * 32 + tid, tok = min(r, R - 1) / G;
-      lse = a.lse[(size_t)(rs.row + tok) * a.n_heads + h * G + min(r, R - 1) % G] * LOG2E;
-      pos = r < R ? first + tok : -1;
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) raw[x] = *reinterpret_cast<const u32x4*>(from[x]);
+    if (tid < 64) {
+      const int r = min(tile * 64 + tid, R - 1), tok = token(r);
+      lse = a.lse[(size_t)(rs.row + tok) * a.n_heads + h * G + r - tok * G] * LOG2E;
+      pos = tile * 64 + tid < R ? first + tok : -1;
     }
   };
   auto put = [&](int to) {
@@ -1041,51 +1059,81 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
     for (int x = 0; x < LOADS; ++x) {
       // 8 elements: 32 j + 16 c + 8 b are those of step 2 j + b in the lanes of half c
       const int at = x * WEIGH_WAVES * 64 + tid, r = at / CH, ch = at % CH;
-      qsh[to][(ch / 4 * 2 + (ch & 1)) * QB + (ch >> 1 & 1) * 33 + r] = raw[x];
+      qsh[to][((r >> 5) * KS + ch / 4 * 2 + (ch & 1)) * QB + (ch >> 1 & 1) * 33 + (r & 31)] = raw[x];
     }
-    if (tid < 32) lsh[to][tid] = lse, psh[to][tid] = pos;
+    if (tid < 64) lsh[to][tid] = lse, psh[to][tid] = pos;
   };
-  float sum[2] = {0.f, 0.f};
-  if (t0 < t1) load(t0), put(0);
-  for (int tile = t0; tile < t1; ++tile) {
-    const int at = (tile - t0) & 1;
-    __syncthreads();                                           // this tile is there, and nobody reads the other place
-    if (tile + 1 < t1) load(tile + 1);
+  float sum[2][2] = {};
+  // 32 of the 64 rows: their scores, what they do not see, and their logarithms, which the tile's place will not keep
+  struct Part {
     f32x16 x[2];
-    x[0] = f32x16{}, x[1] = f32x16{};
-#pragma unroll
-    for (int j = 0; j < KS; ++j) {
-      const bf16x8 qf = __builtin_bit_cast(bf16x8, qsh[at][j * QB + half * 33 + r32]);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[t][j], x[t], 0, 0, 0);
-    }
-    const int p_lo = first + tile * 32 / G, p_hi = first + min(tile * 32 + 31, R - 1) / G;
-    const bool all = e0 + PAGE - 1 <= p_lo && (!a.window || e0 > p_hi - a.window || e0 + PAGE <= a.sinks) && tile * 32 + 32 <= R;
-    if (!all) {
-#pragma unroll
-      for (int y = 0; y < 16; ++y) {
-        const int p = psh[at][8 * (y >> 2) + 4 * half + (y & 3)], low = a.window ? p - a.window : INT_MIN;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const int e = e0 + t * 32 + r32;
-          x[t][y] = (e <= p) & ((e > low) | (e < a.sinks)) ? x[t][y] : -INFINITY;
-        }
-      }
-    }
+    float lse[16];
+  } p0, p1;
+  auto mask = [&](Part& p, int at, int r0) {
+    if (r0 >= see_from && r0 + 32 <= see_to) return;
 #pragma unroll
     for (int y = 0; y < 16; ++y) {
-      const float l = lsh[at][8 * (y >> 2) + 4 * half + (y & 3)];
+      const int pos = psh[at][(r0 & 32) + 8 * (y >> 2) + 4 * half + (y & 3)], low = a.window ? pos - a.window : INT_MIN;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) sum[t] += __builtin_amdgcn_exp2f(fmaf(x[t][y], by, -l));
+      for (int t = 0; t < 2; ++t) {
+        const int e = e0 + t * 32 + r32;
+        p.x[t][y] = (e <= pos) & ((e > low) | (e < a.sinks)) ? p.x[t][y] : -INFINITY;
+      }
     }
-    if (tile + 1 < t1) put(at ^ 1);
+  };
+  auto weights = [&](const Part& p, int y) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) sum[t][y & 1] += __builtin_amdgcn_exp2f(fmaf(p.x[t][y], by, -p.lse[y]));
+  };
+  // scores of `p`, and between their products the weights of `done`
+  auto scores = [&](Part& p, int at, int b, const Part& done, auto both) {
+    constexpr int AHEAD = 4;
+    bf16x8 qf[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) qf[j] = __builtin_bit_cast(bf16x8, qsh[at][(b * KS + j) * QB + half * 33 + r32]);
+    p.x[0] = f32x16{}, p.x[1] = f32x16{};
+#pragma unroll
+    for (int j = 0; j < KS; ++j) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) p.x[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[j % AHEAD], kf[t][j], p.x[t], 0, 0, 0);
+      if (j + AHEAD < KS) qf[j % AHEAD] = __builtin_bit_cast(bf16x8, qsh[at][(b * KS + j + AHEAD) * QB + half * 33 + r32]);
+      if (both.value) {
+#pragma unroll
+        for (int y = 0; y < 16; ++y)
+          if (y * KS / 16 == j) weights(done, y);
+      }
+      __builtin_amdgcn_sched_barrier(0);                       // left alone the products come first, one chain behind the other
+    }
+#pragma unroll
+    for (int y = 0; y < 16; ++y) p.lse[y] = lsh[at][b * 32 + 8 * (y >> 2) + 4 * half + (y & 3)];
+  };
+  if (t0 < t1) {
+    load(t0);
+    put(0);
+    if (t0 + 1 < t1) load(t0 + 1);
+    __syncthreads();
+    scores(p0, 0, 0, p1, std::false_type());
+    for (int tile = t0;; ++tile) {
+      const int at = (tile - t0) & 1;
+      mask(p0, at, tile * 64);
+      scores(p1, at, 1, p0, std::true_type());
+      mask(p1, at, tile * 64 + 32);
+      if (tile + 1 == t1) break;
+      put(at ^ 1);                                             // read last in front of the barrier before
+      if (tile + 2 < t1) load(tile + 2);
+      __syncthreads();
+      scores(p0, at ^ 1, 0, p1, std::true_type());
+    }
+#pragma unroll
+    for (int y = 0; y < 16; ++y) weights(p1, y);
   }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    auto o = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[t]), __float_as_uint(sum[t]), false, false);
-    sum[t] = __uint_as_float(o[0]) + __uint_as_float(o[1]);
+    const unsigned x = __float_as_uint(sum[t][0] + sum[t][1]);
+    auto o = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    sum[t][0] = __uint_as_float(o[0]) + __uint_as_float(o[1]);
   }
-  const float v = half ? sum[1] : sum[0];
+  const float v = half ? sum[1][0] : sum[0][0];
   const int e = e0 + lane;
   if (!has || e >= len) return;
   const size_t line = (size_t)s * c.n_kv_heads + h;
@@ -1422,16 +1470,17 @@ size_t weigh_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int 
 }
 template <int DH>
 static void launch_weigh(const QuantCache& c, const WeighArgs& a, const WeighPlan& p, hipStream_t st) {
-  const dim3 grid(p.groups * p.slices, c.n_kv_heads, c.n_seqs);
+  const dim3 grid(p.groups, c.n_kv_heads, c.n_seqs);
   if (p.row_tiles == 1) weigh_few_kernel<DH, 1><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
   else if (p.row_tiles == 2) weigh_few_kernel<DH, 2><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
   else if (p.row_tiles == 4) weigh_few_kernel<DH, 4><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
-  else weigh_many_kernel<DH><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
+  else weigh_many_kernel<DH><<<dim3((unsigned)p.groups * p.slices * c.n_kv_heads, c.n_seqs), WEIGH_WAVES * 64, 0, st>>>(c, a);
 }
 hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, void* work, hipStream_t st) {
   const WeighPlan p = weigh_plan(c, a.rows != nullptr, a.n_rows, a.n_heads, a.window, a.sinks);
   a.G = a.n_heads / c.n_kv_heads;
   a.slices = p.slices, a.part = (float*)work;
+  a.by_group = ((1ull << 38) + a.G - 1) / a.G;           // r * G < 2^38: (r * this) >> 38 is r / G
   if (c.head_dim == 128) launch_weigh<128>(c, a, p, st);
   else launch_weigh<64>(c, a, p, st);
   hipError_t e = hipGetLastError();

@@ -1542,8 +1542,8 @@ static int check_quant_cache(const spec_quant_cache* c, QuantCache* o) {
   if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > SPEC_CACHE_HEADS_MAX || c->n_seqs < 1 || c->n_seqs > 65535 ||
       (size_t)c->n_seqs * c->n_kv_heads > (1u << 20))
     FAIL(SPEC_E_INVAL, "need pages, 1 to %d heads, 1 to 65535 sequences and at most 2^20 of their heads", SPEC_CACHE_HEADS_MAX);
-  if (c->max_pages < 1 || c->max_pages > SPEC_CACHE_PAGES_MAX || c->table_ld < c->max_pages)
-    FAIL(SPEC_E_INVAL, "need 1 to %d pages a sequence and a table at least as wide", SPEC_CACHE_PAGES_MAX);
+  if (c->max_pages < 1 || c->max_pages > SPEC_CACHE_PAGES_MAX || (size_t)c->max_pages * c->n_kv_heads > (1u << 24) || c->table_ld < c->max_pages)
+    FAIL(SPEC_E_INVAL, "need 1 to %d pages a sequence, at most 2^24 of their heads, and a table at least as wide", SPEC_CACHE_PAGES_MAX);
   if (off_by(c->k, 16) || off_by(c->v, 16) || off_by(c->scale, 8) || off_by(c->table, 4) || off_by(c->len, 4))
     FAIL(SPEC_E_INVAL, "misaligned cache");
   *o = {(uint8_t*)c->k, (uint8_t*)c->v, c->scale, c->table, c->len, c->n_pages, c->n_kv_heads, c->head_dim, c->n_seqs, c->max_pages, c->table_ld};
@@ -1677,7 +1677,7 @@ extern "C" int spec_weigh_quant(const spec_quant_cache* cache, const void* q, lo
              meet(lse, n * n_heads * 4, r.p, r.bytes) || meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, r.p, r.bytes);
   if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
   WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, lse, weight, (size_t)ldw,
-                 0, 0, nullptr};
+                 0, 0, 0, nullptr};
   HIPCHK(launch_weigh_quant(c, a, work, (hipStream_t)stream));
   return SPEC_OK;
 }

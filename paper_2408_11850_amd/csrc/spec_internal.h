@@ -246,6 +246,7 @@ struct WeighArgs {
   float* weight;
   size_t ldw;
   int G, slices;              // set by the launch ...
+  unsigned long long by_group;
   float* part;                // ... sums of slices [slices][n_seqs][n_kv_heads][64 max_pages]
 };
 struct EvictArgs {
