@@ -1384,10 +1384,22 @@ static int most_pages(const QuantCache& c, int rows_seen, int window, int sinks)
   const long long n = ((long long)window + rows_seen) / PAGE + 2 + (sinks + PAGE - 1) / PAGE;
   return (int)(n < c.max_pages ? n : c.max_pages);
 }
+// Tiles of `tile` rows: as many as there can be, and as many as there are where sequences have the same number of rows.
 static long long most_tiles(const QuantCache& c, bool ragged, int n_rows, int G, int tile) {
-  if (ragged) return (long long)n_rows * G / tile + c.n_seqs;
-  return (long long)c.n_seqs * (((long long)(n_rows / c.n_seqs) * G + tile - 1) / tile);
+  const long long each = ((long long)(n_rows / c.n_seqs) * G + tile - 1) / tile;
+  return ragged ? ((long long)n_rows * G + (long long)c.n_seqs * (tile - 1)) / tile : c.n_seqs * each;
 }
+static long long mean_tiles(const QuantCache& c, int n_rows, int G, int tile) {
+  return (long long)c.n_seqs * ((((long long)n_rows * G + c.n_seqs - 1) / c.n_seqs + tile - 1) / tile);
+}
+// Kernel and split of an attention, by the rows of a sequence in the mean, tiles and pages (us, back to back; 64 heads over 8 unless said).
+//   two tiles of 16 rows share a wave's codes where one each would be more than 12 waves a CU, one page a wave (one tile | two):
+//     64 rows of heads behind 1000 entries  11.1 | 13.5      8 sequences, 64 rows behind 4096   39.8 | 27.2      1, 64 behind 8192  20.3 | 18.9
+//   from 160 rows on, and 8 waves a CU, pages pass through LDS (registers | LDS):
+//     256 rows behind 1000   22.1 | 25.8 and 32 heads over 4  11.7 | 20.4      8 sequences, 256 behind 4096   70.0 | 57.0
+//   parts of a sequence so that every CU has a workgroup (one a CU | two):
+//     8 sequences, 64 rows behind 4096   27.0 | 28.6      64 rows behind 8192   18.9 | 23.9      windows of 8 requests   18.7 | 22.2
+//     against it  64 rows behind 131072   76.9 | 71.3
 struct AttendPlan {
   int row_tiles;    // of 16 rows in a wave; 0: many rows
   int row_waves;    // waves of a workgroup that have rows of their own; the others take other pages of theirs
@@ -1397,14 +1409,15 @@ struct AttendPlan {
 static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   AttendPlan p;
   const int G = n_heads / c.n_kv_heads;
-  const long long rows = (long long)((n_rows + c.n_seqs - 1) / c.n_seqs) * G;      // of a sequence, in the mean
-  p.row_tiles = rows > 160 ? 0 : rows > 16 ? 2 : 1;
+  const long long rows = ((long long)n_rows * G + c.n_seqs - 1) / c.n_seqs;      // of a sequence, in the mean
+  const long long waves = mean_tiles(c, n_rows, G, 16) * c.n_kv_heads * most_pages(c, (int)(rows / G) + 1, window, sinks);
+  p.row_tiles = rows > 160 && waves > 8ll * spec_num_cu() ? 0 : rows > 16 && waves > 12ll * spec_num_cu() ? 2 : 1;
   p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
   const int tile = p.row_tiles ? 16 * p.row_tiles * p.row_waves : MANY_ROWS;
   p.tiles = most_tiles(c, ragged, n_rows, G, tile);
-  const long long groups = p.tiles * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
+  const long long groups = mean_tiles(c, n_rows, G, tile) * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
   const long long most = p.row_tiles ? (pages + phases - 1) / phases : pages / 8;
-  const long long want = p.row_tiles ? (2ll * spec_num_cu() + groups - 1) / groups : spec_num_cu() / groups;
+  const long long want = p.row_tiles ? (spec_num_cu() + groups - 1) / groups : spec_num_cu() / groups;
   p.splits = (int)max(1ll, min(min(want, most), (long long)MERGE_PARTS));
   return p;
 }
