@@ -544,7 +544,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
   for (int i = 0; i < n; ++i) {
     const int e0 = seen.page(i0 + i * phases) * PAGE;
     const bool there = id >= 0, more = i + 1 < n;
-    const float by = there ? ks * a.scale_log2e : NAN32, vscale = there ? vs : 0.f;     // no such page: whoever sees it becomes NaN
+    const float by = (there ? ks : 1.f) * a.scale_log2e, vscale = there ? vs : 0.f;
     if (more) id = pages.get(i + 1, &ks, &vs);
     f32x4 s[RT][4];
 #pragma unroll
@@ -559,6 +559,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
       }
     }
     if (more) load_keys<DH>(c, kd, id, h, lane);
+    if (!there) {                                    // no such page: whoever sees it becomes NaN
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[rt][t] = f32x4{NAN32, NAN32, NAN32, NAN32};
+    }
     const bool all = e0 + PAGE - 1 <= see_all && (!a.window || e0 >= low_all || e0 + PAGE <= a.sinks);
     bf16x8 pf[RT][2];
 #pragma unroll
@@ -1017,7 +1023,14 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
       kf[t][j] = to_bf16x8(x[0], x[1], 1.f);
       kf[t][j + 1] = to_bf16x8(x[2], x[3], 1.f);
     }
-  const float by = there ? c.scale[block * 2] * a.scale_log2e : NAN32;             // no such page: whoever sees it becomes NaN
+  const float by = (there ? c.scale[block * 2] : 1.f) * a.scale_log2e;
+  if (!there) {                                                // no such page: whoever sees it becomes NaN
+    constexpr unsigned NANS = 0x7fc07fc0u;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < KS; ++j) kf[t][j] = __builtin_bit_cast(bf16x8, u32x4{NANS, NANS, NANS, NANS});
+  }
   // tiles with rows that see any of the group's pages
   const int lo_e = seen.page(group * WEIGH_WAVES) * PAGE, hi_e = seen.page(min(group * WEIGH_WAVES + WEIGH_WAVES, seen.n) - 1) * PAGE + PAGE - 1;
   const int tiles = (R + 63) / 64, tile0 = max(0, lo_e - first) * G / 64;

@@ -98,6 +98,16 @@ def test_a_page_that_is_none_makes_its_rows_nan(m):
     assert got[:m].isnan().all() and got[2 * m - 1].isnan().all()
 
 
+@pytest.mark.parametrize("heads,kv,m", [(2, 2, 7), (8, 2, 3), (8, 2, 20), (8, 1, 40), (4, 2, 150), (8, 1, 300)])
+def test_rows_beside_those_that_see_such_a_page(heads, kv, m):
+    """Rows of one tile of which some see the page: the others keep their results."""
+    def drop(c):
+        for s in range(len(c.length)):
+            c.table[s, int(c.length[s] - 1) // 64] = -1
+    got, _ = _run([64 * 5 + 1 + m // 2, 64 * 9 + 2], [m, min(m, 70)], heads, kv, 128, change=drop)
+    assert not got[:m - m // 2 - 1].isnan().any() and got[m - 1].isnan().all()
+
+
 @pytest.mark.parametrize("m", [1, 100])
 def test_lengths_beyond_the_table(m):
     def grow(c):

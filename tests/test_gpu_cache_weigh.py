@@ -83,6 +83,17 @@ def test_pages_and_lengths_that_are_none(m):
     _run([400], [m], 4, 2, 64, window=10, sinks=3, change=hidden) if m == 1 else None
 
 
+@pytest.mark.parametrize("m", [1, 5, 40, 200])
+def test_entries_of_a_page_that_is_none_that_no_row_sees(m):
+    """The window begins, and the first entries end, inside such pages: what is hidden there keeps its weight."""
+    def change(c):
+        first = 600 - m - 30 + 1
+        c.table[0, first // 64] = 10 ** 6
+        c.table[0, 0] = -5
+    _run([600], [m], 8, 2, 128, window=30, sinks=5, change=change)
+    _run([600], [m], 4, 4, 64, window=30, sinks=5, change=change)
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (100, 4)])
 @pytest.mark.parametrize("m", [1, 8, 200])
 def test_weights_of_an_attention_add_up(m, window, sinks):
