@@ -23,7 +23,7 @@ class Fp8Cache:
     table int32 [n_seqs][max_pages] (any row stride); length int32 [n_seqs], the entries of every sequence with the rows of the
     calls that follow.  All contiguous but the table's rows, on one GPU."""
 
-    __slots__ = ("k", "v", "scale", "table", "length", "device", "heads", "d", "n_seqs", "capacity", "desc", "ref")
+    __slots__ = ("k", "v", "scale", "table", "length", "device", "heads", "d", "n_seqs", "capacity", "desc", "ref", "sizes")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, scale: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
         need(k.is_cuda and k.dtype is E4M3 and k.dim() == 4 and k.shape[2] == PAGE_TOKENS and k.is_contiguous(),
@@ -44,6 +44,16 @@ class Fp8Cache:
         self.desc = QuantCacheDesc(k.data_ptr(), v.data_ptr(), scale.data_ptr(), table.data_ptr(), length.data_ptr(), n_pages, heads, d,
                                    table.shape[0], table.shape[1], ld)
         self.ref = C.byref(self.desc)
+        self.sizes = {}                                        # workspaces' sizes by what they depend on: asking takes 2 us
+
+    def _work(self, fn, start, n: int, heads: int, window: int, sinks: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+        key = (fn, start is None, n, heads, window, sinks)
+        size = self.sizes.get(key)
+        if size is None:
+            size = self.sizes[key] = fn(self.ref, start, n, heads, window, sinks)
+            if len(self.sizes) > 256:                          # prompts of ever other lengths
+                self.sizes.clear()
+        return like.new_empty(size, dtype=torch.uint8) if size else None
 
     def _rows(self, x: torch.Tensor, heads: int, name: str) -> int:
         """Row stride of [n][heads][d] on this cache's device."""
@@ -127,10 +137,9 @@ def attend_fp8(cache: Fp8Cache, q: torch.Tensor, rows: Optional[torch.Tensor] = 
     elif want_lse:
         lse = q.new_empty((n, heads), dtype=torch.float32)
     lib = load_library()
-    size = lib.spec_attend_quant_workspace_bytes(cache.ref, start, n, heads, window, sinks)
-    work = q.new_empty(size, dtype=torch.uint8) if size else None
+    work = cache._work(lib.spec_attend_quant_workspace_bytes, start, n, heads, window, sinks, q)
     call_on(cache.device, lib.spec_attend_quant, cache.ref, q.data_ptr(), ldq, start, n, heads, d ** -0.5 if scale is None else scale,
-            window, sinks, out.data_ptr(), lse.data_ptr() if lse is not None else None, work.data_ptr() if size else None)
+            window, sinks, out.data_ptr(), lse.data_ptr() if lse is not None else None, work.data_ptr() if work is not None else None)
     return out, lse
 
 
@@ -147,10 +156,9 @@ def weigh_fp8(cache: Fp8Cache, q: torch.Tensor, lse: torch.Tensor, weight: torch
     ldw, start = cache._weights(weight, cache.capacity, "weight"), cache._starts(rows)
     _int32(window, "window"), _int32(sinks, "sinks")
     lib = load_library()
-    size = lib.spec_weigh_quant_workspace_bytes(cache.ref, start, n, heads, window, sinks)
-    work = q.new_empty(size, dtype=torch.uint8) if size else None
+    work = cache._work(lib.spec_weigh_quant_workspace_bytes, start, n, heads, window, sinks, q)
     call_on(cache.device, lib.spec_weigh_quant, cache.ref, q.data_ptr(), ldq, lse.data_ptr(), start, n, heads,
-            d ** -0.5 if scale is None else scale, window, sinks, weight.data_ptr(), ldw, work.data_ptr() if size else None)
+            d ** -0.5 if scale is None else scale, window, sinks, weight.data_ptr(), ldw, work.data_ptr() if work is not None else None)
     return weight
 
 
