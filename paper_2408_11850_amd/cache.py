@@ -46,11 +46,12 @@ class Fp8Cache:
         self.ref = C.byref(self.desc)
         self.sizes = {}                                        # workspaces' sizes by what they depend on: asking takes 2 us
 
-    def _work(self, fn, start, n: int, heads: int, window: int, sinks: int, like: torch.Tensor) -> Optional[torch.Tensor]:
-        key = (fn, start is None, n, heads, window, sinks)
+    def _work(self, call: str, start, n: int, heads: int, window: int, sinks: int, like: torch.Tensor) -> Optional[torch.Tensor]:
+        key = (call, start is None, n, heads, window, sinks)
         size = self.sizes.get(key)
         if size is None:
-            size = self.sizes[key] = fn(self.ref, start, n, heads, window, sinks)
+            ask = getattr(load_library(), call + "_workspace_bytes")
+            size = self.sizes[key] = ask(self.ref, start, n, heads, window, sinks)
             if len(self.sizes) > 256:                          # prompts of ever other lengths
                 self.sizes.clear()
         return like.new_empty(size, dtype=torch.uint8) if size else None
@@ -137,7 +138,7 @@ def attend_fp8(cache: Fp8Cache, q: torch.Tensor, rows: Optional[torch.Tensor] = 
     elif want_lse:
         lse = q.new_empty((n, heads), dtype=torch.float32)
     lib = load_library()
-    work = cache._work(lib.spec_attend_quant_workspace_bytes, start, n, heads, window, sinks, q)
+    work = cache._work("spec_attend_quant", start, n, heads, window, sinks, q)
     call_on(cache.device, lib.spec_attend_quant, cache.ref, q.data_ptr(), ldq, start, n, heads, d ** -0.5 if scale is None else scale,
             window, sinks, out.data_ptr(), lse.data_ptr() if lse is not None else None, work.data_ptr() if work is not None else None)
     return out, lse
@@ -156,7 +157,7 @@ def weigh_fp8(cache: Fp8Cache, q: torch.Tensor, lse: torch.Tensor, weight: torch
     ldw, start = cache._weights(weight, cache.capacity, "weight"), cache._starts(rows)
     _int32(window, "window"), _int32(sinks, "sinks")
     lib = load_library()
-    work = cache._work(lib.spec_weigh_quant_workspace_bytes, start, n, heads, window, sinks, q)
+    work = cache._work("spec_weigh_quant", start, n, heads, window, sinks, q)
     call_on(cache.device, lib.spec_weigh_quant, cache.ref, q.data_ptr(), ldq, lse.data_ptr(), start, n, heads,
             d ** -0.5 if scale is None else scale, window, sinks, weight.data_ptr(), ldw, work.data_ptr() if work is not None else None)
     return weight

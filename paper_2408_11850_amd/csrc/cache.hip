@@ -1394,6 +1394,8 @@ __global__ __launch_bounds__(GATHER_THREADS) void evict_gather_kernel(QuantCache
 }
 
 // ---- launches -----------------------------------------------------------------------------------------------------------------
+// Splits go by the part's 256 compute units, not by what spec_init finds: workspaces and the order of sums follow from a call's arguments alone.
+#define CUS 256
 // most pages that rows of one tile can see, of `rows_seen` neighbouring entries
 static int most_pages(const QuantCache& c, int rows_seen, int window, int sinks) {
   if (!window) return c.max_pages;
@@ -1427,13 +1429,13 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
   const int G = n_heads / c.n_kv_heads;
   const long long rows = ((long long)n_rows * G + c.n_seqs - 1) / c.n_seqs;      // of a sequence, in the mean
   const long long waves = mean_tiles(c, n_rows, G, 16) * c.n_kv_heads * most_pages(c, (int)(rows / G) + 1, window, sinks);
-  p.row_tiles = rows > 160 && waves > 8ll * spec_num_cu() ? 0 : rows > 16 && waves > 12ll * spec_num_cu() ? 2 : 1;
+  p.row_tiles = rows > 160 && waves > 8ll * CUS ? 0 : rows > 16 && waves > 12ll * CUS ? 2 : 1;
   p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
   const int tile = p.row_tiles ? 16 * p.row_tiles * p.row_waves : MANY_ROWS;
   p.tiles = most_tiles(c, ragged, n_rows, G, tile);
   const long long groups = mean_tiles(c, n_rows, G, tile) * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
   const long long most = p.row_tiles ? (pages + phases - 1) / phases : pages / 8;
-  const long long want = p.row_tiles ? (spec_num_cu() + groups - 1) / groups : spec_num_cu() / groups;
+  const long long want = p.row_tiles ? (CUS + groups - 1) / groups : CUS / groups;
   p.splits = (int)max(1ll, min(min(want, most), (long long)MERGE_PARTS));
   return p;
 }
@@ -1485,12 +1487,12 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
   p.slices = 1;
   if (rows <= 64) {
     p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.groups = (int)max(1ll, min((long long)fours, (3ll * spec_num_cu() + lines - 1) / lines));
+    p.groups = (int)max(1ll, min((long long)fours, (3ll * CUS + lines - 1) / lines));
     return p;
   }
   p.row_tiles = 0;
   p.groups = fours;
-  p.slices = (int)max(1ll, min(min(4ll * spec_num_cu() / (lines * fours), (rows + 255) / 256), 64ll));
+  p.slices = (int)max(1ll, min(min(4ll * CUS / (lines * fours), (rows + 255) / 256), 64ll));
   return p;
 }
 size_t weigh_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
