@@ -176,6 +176,8 @@ struct PageList {
 // ---- append ---------------------------------------------------------------------------------------------------------------
 // A workgroup takes the entries of a call that fall into one page: keys and values of a KV head, or eight query heads.  The
 // angles' cosines and sines are made once per workgroup, in revolutions in 64 bits up to the reduction.
+// Bound by memory for many rows: 4095 tokens of 8 heads with 64 query heads (159 MB read and written) 32.4 us, 4.9 TB/s.  One token: 5.2 us,
+// the trips to its length, its page's id, the scale, and the codes that move if it grows.
 template <int T>
 __device__ __forceinline__ void load8(const void* p, size_t at, float (&v)[8]) {
   if (T == SPEC_F32) {
@@ -487,7 +489,10 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const f32x4 (&o)
 }
 
 // Few rows of a KV head: the codes go to registers as operands, RT tiles of 16 rows share them in a wave.  The waves of a workgroup have
-// row_waves sets of rows and take pages in turn.
+// row_waves sets of rows and take pages in turn.  No LDS on the way, as no other wave wants these codes: pages that four waves share
+// through LDS, a tile of rows each, were slower (81 us against 69 for 64 rows of heads behind 131072), since every wave converts them.
+// One row each of 16 sequences, 32 heads: 627 MB in 115 us, 5.5 TB/s.  64 rows of 8 heads behind 131072: 268 MB in 69 us, 3.9 TB/s, what
+// registers for one page in flight and two waves a SIMD let through.  One token behind 4096: 6.7 us, four dependent trips to memory.
 #define FEW_WAVES 4
 template <int DH, int RT>
 __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_kernel(QuantCache c, AttendArgs a) {
@@ -624,6 +629,11 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
 // way to LDS.  S^T = K Q^T and O^T += V^T P^T, 32 x 32 x 16: row 8 b + 4 c + i of a key tile is entry 16 (b / 2) + 8 c + 4 (b % 2) + i, so that
 // again a lane's scores are the operand it gives, here against eight neighbouring entries of a value's row.  Scores of the next page
 // are formed while the softmax of the present one runs: keys are in LDS one page ahead of values.
+// A prompt of 4095 tokens, 64 heads over 8, d 128: 290 to 330 us, up to 0.96 PFLOP/s; 2.0 us per page, of which reading operands from LDS
+// would take 1.0 alone, the products 0.9, softmax and conversion 1.1.  It is no single one of them: without products, without LDS reads,
+// without the maxima or without the barrier the time stays, without conversion it falls by 15 %.  Slower were 64 rows a wave on half
+// the waves (538: accumulators and queries exceed the registers that vector instructions reach), two workgroups of 4 waves (317
+// against 303: each converts the page), values a page behind, so that all products run beside the softmax (317).
 #define MANY_WAVES 8
 #define MANY_ROWS (MANY_WAVES * 32)
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -832,7 +842,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
 }
 
 // Parts of a row's attention together.  WAVES waves have a row and head: a lane the maximum and sum of a part (there are at most 64), then
-// 4 elements of some of the parts, the first eight of them asked for beside the sums.
+// 4 elements of some of the parts, the first eight of them asked for beside the sums.  64 parts of 64 rows: 4.4 to 5 us (a wave that adds
+// one part after the other: 62); two trips to memory and the launch.
 #define MERGE_WAVES 4
 #define MERGE_PARTS 64
 template <int DH, int WAVES>
@@ -902,7 +913,8 @@ __device__ __forceinline__ Rows rows_of(const QuantCache& c, const int* rows, in
 }
 
 // Few rows: their queries stay in registers, up to RT tiles of 16 at a time, and a wave goes over pages.  S^T = K Q^T as in the attention:
-// a lane's scores belong to one row, so that sums over the rows of a tile are sums over 16 lanes, once per page.
+// a lane's scores belong to one row, so that sums over the rows of a tile are sums over 16 lanes, once per page.  One row each of 8
+// sequences, 64 heads over 8, 34 MB of keys: 13 us, trips to memory before the first page and one or two pages a wave.
 #define WEIGH_WAVES 4
 template <int DH, int RT>
 __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCache c, WeighArgs a) {
@@ -996,7 +1008,8 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
 
 // Many rows: a wave keeps the 64 keys of a page as operands and the workgroup goes over tiles of 64 rows, whose queries, logarithms and
 // entries pass through LDS.  S = Q K^T, 32 x 32 x 16: a lane's scores belong to one entry.  The tiles that see a group of pages are dealt to
-// `slices` workgroups; sums of slices are added in their order.
+// `slices` workgroups; sums of slices are added in their order.  2047 rows, 64 heads over 8, 34.9 GFLOP: 56 us and 4.8 for the slices' sums,
+// about 6 us of it before the first product and nine tiles behind; three workgroups a CU do not fit the registers (142, spilling).
 template <int DH>
 __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCache c, WeighArgs a) {
   constexpr int KS = DH / 16, QB = 66, CH = DH / 8, LOADS = 64 * CH / (WEIGH_WAVES * 64);
@@ -1181,6 +1194,8 @@ __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs 
 // One workgroup per sequence and head finds the weight of the last entry that is kept, 11 bits of an ordered key at a time (the first
 // ones are sign, exponent and two more, so that few entries of a wave meet in a counter), and lists the entries that are kept in their
 // order; then a workgroup per page of 64 of them moves their codes.  A wave has a stretch of entries, in registers where that is up to 1024.
+// Select: 4096 entries of one sequence 10 us, 16 ragged sequences of up to 16384 17 us; barriers and counters in LDS.  Gather of 2048
+// entries of those 16, 8 heads of 128: 55 us; a value's elements are 64 bytes apart, so nearly all pages of values are read whole.
 #define SELECT_THREADS 1024
 #define SELECT_WAVES (SELECT_THREADS / 64)
 #define SELECT_KEYS 16
@@ -1461,6 +1476,7 @@ hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hi
   else launch_attend<64>(c, a, p, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
+  // four waves a row from 17 parts on, unless rows alone fill the chip
   const bool wide = p.splits > 16 && all <= (1u << 16);
   const unsigned groups = wide ? (unsigned)all : (unsigned)((all + MERGE_WAVES - 1) / MERGE_WAVES);
   if (c.head_dim == 128) {
@@ -1490,6 +1506,8 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
     p.groups = (int)max(1ll, min((long long)fours, (3ll * CUS + lines - 1) / lines));
     return p;
   }
+  // many rows: tiles of 64 to so many slices that every CU has four workgroups, each at least 4 tiles (2047 rows of 64 heads over 8, us):
+  //   4 slices 192, 8 100, 16 to 32 58 to 65
   p.row_tiles = 0;
   p.groups = fours;
   p.slices = (int)max(1ll, min(min(4ll * CUS / (lines * fours), (rows + 255) / 256), 64ll));
