@@ -9,6 +9,7 @@
 //
 // Entries are held in the order of their sequence; the rows of a call are its last ones.  Row j of M sees the entries up to its
 // own, len - M + j, and of those, with a window, the last `window` and the first `sinks`.
+#include <float.h>
 #include <limits.h>
 
 #include <type_traits>
@@ -1016,6 +1017,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   __shared__ u32x4 qsh[2][2 * KS * QB];
   __shared__ __align__(16) float lsh[2][64];
   __shared__ __align__(16) int psh[2][64];
+  __shared__ int nans[2];                                      // whether a row of the tile has a NaN as its logarithm
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
   // pages that most rows see first
   const int h = blockIdx.x % c.n_kv_heads, s = blockIdx.y, G = a.G, group = blockIdx.x / c.n_kv_heads / a.slices, slice = blockIdx.x / c.n_kv_heads % a.slices;
@@ -1090,16 +1092,27 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
       const int at = x * WEIGH_WAVES * 64 + tid, r = at / CH, ch = at % CH;
       qsh[to][((r >> 5) * KS + ch / 4 * 2 + (ch & 1)) * QB + (ch >> 1 & 1) * 33 + (r & 31)] = raw[x];
     }
-    if (tid < 64) lsh[to][tid] = lse, psh[to][tid] = pos;
+    // -inf, the score of what a row does not see, less its logarithm has to be -inf: that of a row that sees nothing becomes finite here, a
+    // NaN where scores are hidden
+    if (tid < 64) {
+      lsh[to][tid] = lse < -FLT_MAX ? -FLT_MAX : lse, psh[to][tid] = pos;
+      nans[to] = __ballot(lse != lse) != 0;
+    }
   };
   float sum[2][2] = {};
   // 32 of the 64 rows: their scores, what they do not see, and their logarithms, which the tile's place will not keep
   struct Part {
     f32x16 x[2];
     float lse[16];
+    int nans;
   } p0, p1;
   auto mask = [&](Part& p, int at, int r0) {
     if (r0 >= see_from && r0 + 32 <= see_to) return;
+    if (__builtin_amdgcn_readfirstlane(p.nans)) {              // to the scores, of which only those that count stay
+#pragma unroll
+      for (int y = 0; y < 16; ++y)
+        if (p.lse[y] != p.lse[y]) p.x[0][y] = p.x[1][y] = p.lse[y], p.lse[y] = 0.f;
+    }
 #pragma unroll
     for (int y = 0; y < 16; ++y) {
       const int pos = psh[at][(r0 & 32) + 8 * (y >> 2) + 4 * half + (y & 3)], low = a.window ? pos - a.window : INT_MIN;
@@ -1135,6 +1148,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
     }
 #pragma unroll
     for (int y = 0; y < 16; ++y) p.lse[y] = lsh[at][b * 32 + 8 * (y >> 2) + 4 * half + (y & 3)];
+    p.nans = nans[at];
   };
   if (t0 < t1) {
     load(t0);

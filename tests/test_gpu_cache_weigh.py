@@ -108,3 +108,43 @@ def test_weights_of_an_attention_add_up(m, window, sinks):
     again = amd.weigh_fp8(g, q, lse, w.clone(), window=window, sinks=sinks)
     for s, n in enumerate((900, 300)):
         assert torch.allclose(again[s, :, :n - m], 2 * w[s, :, :n - m], rtol=1e-6) and torch.equal(again[s, :, n - m:], w[s, :, n - m:])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m,n", [(9, 4), (100, 70), (300, 130)])
+def test_rows_without_entries_with_their_own_logarithms(m, n, d):
+    """Rows in front of entry 0 have -inf as the logarithm of their sum and add nothing; the others hand out 1 each."""
+    amd, rng = _amd(), np.random.default_rng(5)
+    g = to_gpu(amd, make(rng, [n, 2 * m], 2, d, junk=True))
+    q = torch.from_numpy(normal(rng, 2 * m, 8, d)).cuda().to(torch.bfloat16)
+    _, lse = amd.attend_fp8(g, q, want_lse=True)
+    assert torch.isneginf(lse[:m - n]).all() and torch.isfinite(lse[m - n:]).all()
+    w = amd.weigh_fp8(g, q, lse, torch.zeros(2, 2, g.capacity, device="cuda"))
+    want = torch.tensor([n * 4.0, m * 4.0], device="cuda", dtype=torch.float64)[:, None]
+    assert ((w.double().sum(2) - want).abs() <= want * 1e-4).all()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("window", [0, 20])
+@pytest.mark.parametrize("m", [4, 16, 200])
+def test_a_row_whose_logarithm_is_none_touches_only_what_it_sees(m, window, value):
+    """Row j with NaN: NaN; with +inf: nothing; with -inf: inf, to the entries that it sees, and all others as without it."""
+    amd, rng = _amd(), np.random.default_rng(6)
+    n, j = 300, m // 2
+    g = to_gpu(amd, make(rng, [n], 2, 128, junk=True))
+    q = torch.from_numpy(normal(rng, m, 8, 128)).cuda().to(torch.bfloat16)
+    _, lse = amd.attend_fp8(g, q, window=window, want_lse=True)
+    odd, none = lse.clone(), lse.clone()
+    odd[j, 4:] = value
+    none[j, 4:] = float("inf")
+    got = amd.weigh_fp8(g, q, odd, torch.zeros(1, 2, g.capacity, device="cuda"), window=window)
+    without = amd.weigh_fp8(g, q, none, torch.zeros(1, 2, g.capacity, device="cuda"), window=window)
+    assert torch.isfinite(without).all()
+    last = n - m + j
+    seen = torch.zeros(g.capacity, dtype=torch.bool, device="cuda")
+    seen[max(0, last - window + 1) if window else 0:last + 1] = True
+    assert torch.equal(got[0, 0], without[0, 0]) and torch.equal(got[0, 1][~seen], without[0, 1][~seen])
+    if value == float("inf"):
+        assert torch.equal(got, without)
+    else:
+        assert (torch.isnan(got[0, 1][seen]) if value != value else torch.isposinf(got[0, 1][seen])).all()
