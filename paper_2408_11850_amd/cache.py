@@ -21,7 +21,8 @@ class Fp8Cache:
 
     k e4m3 [n_pages][heads][64][d]; v e4m3 [n_pages][heads][d][64]; scale fp32 [n_pages][heads][2] (of the keys, of the values);
     table int32 [n_seqs][max_pages] (any row stride); length int32 [n_seqs], the entries of every sequence with the rows of the
-    calls that follow.  All contiguous but the table's rows, on one GPU."""
+    calls that follow.  All contiguous but the table's rows, on one GPU.  Their values may change at any time, as the calls on a stream see
+    them; other tensors need another Fp8Cache."""
 
     __slots__ = ("k", "v", "scale", "table", "length", "device", "heads", "d", "n_seqs", "capacity", "desc", "ref", "sizes")
 
@@ -58,14 +59,17 @@ class Fp8Cache:
 
     def _rows(self, x: torch.Tensor, heads: int, name: str) -> int:
         """Row stride of [n][heads][d] on this cache's device."""
-        if x.dim() != 3 or x.get_device() != self.device or x.shape[2] != self.d or not heads or (heads > 0 and x.shape[1] != heads):
+        if x.dim() != 3 or x.get_device() != self.device:
             raise ValueError(f"{name}: [rows][heads][d] of the cache's d on its device is wanted")
-        st = x.stride()
-        if st[2] != 1 or (st[1] != self.d and x.shape[1] != 1):
+        n, h, d = x.shape                                      # once: a look at a tensor's attribute takes 0.1 us
+        ld, apart, one = x.stride()
+        if d != self.d or not heads or (heads > 0 and h != heads):
+            raise ValueError(f"{name}: [rows][heads][d] of the cache's d on its device is wanted")
+        if one != 1 or (apart != d and h != 1):
             raise ValueError(f"{name}: the heads of a row have to be neighbours")
-        if x.shape[0] >> 31 or x.shape[1] >> 31:               # ctypes would keep the low 32 bits
+        if (n | h) >> 31:                                      # ctypes would keep the low 32 bits
             raise ValueError(f"{name}: rows and heads below 2^31 are wanted")
-        return st[0] if x.shape[0] > 1 else x.shape[1] * self.d
+        return ld if n > 1 else h * d
 
     def _starts(self, rows: Optional[torch.Tensor]):
         if rows is None:
@@ -103,7 +107,7 @@ def append_fp8(cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, q: Optional[to
         ldq, heads = cache._rows(q, -1, "q"), q.shape[1]
         if q.dtype is not k.dtype or q.shape[0] != n:
             raise ValueError("q: as many rows as k, of its type, are wanted")
-        out = q.new_empty((n, heads, cache.d), dtype=torch.bfloat16)
+        out = q.new_empty(n, heads, cache.d, dtype=torch.bfloat16)
     if position is not None and not (position.dtype is torch.int32 and position.shape == (cache.n_seqs,) and position.is_contiguous() and
                                      position.get_device() == cache.device):
         raise ValueError("position: int32 [n_seqs] on the cache's device is wanted")
@@ -129,14 +133,14 @@ def attend_fp8(cache: Fp8Cache, q: torch.Tensor, rows: Optional[torch.Tensor] = 
     start = cache._starts(rows)
     _int32(window, "window"), _int32(sinks, "sinks")
     if out is None:
-        out = q.new_empty((n, heads, d))
+        out = q.new_empty(n, heads, d)
     elif not (out.dtype is torch.bfloat16 and out.shape == q.shape and out.is_contiguous() and out.get_device() == cache.device):
         raise ValueError("out: contiguous bfloat16 of the shape of q on its device is wanted")
     if lse is not None:
         if not (lse.dtype is torch.float32 and lse.shape == (n, heads) and lse.is_contiguous() and lse.get_device() == cache.device):
             raise ValueError("lse: contiguous float32 [n][query heads] on the device of q is wanted")
     elif want_lse:
-        lse = q.new_empty((n, heads), dtype=torch.float32)
+        lse = q.new_empty(n, heads, dtype=torch.float32)
     lib = load_library()
     work = cache._work("spec_attend_quant", start, n, heads, window, sinks, q)
     call_on(cache.device, lib.spec_attend_quant, cache.ref, q.data_ptr(), ldq, start, n, heads, d ** -0.5 if scale is None else scale,
@@ -177,9 +181,9 @@ def evict_fp8(cache: Fp8Cache, weight: torch.Tensor, to: Fp8Cache, budget: int, 
         raise ValueError("to: a cache of the same heads and sequences on the same device is wanted")
     if budget > to.capacity:
         raise ValueError("budget: more than the new table holds")
-    kept = weight.new_empty((cache.n_seqs, cache.heads, budget), dtype=torch.int32)
+    kept = weight.new_empty(cache.n_seqs, cache.heads, budget, dtype=torch.int32)
     if to_weight is None:
-        to_weight = weight.new_empty((cache.n_seqs, cache.heads, budget))
+        to_weight = weight.new_empty(cache.n_seqs, cache.heads, budget)
     ldt = to._weights(to_weight, budget, "to_weight")
     call_on(cache.device, load_library().spec_evict_quant, cache.ref, weight.data_ptr(), ldw, to.ref, budget, sinks, recent,
             kept.data_ptr(), to_weight.data_ptr(), ldt)
