@@ -469,7 +469,7 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[4], f32x4 (&o)[DH / 16],
 }
 // a row's result, or its part: 4 elements of every 16 in this lane
 template <int DH>
-__device__ __forceinline__ void store_rows(const AttendArgs& a, const f32x4 (&o)[DH / 16], float m, float l, int pos, int split, size_t row_at, int g) {
+__device__ __forceinline__ void store_rows(const AttendArgs& a, const f32x4 (&o)[DH / 16], float m, float l, int pos, int split, size_t row_at, size_t part_at, int g) {
   if (a.splits == 1) {
     const bool empty = pos < 0;
     const float inv = empty ? 0.f : 1.f / l;
@@ -482,7 +482,7 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const f32x4 (&o)
     }
     if (a.lse && g == 0) a.lse[row_at] = empty ? -INFINITY : (m + __log2f(l)) * LN2;
   } else {
-    const size_t at = (size_t)split * a.n_rows * a.n_heads + row_at;
+    const size_t at = split * a.part_rows + part_at;
 #pragma unroll
     for (int d = 0; d < DH / 16; ++d) *reinterpret_cast<f32x4*>(a.part + at * DH + d * 16 + g * 4) = o[d];
     if (g == 0) a.part_ml[at] = make_float2(pos < 0 ? -INFINITY : m, l);       // -inf: the row sees nothing
@@ -502,15 +502,21 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
   __shared__ float2 mlsh[FEW_WAVES][RT][16];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   const unsigned parts = c.n_kv_heads * a.splits, part = blockIdx.x % parts;
-  const int h = part % c.n_kv_heads, split = part / c.n_kv_heads, G = a.G, tile_rows = 16 * RT * a.row_waves;
-  Span sp = find_span(c, a.rows, a.n_rows, blockIdx.x / parts, [&](int M) { return (M * G + tile_rows - 1) / tile_rows; });
+  const int h = part % c.n_kv_heads, split = part / c.n_kv_heads, G = a.G;
+  // sets of rows of a sequence with R: as the call says, or where its sequences differ as the sequence does
+  auto row_waves = [&](int R) { return a.row_waves ? a.row_waves : R > 32 * RT ? 4 : R > 16 * RT ? 2 : 1; };
+  Span sp = find_span(c, a.rows, a.n_rows, blockIdx.x / parts, [&](int M) {
+    const int tile_rows = 16 * RT * row_waves(M * G);
+    return M * G <= a.upto ? (M * G + tile_rows - 1) / tile_rows : 0;
+  });
   sp.s = __builtin_amdgcn_readfirstlane(sp.s);
   if (sp.s < 0) return;
   sp.t = __builtin_amdgcn_readfirstlane(sp.t), sp.row = __builtin_amdgcn_readfirstlane(sp.row), sp.M = __builtin_amdgcn_readfirstlane(sp.M);
+  const size_t part_from = a.per ? ((size_t)sp.s * a.per - sp.row) * a.n_heads : 0;       // of the parts, less that of the rows
   const int given = __builtin_amdgcn_readfirstlane(sp.len);
   const bool beyond = given > c.max_pages * PAGE;    // nothing is read; the rows become NaN
   const int len = max(given, 0), first = len - sp.M, R = sp.M * G;
-  const int phases = FEW_WAVES / a.row_waves, rw = w % a.row_waves, phase = w / a.row_waves;
+  const int sets = row_waves(R), tile_rows = 16 * RT * sets, phases = FEW_WAVES / sets, rw = w % sets, phase = w / sets;
   const int wg0 = sp.t * tile_rows, wg_last = min(wg0 + tile_rows, R) - 1, r0 = wg0 + rw * 16 * RT, r_last = min(r0 + 16 * RT, R) - 1;
   const Seen seen = seen_pages(first + wg0 / G, beyond ? -1 : first + wg_last / G, a.window, a.sinks);
   const int per = (seen.n + a.splits - 1) / a.splits, i0 = split * per + phase;
@@ -605,13 +611,13 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     float top = NONE, sum = 0.f;
-    for (int x = rw; x < FEW_WAVES; x += a.row_waves) top = fmaxf(top, mlsh[x][rt][r16].x);
-    for (int x = rw; x < FEW_WAVES; x += a.row_waves) sum += mlsh[x][rt][r16].y * __builtin_amdgcn_exp2f(mlsh[x][rt][r16].x - top);
+    for (int x = rw; x < FEW_WAVES; x += sets) top = fmaxf(top, mlsh[x][rt][r16].x);
+    for (int x = rw; x < FEW_WAVES; x += sets) sum += mlsh[x][rt][r16].y * __builtin_amdgcn_exp2f(mlsh[x][rt][r16].x - top);
     const float f = __builtin_amdgcn_exp2f(m[rt] - top);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       o[rt][d] *= f;
-      if (phase) osh[w - a.row_waves][rt][d][lane] = o[rt][d];
+      if (phase) osh[w - sets][rt][d][lane] = o[rt][d];
     }
     m[rt] = top, l[rt] = sum;
   }
@@ -619,10 +625,10 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
   if (phase) return;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    for (int x = rw; x < FEW_WAVES - a.row_waves; x += a.row_waves)
+    for (int x = rw; x < FEW_WAVES - sets; x += sets)
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[rt][d] += osh[x][rt][d][lane];
-    if (r0 + rt * 16 + r16 < R) store_rows<DH>(a, o[rt], m[rt], beyond ? NAN32 : l[rt], pos[rt], split, row_at[rt], g);
+    if (r0 + rt * 16 + r16 < R) store_rows<DH>(a, o[rt], m[rt], beyond ? NAN32 : l[rt], pos[rt], split, row_at[rt], row_at[rt] + part_from, g);
   }
 }
 
@@ -648,7 +654,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
   const unsigned parts = c.n_kv_heads * a.splits, part = blockIdx.x % parts;
   const int h = part % c.n_kv_heads, split = part / c.n_kv_heads, G = a.G;
-  Span sp = find_span(c, a.rows, a.n_rows, gridDim.x / parts - 1 - blockIdx.x / parts, [&](int M) { return (M * G + MANY_ROWS - 1) / MANY_ROWS; });
+  Span sp = find_span(c, a.rows, a.n_rows, gridDim.x / parts - 1 - blockIdx.x / parts, [&](int M) { return M * G > a.above ? (M * G + MANY_ROWS - 1) / MANY_ROWS : 0; });
   sp.s = __builtin_amdgcn_readfirstlane(sp.s);
   if (sp.s < 0) return;
   sp.t = __builtin_amdgcn_readfirstlane(sp.t), sp.row = __builtin_amdgcn_readfirstlane(sp.row), sp.M = __builtin_amdgcn_readfirstlane(sp.M);
@@ -832,7 +838,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
       }
     if (a.lse && half == 0) a.lse[row_at] = empty ? -INFINITY : (m + __log2f(l)) * LN2;
   } else {
-    const size_t at = (size_t)split * a.n_rows * a.n_heads + row_at;
+    const size_t at = split * a.part_rows + row_at;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -852,10 +858,25 @@ __global__ __launch_bounds__(MERGE_WAVES * 64) void attend_merge_kernel(QuantCac
   constexpr int LANES = DH / 4, WAYS = 64 / LANES * WAVES, AHEAD = 8;
   __shared__ f32x4 osh[MERGE_WAVES][LANES];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, way = w % WAVES * (64 / LANES) + lane / LANES;
-  const size_t all = (size_t)a.n_rows * a.n_heads, at = (size_t)blockIdx.x * (MERGE_WAVES / WAVES) + w / WAVES;
+  const size_t all = a.part_rows, at = (size_t)blockIdx.x * (MERGE_WAVES / WAVES) + w / WAVES;
   if (at >= all) return;                                                        // WAVES == 4: the whole workgroup
-  const int row = (int)(at / a.n_heads);
-  if (a.rows && (row >= a.rows[c.n_seqs] || row < a.rows[0])) return;         // rows of no sequence have no parts and stay as they are
+  int row = (int)(at / a.n_heads);
+  if (a.per) {
+    const int s = row / a.per, first = min(max(a.rows[s], 0), a.n_rows), M = min(max(a.rows[s + 1], first), a.n_rows) - first;
+    row -= s * a.per;
+    if (row >= M || M * a.G > a.upto) return;
+    row += first;
+  } else if (a.rows) {
+    if (row >= a.rows[c.n_seqs] || row < a.rows[0]) return;                   // rows of no sequence have no parts and stay as they are
+    if (a.above) {
+      int s = 0;                                                                // sequences that end in front of the row
+      for (int base = 0; base < c.n_seqs; base += 64)
+        s += __popcll(__ballot(base + lane < c.n_seqs && a.rows[min(base + lane, c.n_seqs - 1) + 1] <= row));
+      s = min(s, c.n_seqs - 1);
+      if ((min(a.rows[s + 1], a.n_rows) - max(a.rows[s], 0)) * a.G <= a.above) return;
+    }
+  }
+  const size_t to = (size_t)row * a.n_heads + at % a.n_heads;
   const float2 ml = lane < a.splits ? a.part_ml[lane * all + at] : make_float2(-INFINITY, 0.f);
   const float* from = a.part + at * DH + (lane % LANES) * 4;
   f32x4 ahead[AHEAD];
@@ -890,8 +911,8 @@ __global__ __launch_bounds__(MERGE_WAVES * 64) void attend_merge_kernel(QuantCac
   bf16 b[4];
 #pragma unroll
   for (int x = 0; x < 4; ++x) b[x] = __float2bfloat16(o[x] * inv);
-  *reinterpret_cast<uint2*>(a.out + at * DH + lane * 4) = *reinterpret_cast<const uint2*>(b);
-  if (a.lse && lane == 0) a.lse[at] = empty ? -INFINITY : (top + __log2f(sum)) * LN2;
+  *reinterpret_cast<uint2*>(a.out + to * DH + lane * 4) = *reinterpret_cast<const uint2*>(b);
+  if (a.lse && lane == 0) a.lse[to] = empty ? -INFINITY : (top + __log2f(sum)) * LN2;
 }
 
 // ---- attention weight of the entries ------------------------------------------------------------------------------------------
@@ -1447,60 +1468,81 @@ static long long mean_tiles(const QuantCache& c, int n_rows, int G, int tile) {
 //   parts of a sequence so that every CU has a workgroup (one a CU | two):
 //     8 sequences, 64 rows behind 4096   27.0 | 28.6      64 rows behind 8192   18.9 | 23.9      windows of 8 requests   18.7 | 22.2
 //     against it  64 rows behind 131072   76.9 | 71.3
-struct AttendPlan {
+// One launch (and a merge) takes all sequences, or where they may differ two of them those of more than SHORT rows of a KV head and the others.
+// The host does not know which there are, so rows of heads have to be so many that a launch with nothing to do does not count (one | two):
+//     a prompt of 2048 tokens and 31 single ones behind 8192   332 | 192      a prompt of 300 and 16 single ones behind 4000   102 | 57
+//     512 behind 3584 and the same 31   275 | 188      a prompt of 2048 and 4 windows of 8 behind 32768   889 | 172
+//     against it  256 behind 768 and 63 single ones behind 2048   62 | 78      8 times 64 behind 2048   59 | 63      64 windows of 8   127 | 131
+#define SHORT 160
+struct AttendPass {
   int row_tiles;    // of 16 rows in a wave; 0: many rows
   int row_waves;    // waves of a workgroup that have rows of their own; the others take other pages of theirs
   int splits;
   long long tiles;
+  int above, upto, per;
+  size_t part_rows;
+};
+struct AttendPlan {
+  AttendPass pass[2];
+  int n;
 };
 static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   AttendPlan p;
   const int G = n_heads / c.n_kv_heads;
-  const long long rows = ((long long)n_rows * G + c.n_seqs - 1) / c.n_seqs;      // of a sequence, in the mean
+  const long long total = (long long)n_rows * G, rows = (total + c.n_seqs - 1) / c.n_seqs;      // of a sequence, in the mean
   const long long waves = mean_tiles(c, n_rows, G, 16) * c.n_kv_heads * most_pages(c, (int)(rows / G) + 1, window, sinks);
-  p.row_tiles = rows > 160 && waves > 8ll * CUS ? 0 : rows > 16 && waves > 12ll * CUS ? 2 : 1;
-  p.row_waves = rows > 64 ? 4 : rows > 32 ? 2 : 1;
-  const int tile = p.row_tiles ? 16 * p.row_tiles * p.row_waves : MANY_ROWS;
-  p.tiles = most_tiles(c, ragged, n_rows, G, tile);
-  const long long groups = mean_tiles(c, n_rows, G, tile) * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / p.row_waves;
-  const long long most = p.row_tiles ? (pages + phases - 1) / phases : pages / 8;
-  const long long want = p.row_tiles ? (CUS + groups - 1) / groups : CUS / groups;
-  p.splits = (int)max(1ll, min(min(want, most), (long long)MERGE_PARTS));
+  const bool mixed = ragged && c.n_seqs > 1 && G <= SHORT && total > 2048 && waves > 8ll * CUS;
+  p.n = mixed ? 2 : 1;
+  for (int i = 0; i < p.n; ++i) {
+    AttendPass& x = p.pass[i];
+    const bool many = mixed ? i == 0 : rows > SHORT && waves > 8ll * CUS;
+    x.row_tiles = many ? 0 : mixed || (rows > 16 && waves > 12ll * CUS) ? 2 : 1;
+    x.row_waves = mixed ? 0 : rows > 64 ? 4 : rows > 32 ? 2 : 1;
+    x.above = mixed && many ? SHORT : 0, x.upto = mixed && !many ? SHORT : INT_MAX, x.per = mixed && !many ? SHORT / G : 0;
+    x.part_rows = (size_t)(x.per ? (long long)c.n_seqs * x.per : n_rows) * n_heads;
+    // rows of a workgroup, the most tiles there can be, and how many there will be about: a row of every sequence is not the long ones'
+    const int tile = many ? MANY_ROWS : 16 * x.row_tiles * max(x.row_waves, 1);
+    x.tiles = !mixed ? most_tiles(c, ragged, n_rows, G, tile) : many ? total / (MANY_ROWS / 2) : 2ll * c.n_seqs;
+    const long long about = !mixed ? mean_tiles(c, n_rows, G, tile) : many ? max(1ll, (total - (long long)c.n_seqs * G + tile - 1) / tile) : c.n_seqs;
+    const long long groups = about * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / max(x.row_waves, 1);
+    const long long most = many ? pages / 8 : (pages + phases - 1) / phases;
+    const long long want = many ? CUS / groups : (CUS + groups - 1) / groups;
+    x.splits = (int)max(1ll, min(min(want, most), (long long)MERGE_PARTS));
+  }
   return p;
 }
 size_t attend_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   const AttendPlan p = attend_plan(c, ragged, n_rows, n_heads, window, sinks);
-  return p.splits == 1 ? 0 : (size_t)p.splits * n_rows * n_heads * (c.head_dim + 2) * sizeof(float);
+  size_t most = 0;                                     // passes run one behind the other
+  for (int i = 0; i < p.n; ++i)
+    if (p.pass[i].splits > 1) most = std::max(most, p.pass[i].splits * p.pass[i].part_rows * (c.head_dim + 2) * sizeof(float));
+  return most;
 }
 template <int DH>
-static void launch_attend(const QuantCache& c, const AttendArgs& a, const AttendPlan& p, hipStream_t st) {
+static hipError_t launch_attend(const QuantCache& c, const AttendArgs& a, const AttendPass& p, hipStream_t st) {
   const unsigned groups = (unsigned)(p.tiles * c.n_kv_heads * p.splits);
   if (p.row_tiles == 1) attend_few_kernel<DH, 1><<<groups, FEW_WAVES * 64, 0, st>>>(c, a);
   else if (p.row_tiles == 2) attend_few_kernel<DH, 2><<<groups, FEW_WAVES * 64, 0, st>>>(c, a);
   else attend_many_kernel<DH><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  // four waves a row from 17 parts on, unless rows alone fill the chip
+  if (p.splits > 16 && a.part_rows <= (1u << 16)) attend_merge_kernel<DH, 4><<<(unsigned)a.part_rows, MERGE_WAVES * 64, 0, st>>>(c, a);
+  else attend_merge_kernel<DH, 1><<<(unsigned)((a.part_rows + MERGE_WAVES - 1) / MERGE_WAVES), MERGE_WAVES * 64, 0, st>>>(c, a);
+  return hipGetLastError();
 }
 hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hipStream_t st) {
   const AttendPlan p = attend_plan(c, a.rows != nullptr, a.n_rows, a.n_heads, a.window, a.sinks);
   a.G = a.n_heads / c.n_kv_heads;
-  a.splits = p.splits, a.row_waves = p.row_waves;
-  const size_t all = (size_t)a.n_rows * a.n_heads;
   a.part = (float*)work;
-  a.part_ml = (float2*)(a.part + (size_t)p.splits * all * c.head_dim);
-  if (c.head_dim == 128) launch_attend<128>(c, a, p, st);
-  else launch_attend<64>(c, a, p, st);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  // four waves a row from 17 parts on, unless rows alone fill the chip
-  const bool wide = p.splits > 16 && all <= (1u << 16);
-  const unsigned groups = wide ? (unsigned)all : (unsigned)((all + MERGE_WAVES - 1) / MERGE_WAVES);
-  if (c.head_dim == 128) {
-    if (wide) attend_merge_kernel<128, 4><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
-    else attend_merge_kernel<128, 1><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
-  } else {
-    if (wide) attend_merge_kernel<64, 4><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
-    else attend_merge_kernel<64, 1><<<groups, MERGE_WAVES * 64, 0, st>>>(c, a);
+  for (int i = 0; i < p.n; ++i) {
+    const AttendPass& x = p.pass[i];
+    a.splits = x.splits, a.row_waves = x.row_waves, a.above = x.above, a.upto = x.upto, a.per = x.per, a.part_rows = x.part_rows;
+    a.part_ml = (float2*)(a.part + x.splits * x.part_rows * c.head_dim);
+    const hipError_t e = c.head_dim == 128 ? launch_attend<128>(c, a, x, st) : launch_attend<64>(c, a, x, st);
+    if (e != hipSuccess) return e;
   }
-  return hipGetLastError();
+  return hipSuccess;
 }
 struct WeighPlan {
   int row_tiles;    // of 16 rows, in registers; 0: many rows

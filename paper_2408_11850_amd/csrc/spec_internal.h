@@ -231,8 +231,12 @@ struct AttendArgs {
   int window, sinks;
   bf16* out;
   float* lse;                 // may be null
-  int G, splits, row_waves;   // set by the launch ...
-  float* part;                // ... parts [splits][n_rows][n_heads][head_dim] and their maxima and sums
+  int G, splits;              // set by the launch ...
+  int row_waves;              // ... 0: by the sequence
+  int above, upto;            // ... sequences with more than `above` and at most `upto` rows of a KV head are taken
+  int per;                    // > 0: their parts stand `per` rows apart, else where the call's rows do
+  size_t part_rows;           // rows of heads with a part
+  float* part;                // parts [splits][part_rows][head_dim] and their maxima and sums
   float2* part_ml;
 };
 struct WeighArgs {

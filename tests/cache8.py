@@ -78,3 +78,8 @@ def check_attention(got, lse, want, want_lse, mass, size, d, n):
         room = off + 8 * EPS * (np.abs(np.where(there, want_lse, 0)) + 1 + worst)
         with np.errstate(invalid="ignore"):
             assert (np.abs(lse - want_lse) <= room)[there].all()
+
+
+# (rows, lengths, heads, kv): prompts, drafts and single tokens in one batch, so many rows that sequences of few and of many have kernels of their own
+MIXED = [([600, 1, 0, 5, 40, 41, 1], [700, 900, 0, 77, 300, 41, 2000], 8, 2), ([150, 3, 8, 9, 0, 1], [150, 500, 1000, 9, 64, 640], 40, 2),
+         ([1] * 60 + [500], [130] * 60 + [600], 8, 2), ([1050] + [1] * 15, [1050] + [65] * 15, 32, 16), ([0, 257, 0, 257, 32, 33, 0], [9, 300, 0, 257, 90, 600, 1], 8, 2)]

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import cache8
-from tests.cache8 import bf16, check_attention, make, normal, starts_of, to_gpu
+from tests.cache8 import MIXED, bf16, check_attention, make, normal, starts_of, to_gpu
 from tests.util import gpu_available
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs a GPU")]
@@ -150,3 +150,20 @@ def test_split_and_unsplit_rows_agree():
     assert torch.equal(among, among[:1].expand(200, 64, 128)) and torch.equal(lse2, lse2[:1].expand(200, 64))
     assert ((alone[0].float() - among[0].float()).abs() <= 2.0 ** -7 * alone[0].float().abs() + 2.0 ** -9).all()
     assert ((lse - lse2[:1]).abs() <= 1e-5).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 5)])
+@pytest.mark.parametrize("rows,lengths,heads,kv", MIXED)
+def test_prompts_and_single_tokens_in_one_batch(rows, lengths, heads, kv, window, sinks, d):
+    _run(lengths, rows, heads, kv, d, window, sinks, pad_rows=3)
+
+
+def test_pages_and_lengths_that_are_none_in_a_mixed_batch():
+    """Pages that are none and lengths beyond the table, in front of and behind sequences of the other kind."""
+    def change(c):
+        c.table[0, 2] = 10 ** 6
+        c.table[3, 1] = -1
+        c.length[2] = 64 * c.table.shape[1] + 1
+        c.length[5] = 64 * c.table.shape[1] + 7
+    _run([700, 300, 600, 200, 5, 90, 400], [600, 1, 300, 3, 9, 1, 41], 8, 2, 128, change=change, pad_rows=1)

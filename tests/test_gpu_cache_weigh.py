@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import cache8
-from tests.cache8 import EPS, bf16, make, normal, starts_of, to_gpu
+from tests.cache8 import EPS, MIXED, bf16, make, normal, starts_of, to_gpu
 from tests.util import gpu_available
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs a GPU")]
@@ -148,3 +148,10 @@ def test_a_row_whose_logarithm_is_none_touches_only_what_it_sees(m, window, valu
         assert torch.equal(got, without)
     else:
         assert (torch.isnan(got[0, 1][seen]) if value != value else torch.isposinf(got[0, 1][seen])).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (200, 5)])
+@pytest.mark.parametrize("rows,lengths,heads,kv", MIXED)
+def test_prompts_and_single_tokens_in_one_batch(rows, lengths, heads, kv, window, sinks, d):
+    _run(lengths, rows, heads, kv, d, window, sinks)
