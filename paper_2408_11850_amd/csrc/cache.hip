@@ -934,6 +934,12 @@ __device__ __forceinline__ Rows rows_of(const QuantCache& c, const int* rows, in
   return r;
 }
 
+// slices of a sequence's tiles of 64 rows where sequences differ, 0 if its rows are few
+__device__ __forceinline__ int slices_of(const WeighArgs& a, int M) {
+  const int R = M * a.G;
+  return R > a.above ? ((R + 63) / 64 + a.tiles - 1) / a.tiles : 0;
+}
+
 // Few rows: their queries stay in registers, up to RT tiles of 16 at a time, and a wave goes over pages.  S^T = K Q^T as in the attention:
 // a lane's scores belong to one row, so that sums over the rows of a tile are sums over 16 lanes, once per page.  One row each of 8
 // sequences, 64 heads over 8, 34 MB of keys: 13 us, trips to memory before the first page and one or two pages a wave.
@@ -944,7 +950,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
   const int h = blockIdx.y, s = blockIdx.z, G = a.G;
   const Rows rs = rows_of(c, a.rows, a.n_rows, s, G);
-  if (rs.none) return;
+  if (rs.none || rs.R > a.upto) return;
   const int first = rs.first, len = rs.len;
   const Seen seen = seen_pages(first, len - 1, a.window, a.sinks);
   const int from = blockIdx.x * WEIGH_WAVES + w, step = gridDim.x * WEIGH_WAVES;
@@ -1030,7 +1036,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
 
 // Many rows: a wave keeps the 64 keys of a page as operands and the workgroup goes over tiles of 64 rows, whose queries, logarithms and
 // entries pass through LDS.  S = Q K^T, 32 x 32 x 16: a lane's scores belong to one entry.  The tiles that see a group of pages are dealt to
-// `slices` workgroups; sums of slices are added in their order.  2047 rows, 64 heads over 8, 34.9 GFLOP: 56 us and 4.8 for the slices' sums,
+// `slices` workgroups, or to as many of them as `a.tiles` asks for where sequences differ; sums of slices are added in their order.  2047 rows, 64 heads over 8, 34.9 GFLOP: 56 us and 4.8 for the slices' sums,
 // about 6 us of it before the first product and nine tiles behind; three workgroups a CU do not fit the registers (142, spilling).
 template <int DH>
 __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCache c, WeighArgs a) {
@@ -1041,7 +1047,14 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   __shared__ int nans[2];                                      // whether a row of the tile has a NaN as its logarithm
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
   // pages that most rows see first
-  const int h = blockIdx.x % c.n_kv_heads, s = blockIdx.y, G = a.G, group = blockIdx.x / c.n_kv_heads / a.slices, slice = blockIdx.x / c.n_kv_heads % a.slices;
+  const int h = blockIdx.x % c.n_kv_heads, G = a.G, group = blockIdx.x / c.n_kv_heads / a.slices;
+  int s = blockIdx.y, slice = blockIdx.x / c.n_kv_heads % a.slices, slices = a.slices;
+  if (a.tiles) {
+    const Span sp = find_span(c, a.rows, a.n_rows, blockIdx.y, [&](int M) { return slices_of(a, M); });
+    s = __builtin_amdgcn_readfirstlane(sp.s);
+    if (s < 0) return;
+    slice = __builtin_amdgcn_readfirstlane(sp.t), slices = slices_of(a, __builtin_amdgcn_readfirstlane(sp.M));
+  }
   const Rows rs = rows_of(c, a.rows, a.n_rows, s, G);
   if (rs.none) return;
   const int first = rs.first, len = rs.len, R = rs.R;
@@ -1075,7 +1088,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   const int tiles = (R + 63) / 64, tile0 = max(0, lo_e - first) * G / 64;
   int tile1 = tiles;
   if (a.window && lo_e >= a.sinks && hi_e + a.window - first < rs.M) tile1 = min(tiles, max(0, hi_e + a.window - first) * G / 64 + 1);
-  const int all_tiles = max(0, tile1 - tile0), t0 = tile0 + (int)((long long)slice * all_tiles / a.slices), t1 = tile0 + (int)((long long)(slice + 1) * all_tiles / a.slices);
+  const int all_tiles = max(0, tile1 - tile0), t0 = tile0 + (int)((long long)slice * all_tiles / slices), t1 = tile0 + (int)((long long)(slice + 1) * all_tiles / slices);
   auto token = [&](int r) { return (int)((unsigned long long)(unsigned)r * a.by_group >> 38); };      // r / G
   // rows that see all of this wave's page
   const int see_from = max(0, e0 + PAGE - 1 - first) * G;
@@ -1200,28 +1213,37 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   const float v = half ? sum[1][0] : sum[0][0];
   const int e = e0 + lane;
   if (!has || e >= len) return;
-  const size_t line = (size_t)s * c.n_kv_heads + h;
-  if (a.slices == 1) {
-    float* to = a.weight + line * a.ldw + e;
+  if (slices == 1) {
+    float* to = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw + e;
     *to = e < first ? *to + v : v;                             // an entry of these rows begins here
-  } else a.part[((size_t)slice * c.n_seqs * c.n_kv_heads + line) * c.max_pages * PAGE + e] = v;
+  } else a.part[((a.tiles ? blockIdx.y : (size_t)slice * c.n_seqs + s) * c.n_kv_heads + h) * c.max_pages * PAGE + e] = v;
 }
 
 __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs a) {
   const int h = blockIdx.y, s = blockIdx.z;
   const Rows rs = rows_of(c, a.rows, a.n_rows, s, a.G);
   if (rs.none) return;
+  int slices = a.slices, from = s;                             // the first of its slices
+  if (a.tiles) {
+    slices = slices_of(a, rs.M), from = 0;
+    for (int base = 0; base < s; base += 64) {
+      const int x = base + (int)(threadIdx.x & 63), first = x < s ? min(max(a.rows[x], 0), a.n_rows) : 0;
+      const int mine = x < s ? slices_of(a, min(max(a.rows[x + 1], first), a.n_rows) - first) : 0;
+      from += __builtin_amdgcn_readlane(lanes_upto(mine), 63);
+    }
+    if (slices < 2 || from + slices > a.ids) return;           // written by its only slice; beyond: row numbers that do not rise
+  }
   const Seen seen = seen_pages(rs.first, rs.len - 1, a.window, a.sinks);
   const int i = blockIdx.x * 4 + threadIdx.x / PAGE;
   if (i >= seen.n) return;
   const int e = seen.page(i) * PAGE + threadIdx.x % PAGE;
   if (e >= rs.len) return;
-  const size_t line = (size_t)s * c.n_kv_heads + h, all = (size_t)c.n_seqs * c.n_kv_heads * c.max_pages * PAGE;
-  const float* p = a.part + line * c.max_pages * PAGE + e;
-  float* to = a.weight + line * a.ldw + e;
+  const size_t block = (size_t)c.n_kv_heads * c.max_pages * PAGE, all = a.tiles ? block : c.n_seqs * block;
+  const float* p = a.part + ((size_t)from * c.n_kv_heads + h) * c.max_pages * PAGE + e;
+  float* to = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw + e;
   float v = e < rs.first ? *to : 0.f;                          // an entry of these rows begins here
 #pragma unroll 8
-  for (int x = 0; x < a.slices; ++x) v += p[x * all];
+  for (int x = 0; x < slices; ++x) v += p[x * all];
   *to = v;
 }
 
@@ -1544,54 +1566,79 @@ hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hi
   }
   return hipSuccess;
 }
-struct WeighPlan {
+struct WeighPass {
   int row_tiles;    // of 16 rows, in registers; 0: many rows
-  int pages;        // most that are seen
   int groups;       // workgroups in x, over the slices' number
-  int slices;
+  int slices;       // of every sequence, or
+  int tiles, ids;   // tiles of 64 rows in one, and how many of them there can be
+  int above, upto;  // sequences with more than `above` and at most `upto` rows of a KV head are taken
 };
+struct WeighPlan {
+  WeighPass pass[2];
+  int n, pages;     // most that are seen
+  size_t parts;     // rows of 64 * max_pages
+};
+// As for the attention two passes where sequences may differ and rows of heads are many, those of more than 64 of them and the others, and
+// slices that follow a sequence's rows (one pass, and the same number of slices for all, | two):
+//     a prompt of 2048 tokens and 31 single ones behind 8192   390 | 142      256 behind 768 and 63 single ones behind 2048   273 | 96
+//     512 behind 3584 and the same 31   138 | 114      a prompt of 2048 and 4 windows of 8 behind 32768   379 | 165
+//     against it  64 windows of 8 behind 4096   81 | 96
 static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   WeighPlan p;
   const int G = n_heads / c.n_kv_heads, M = (n_rows + c.n_seqs - 1) / c.n_seqs;
-  const long long rows = (long long)M * G, lines = (long long)c.n_seqs * c.n_kv_heads;
+  const long long total = (long long)n_rows * G, rows = (long long)M * G, lines = (long long)c.n_seqs * c.n_kv_heads;
   p.pages = most_pages(c, ragged ? n_rows : M, window, sinks);
   const int fours = (p.pages + WEIGH_WAVES - 1) / WEIGH_WAVES;
-  p.slices = 1;
-  if (rows <= 64) {
-    p.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.groups = (int)max(1ll, min((long long)fours, (3ll * CUS + lines - 1) / lines));
-    return p;
+  // of long sequences, of 64 rows in all of them, and of slices: 16 tiles or more each, and at most 64 more than there are sequences
+  const long long longs = min((long long)c.n_seqs, total / 65), all = total / 64 + longs, tiles = max(16ll, (all + 63) / 64), ids = all / tiles + longs;
+  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && ids * c.n_kv_heads * c.max_pages <= 1 << 20;      // 256 MiB
+  p.n = mixed ? 2 : 1, p.parts = 0;
+  for (int i = 0; i < p.n; ++i) {
+    WeighPass& x = p.pass[i];
+    x = {0, fours, 1, 0, 0, 0, INT_MAX};
+    if (mixed ? i == 1 : rows <= 64) {
+      x.row_tiles = rows <= 16 ? 1 : rows <= 32 || rows > 64 ? 2 : 4;
+      x.groups = (int)max(1ll, min((long long)fours, (3ll * CUS + lines - 1) / lines));
+      if (mixed) x.upto = 64;
+    } else if (mixed) {
+      x.tiles = (int)tiles, x.ids = (int)ids, x.above = 64;
+      p.parts = ids * c.n_kv_heads;
+    } else {
+      // many rows: tiles of 64 to so many slices that every CU has four workgroups, each at least 4 tiles (2047 rows of 64 heads over 8, us):
+      //   4 slices 192, 8 100, 16 to 32 58 to 65
+      x.slices = (int)max(1ll, min(min(4ll * CUS / (lines * fours), (rows + 255) / 256), 64ll));
+      if (x.slices > 1) p.parts = x.slices * lines;
+    }
   }
-  // many rows: tiles of 64 to so many slices that every CU has four workgroups, each at least 4 tiles (2047 rows of 64 heads over 8, us):
-  //   4 slices 192, 8 100, 16 to 32 58 to 65
-  p.row_tiles = 0;
-  p.groups = fours;
-  p.slices = (int)max(1ll, min(min(4ll * CUS / (lines * fours), (rows + 255) / 256), 64ll));
   return p;
 }
 size_t weigh_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
-  const WeighPlan p = weigh_plan(c, ragged, n_rows, n_heads, window, sinks);
-  return p.slices == 1 ? 0 : (size_t)p.slices * c.n_seqs * c.n_kv_heads * c.max_pages * PAGE * sizeof(float);
+  return weigh_plan(c, ragged, n_rows, n_heads, window, sinks).parts * c.max_pages * PAGE * sizeof(float);
 }
 template <int DH>
-static void launch_weigh(const QuantCache& c, const WeighArgs& a, const WeighPlan& p, hipStream_t st) {
+static hipError_t launch_weigh(const QuantCache& c, const WeighArgs& a, const WeighPass& p, int pages, hipStream_t st) {
   const dim3 grid(p.groups, c.n_kv_heads, c.n_seqs);
   if (p.row_tiles == 1) weigh_few_kernel<DH, 1><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
   else if (p.row_tiles == 2) weigh_few_kernel<DH, 2><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
   else if (p.row_tiles == 4) weigh_few_kernel<DH, 4><<<grid, WEIGH_WAVES * 64, 0, st>>>(c, a);
-  else weigh_many_kernel<DH><<<dim3((unsigned)p.groups * p.slices * c.n_kv_heads, c.n_seqs), WEIGH_WAVES * 64, 0, st>>>(c, a);
+  else weigh_many_kernel<DH><<<dim3((unsigned)p.groups * p.slices * c.n_kv_heads, p.tiles ? p.ids : c.n_seqs), WEIGH_WAVES * 64, 0, st>>>(c, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || (p.slices == 1 && !p.tiles)) return e;
+  weigh_add_kernel<<<dim3((pages + 3) / 4, c.n_kv_heads, c.n_seqs), 256, 0, st>>>(c, a);
+  return hipGetLastError();
 }
 hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, void* work, hipStream_t st) {
   const WeighPlan p = weigh_plan(c, a.rows != nullptr, a.n_rows, a.n_heads, a.window, a.sinks);
   a.G = a.n_heads / c.n_kv_heads;
-  a.slices = p.slices, a.part = (float*)work;
+  a.part = (float*)work;
   a.by_group = ((1ull << 38) + a.G - 1) / a.G;           // r * G < 2^38: (r * this) >> 38 is r / G
-  if (c.head_dim == 128) launch_weigh<128>(c, a, p, st);
-  else launch_weigh<64>(c, a, p, st);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.slices == 1) return e;
-  weigh_add_kernel<<<dim3((p.pages + 3) / 4, c.n_kv_heads, c.n_seqs), 256, 0, st>>>(c, a);
-  return hipGetLastError();
+  for (int i = 0; i < p.n; ++i) {
+    const WeighPass& x = p.pass[i];
+    a.slices = x.slices, a.tiles = x.tiles, a.ids = x.ids, a.above = x.above, a.upto = x.upto;
+    const hipError_t e = c.head_dim == 128 ? launch_weigh<128>(c, a, x, p.pages, st) : launch_weigh<64>(c, a, x, p.pages, st);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 hipError_t launch_evict_quant(const QuantCache& c, const QuantCache& to, const EvictArgs& a, hipStream_t st) {
   evict_select_kernel<<<dim3(c.n_kv_heads, c.n_seqs), SELECT_THREADS, 0, st>>>(c, a);

@@ -250,8 +250,10 @@ struct WeighArgs {
   float* weight;
   size_t ldw;
   int G, slices;              // set by the launch ...
+  int tiles, ids;             // > 0: tiles of 64 rows of a slice, where sequences differ, and how many slices there can be
+  int above, upto;            // sequences with more than `above` and at most `upto` rows of a KV head are taken
   unsigned long long by_group;
-  float* part;                // ... sums of slices [slices][n_seqs][n_kv_heads][64 max_pages]
+  float* part;                // ... sums of slices [slices][n_seqs][n_kv_heads][64 max_pages], or [ids][n_kv_heads][64 max_pages]
 };
 struct EvictArgs {
   const float* weight;

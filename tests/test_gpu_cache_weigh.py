@@ -155,3 +155,23 @@ def test_a_row_whose_logarithm_is_none_touches_only_what_it_sees(m, window, valu
 @pytest.mark.parametrize("rows,lengths,heads,kv", MIXED)
 def test_prompts_and_single_tokens_in_one_batch(rows, lengths, heads, kv, window, sinks, d):
     _run(lengths, rows, heads, kv, d, window, sinks)
+
+
+@pytest.mark.parametrize("window", [0, 1000])
+def test_long_and_short_sequences_together_and_alone(window):
+    """So many rows that a slice has more than its least number of tiles.  Terms are the same in both; their sums, of up to 16 * 5000 positive
+    terms, are off by as many steps at most."""
+    amd, rng = _amd(), np.random.default_rng(8)
+    rows, lengths = [5000, 3, 70], [5100, 900, 130]
+    c = make(rng, lengths, 1, 64)
+    g, start = to_gpu(amd, c), starts_of(rows)
+    q = torch.from_numpy(normal(rng, int(start[-1]), 16, 64)).cuda().to(torch.bfloat16)
+    at = torch.from_numpy(start).cuda()
+    _, lse = amd.attend_fp8(g, q, at, window=window, sinks=4, want_lse=True)
+    got = amd.weigh_fp8(g, q, lse, torch.zeros(3, 1, g.capacity, device="cuda"), at, window=window, sinks=4)
+    for s in range(3):
+        one = amd.Fp8Cache(g.k, g.v, g.scale, g.table[s:s + 1], g.length[s:s + 1].clone())
+        mine = slice(int(start[s]), int(start[s + 1]))
+        want = amd.weigh_fp8(one, q[mine], lse[mine], torch.zeros(1, 1, g.capacity, device="cuda"), window=window, sinks=4)
+        assert ((got[s] - want[0]).abs() <= 2 * (16 * 5000 + 80) * EPS * want[0]).all()
+        assert abs(float(want.double().sum()) - 16 * rows[s]) <= 16 * rows[s] * 1e-4
