@@ -283,3 +283,36 @@ def test_python_calls_refuse():
                  change(3, g.table[:, ::2]), change(3, g.table[:, :0]), change(4, g.length[:1]), change(4, g.length.cpu()), change(0, g.k[:-1])):
         with pytest.raises(ValueError):
             amd.Fp8Cache(*args)
+
+
+def test_a_captured_batch_whose_rows_move_between_its_sequences():
+    """Prompts and single tokens change places between replays: rows of all sequences are looked up when a graph runs."""
+    amd, rng = _amd(), np.random.default_rng(11)
+    heads, kv, d, n = 8, 2, 128, 700
+    g = to_gpu(amd, make(rng, [900, 900, 900, 900], kv, d))
+    q = torch.from_numpy(normal(rng, n, heads, d)).cuda().to(torch.bfloat16)
+    start = torch.tensor([0, 600, 601, 641, 700], dtype=torch.int32, device="cuda")
+    weight = torch.zeros(4, kv, g.capacity, device="cuda")
+
+    def step():
+        weight.zero_()
+        out, lse = amd.attend_fp8(g, q, start, want_lse=True)
+        return out, lse, amd.weigh_fp8(g, q, lse, weight, start)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for rows in ([600, 1, 40, 59], [1, 1, 697, 1], [0, 350, 0, 350], [40, 41, 578, 41], [600, 1, 40, 59]):
+        start.copy_(torch.from_numpy(starts_of(rows)))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.isfinite(got[0]).all()
+        assert ((got[2].double().sum(2) - torch.tensor(rows, device="cuda")[:, None] * 4).abs() <= 2800 * 1e-4).all()
