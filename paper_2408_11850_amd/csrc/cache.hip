@@ -1366,6 +1366,10 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(QuantCache
   for (int i = tid; i < a.recent; i += SELECT_THREADS) kept[a.budget - a.recent + i] = hi + i, to_weight[a.budget - a.recent + i] = weight[hi + i];
 }
 
+// What moves codes from a page's scale to 2^e.  A code that is not 0 is at least 2^-9, so that e is above its scale's exponent less 18: only
+// zeros, of which the new scale knows nothing, meet a factor beyond fp32, and it has to stay finite for them.
+__device__ __forceinline__ float moved_by(float scale, int e) { return fminf(scale * power(-e), 0x1p127f); }
+
 #define GATHER_THREADS 256
 template <int DH>
 __global__ __launch_bounds__(GATHER_THREADS) void evict_gather_kernel(QuantCache c, QuantCache o, EvictArgs a) {
@@ -1443,13 +1447,13 @@ __global__ __launch_bounds__(GATHER_THREADS) void evict_gather_kernel(QuantCache
   for (int i = 0; i < KSTEPS; ++i) {
     const int t = (i * GATHER_THREADS + tid) / CH, ch = tid % CH;
     if (t >= n) continue;
-    const float by = scales[t][0] * power(-e[0]);
+    const float by = moved_by(scales[t][0], e[0]);
     u32x4 x;
 #pragma unroll
     for (int y = 0; y < 4; ++y) x[y] = moved4(k[i][y], by);
     *reinterpret_cast<u32x4*>(o.k + block + t * DH + ch * 16) = x;
   }
-  const float by = scales[lane][1] * power(-e[1]);
+  const float by = moved_by(scales[lane][1], e[1]);
 #pragma unroll
   for (int i = 0; i < VS; ++i)
     vt[w * VS + i][lane] = (unsigned char)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8((int)v[i], 0) * by, 0.f, 0, false);
