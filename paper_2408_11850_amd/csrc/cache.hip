@@ -32,7 +32,8 @@ typedef __attribute__((ext_vector_type(8), aligned(2))) unsigned short bf16x8a;
 #define LOG2E 1.4426950408889634f
 #define LN2 0.6931471805599453f
 
-// eight codes times a power of two, exactly
+// Eight codes times a power of two, exactly.  Keys take their page's scale here, not in the factor of their scores: 2^-100 or 2^112 times a
+// softmax's scale may be 0 or infinite, and that times a hidden score, or a zero, NaN.
 __device__ __forceinline__ bf16x8 to_bf16x8(unsigned lo, unsigned hi, float scale) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
   const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
@@ -418,7 +419,7 @@ __device__ __forceinline__ u32x4 first_bytes(u32x4 v, int n) {
   }
   return v;
 }
-// A page's scores s (times `by` to the base 2; of the entries from `from` on) into weights pf, their sum l and reference m; o follows m.
+// A page's scores s (times `by`, the call's scale, to the base 2; of the entries from `from` on) into weights pf, their sum l and reference m; o follows m.
 // all: every row sees the whole page, else up to pos, above low or below sinks.
 template <int DH>
 __device__ __forceinline__ void softmax_step(f32x4 (&s)[4], f32x4 (&o)[DH / 16], float& m, float& l, bf16x8 (&pf)[2], float by, bool all,
@@ -559,7 +560,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
   for (int i = 0; i < n; ++i) {
     const int e0 = seen.page(i0 + i * phases) * PAGE;
     const bool there = id >= 0, more = i + 1 < n;
-    const float by = (there ? ks : 1.f) * a.scale_log2e, vscale = there ? vs : 0.f;
+    const float kscale = ks, vscale = there ? vs : 0.f;
     if (more) id = pages.get(i + 1, &ks, &vs);
     f32x4 s[RT][4];
 #pragma unroll
@@ -568,7 +569,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
       for (int rt = 0; rt < RT; ++rt) s[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < KS; ++j) {
-        const bf16x8 kf = to_bf16x8(kd[t][j >> 1][(j & 1) * 2], kd[t][j >> 1][(j & 1) * 2 + 1], 1.f);
+        const bf16x8 kf = to_bf16x8(kd[t][j >> 1][(j & 1) * 2], kd[t][j >> 1][(j & 1) * 2 + 1], kscale);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][j], s[rt][t], 0, 0, 0);
       }
@@ -584,7 +585,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
     bf16x8 pf[RT][2];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
-      softmax_step<DH>(s[rt], o[rt], m[rt], l[rt], pf[rt], by, all, e0 + 16 * g, pos[rt], a.window ? pos[rt] - a.window : INT_MIN, a.sinks);
+      softmax_step<DH>(s[rt], o[rt], m[rt], l[rt], pf[rt], a.scale_log2e, all, e0 + 16 * g, pos[rt], a.window ? pos[rt] - a.window : INT_MIN, a.sinks);
     // entries behind the last one, or of no page, may hold anything: 0 times a NaN would be one
     if (!there || e0 + PAGE > len) {
       const int live = there ? min(len - e0, PAGE) - 16 * g : 0;
@@ -982,7 +983,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
     int id = pages.get(0, &ks, &vs);
     for (int i = 0; i < mine; ++i) {
       const int e0 = seen.page(from + i * step) * PAGE;
-      const float by = id >= 0 ? ks * a.scale_log2e : NAN32;   // no such page: whoever sees it becomes NaN
+      const float kscale = ks, by = id >= 0 ? a.scale_log2e : NAN32;      // no such page: whoever sees it becomes NaN
       u32x4 now[4][DH / 64];
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -1001,7 +1002,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
         for (int rt = 0; rt < RT; ++rt) x[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-          const bf16x8 kf = to_bf16x8(now[t][j >> 1][(j & 1) * 2], now[t][j >> 1][(j & 1) * 2 + 1], 1.f);
+          const bf16x8 kf = to_bf16x8(now[t][j >> 1][(j & 1) * 2], now[t][j >> 1][(j & 1) * 2 + 1], kscale);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) x[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][j], x[rt], 0, 0, 0);
         }
@@ -1066,16 +1067,17 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   const int id = c.table[(size_t)s * c.table_ld + page];
   const bool there = (unsigned)id < (unsigned)c.n_pages;
   const size_t block = (size_t)(there ? id : 0) * c.n_kv_heads + h;
+  const float kscale = c.scale[block * 2];
   bf16x8 kf[2][KS];
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int j = 0; j < KS; j += 2) {                          // 16 bytes of a key are two operands: d in that order on both sides
       const u32x4 x = *reinterpret_cast<const u32x4*>(c.k + block * PAGE * DH + (t * 32 + r32) * DH + j * 16 + half * 16);
-      kf[t][j] = to_bf16x8(x[0], x[1], 1.f);
-      kf[t][j + 1] = to_bf16x8(x[2], x[3], 1.f);
+      kf[t][j] = to_bf16x8(x[0], x[1], kscale);
+      kf[t][j + 1] = to_bf16x8(x[2], x[3], kscale);
     }
-  const float by = (there ? c.scale[block * 2] : 1.f) * a.scale_log2e;
+  const float by = a.scale_log2e;
   if (!there) {                                                // no such page: whoever sees it becomes NaN
     constexpr unsigned NANS = 0x7fc07fc0u;
 #pragma unroll
