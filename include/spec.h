@@ -340,7 +340,7 @@ int spec_append_quant(const spec_quant_cache* cache, const void* k_dev, long lon
                       const int32_t* row_start_dev, int n_rows, const void* q_dev, long long ldq, int n_heads, float theta,
                       const int32_t* position_dev, void* q_out_dev, void* stream);
 /* out[n_rows][n_heads][head_dim] (bf16) = softmax(scale * q k) v over the entries that a row sees; q bf16, rows ldq elements apart
- * (a multiple of 8, rows at 16-byte addresses; 0: one row for all).  lse[n_rows][n_heads] (NULL: not wanted): natural logarithm of the sum of
+ * (a multiple of 8, rows at 16-byte addresses; 0: one row for all); scale positive, and finite times log2(e).  lse[n_rows][n_heads] (NULL: not wanted): natural logarithm of the sum of
  * exp(scale * q k).  Sums and statistics in fp32, weights rounded to bf16 for the product with the values.
  * work_dev: 16-byte aligned device memory of spec_attend_quant_workspace_bytes (the same arguments; 0: NULL will do), for this call alone
  * until it has run. */

@@ -1557,12 +1557,13 @@ static int check_cache_rows(const QuantCache& c, const int32_t* row_start, int n
   if (off_by(row_start, 4)) FAIL(SPEC_E_INVAL, "misaligned row_start");
   return SPEC_OK;
 }
+constexpr float LOG2E = 1.4426950408889634f;
 // q of attention: 16-byte loads; a window that hides nothing is none
 static int check_cache_q(const QuantCache& c, const void* q, long long ldq, int n_heads, float scale, int* window, int* sinks) {
   if (!q) FAIL(SPEC_E_INVAL, "null pointer");
   if ((ldq && ldq < (long long)n_heads * c.head_dim) || ldq % 8 || off_by(q, 16))
     FAIL(SPEC_E_INVAL, "rows of q start at multiples of 16 bytes and do not overlap");
-  if (!(scale > 0.0f) || scale == INFINITY) FAIL(SPEC_E_INVAL, "scale must be positive and finite");
+  if (!(scale > 0.0f) || scale * LOG2E == INFINITY) FAIL(SPEC_E_INVAL, "scale must be positive, and finite times log2(e)");
   if (*window < 0 || *sinks < 0) FAIL(SPEC_E_INVAL, "window and sinks must not be negative");
   if (*window >= c.max_pages * SPEC_PAGE_TOKENS) *window = 0;
   *sinks = *window ? std::min(*sinks, c.max_pages * SPEC_PAGE_TOKENS) : 0;
@@ -1649,7 +1650,7 @@ extern "C" int spec_attend_quant(const spec_quant_cache* cache, const void* q, l
     for (int j = 0; j < i; ++j) clash |= meet(to[j].p, to[j].bytes, to[i].p, to[i].bytes);
     if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
   }
-  AttendArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, (bf16*)out, lse,
+  AttendArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * LOG2E, window, sinks, (bf16*)out, lse,
                   0, 0, 0, 0, 0, 0, 0, nullptr, nullptr};
   HIPCHK(launch_attend_quant(c, a, work, (hipStream_t)stream));
   return SPEC_OK;
@@ -1676,7 +1677,7 @@ extern "C" int spec_weigh_quant(const spec_quant_cache* cache, const void* q, lo
     clash |= meets_cache(c, r.p, r.bytes) || meet(row_start, row_start ? (size_t)(c.n_seqs + 1) * 4 : 0, r.p, r.bytes) ||
              meet(lse, n * n_heads * 4, r.p, r.bytes) || meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, r.p, r.bytes);
   if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
-  WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * 1.4426950408889634f, window, sinks, lse, weight, (size_t)ldw,
+  WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * LOG2E, window, sinks, lse, weight, (size_t)ldw,
                  0, 0, 0, 0, 0, 0, 0, nullptr};
   HIPCHK(launch_weigh_quant(c, a, work, (hipStream_t)stream));
   return SPEC_OK;

@@ -1,0 +1,18 @@
+"""Workspaces of the calls on a paged 8-bit cache stay small, and a softmax scale is finite to the base 2 too (no GPU is needed)."""
+import ctypes as C
+
+import pytest
+
+from tests.test_abi_cache import LSE, OUT, Q, ROWS, W, WORK, _attend, _cache, amd  # noqa: F401
+
+
+def _sizes(amd, n, heads, window=0, sinks=0, rows=ROWS, **c):
+    lib, cache = amd.load_library(), _cache(amd, **c)
+    return [f(C.byref(cache), rows, n, heads, window, sinks) for f in (lib.spec_attend_quant_workspace_bytes, lib.spec_weigh_quant_workspace_bytes)]
+
+
+@pytest.mark.parametrize("by", [2.4e38, 3.4e38])
+def test_scales_that_overflow_to_the_base_2_are_refused(amd, by):  # noqa: F811
+    assert _attend(amd, by=by) == amd.SPEC_E_INVAL
+    cache = _cache(amd)
+    assert amd.load_library().spec_weigh_quant(C.byref(cache), Q, 1024, LSE, ROWS, 7, 8, by, 0, 0, W, 256, WORK, None) == amd.SPEC_E_INVAL
