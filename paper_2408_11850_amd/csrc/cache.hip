@@ -545,7 +545,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
   f32x4 o[RT][DT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    m[rt] = NONE, l[rt] = 0.f;
+    m[rt] = pos[rt] < 0 ? 0.f : NONE, l[rt] = 0.f;       // a lane without a row is not FAR: its neighbours' scores are as in a full tile
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[rt][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
 #pragma unroll
   for (int j = 0; j < KS; ++j)
     qf[j] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(a.q + (size_t)(sp.row + tok) * a.ldq + (size_t)hq * DH + half * 8 + j * 16));
-  float m = NONE, l = 0.f;
+  float m = pos < 0 ? 0.f : NONE, l = 0.f;      // as in tiles of 16: lanes without a row are not FAR
   f32x16 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x16{};
