@@ -1221,7 +1221,7 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCa
   if (slices == 1) {
     float* to = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw + e;
     *to = e < first ? *to + v : v;                             // an entry of these rows begins here
-  } else a.part[((a.tiles ? blockIdx.y : (size_t)slice * c.n_seqs + s) * c.n_kv_heads + h) * c.max_pages * PAGE + e] = v;
+  } else a.part[(((a.tiles ? blockIdx.y : (size_t)slice * c.n_seqs + s) * c.n_kv_heads + h) * a.pages + i) * PAGE + lane] = v;
 }
 
 __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs a) {
@@ -1243,8 +1243,8 @@ __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs 
   if (i >= seen.n) return;
   const int e = seen.page(i) * PAGE + threadIdx.x % PAGE;
   if (e >= rs.len) return;
-  const size_t block = (size_t)c.n_kv_heads * c.max_pages * PAGE, all = a.tiles ? block : c.n_seqs * block;
-  const float* p = a.part + ((size_t)from * c.n_kv_heads + h) * c.max_pages * PAGE + e;
+  const size_t block = (size_t)c.n_kv_heads * a.pages * PAGE, all = a.tiles ? block : c.n_seqs * block;
+  const float* p = a.part + (((size_t)from * c.n_kv_heads + h) * a.pages + i) * PAGE + threadIdx.x % PAGE;
   float* to = a.weight + ((size_t)s * c.n_kv_heads + h) * a.ldw + e;
   float v = e < rs.first ? *to : 0.f;                          // an entry of these rows begins here
 #pragma unroll 8
@@ -1585,7 +1585,7 @@ struct WeighPass {
 struct WeighPlan {
   WeighPass pass[2];
   int n, pages;     // most that are seen
-  size_t parts;     // rows of 64 * max_pages
+  size_t parts;     // rows of 64 * pages
 };
 // As for the attention two passes where sequences may differ and rows of heads are many, those of more than 64 of them and the others, and
 // slices that follow a sequence's rows (one pass, and the same number of slices for all, | two):
@@ -1600,7 +1600,7 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
   const int fours = (p.pages + WEIGH_WAVES - 1) / WEIGH_WAVES;
   // of long sequences, of 64 rows in all of them, and of slices: 16 tiles or more each, and at most 64 more than there are sequences
   const long long longs = min((long long)c.n_seqs, total / 65), all = total / 64 + longs, tiles = max(16ll, (all + 63) / 64), ids = all / tiles + longs;
-  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && ids * c.n_kv_heads * c.max_pages <= 1 << 20;      // 256 MiB
+  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && ids * c.n_kv_heads * p.pages <= 1 << 20;      // 256 MiB
   p.n = mixed ? 2 : 1, p.parts = 0;
   for (int i = 0; i < p.n; ++i) {
     WeighPass& x = p.pass[i];
@@ -1622,7 +1622,8 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
   return p;
 }
 size_t weigh_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
-  return weigh_plan(c, ragged, n_rows, n_heads, window, sinks).parts * c.max_pages * PAGE * sizeof(float);
+  const WeighPlan p = weigh_plan(c, ragged, n_rows, n_heads, window, sinks);
+  return p.parts * p.pages * PAGE * sizeof(float);
 }
 template <int DH>
 static hipError_t launch_weigh(const QuantCache& c, const WeighArgs& a, const WeighPass& p, int pages, hipStream_t st) {
@@ -1640,6 +1641,7 @@ hipError_t launch_weigh_quant(const QuantCache& c, WeighArgs a, void* work, hipS
   const WeighPlan p = weigh_plan(c, a.rows != nullptr, a.n_rows, a.n_heads, a.window, a.sinks);
   a.G = a.n_heads / c.n_kv_heads;
   a.part = (float*)work;
+  a.pages = p.pages;
   a.by_group = ((1ull << 38) + a.G - 1) / a.G;           // r * G < 2^38: (r * this) >> 38 is r / G
   for (int i = 0; i < p.n; ++i) {
     const WeighPass& x = p.pass[i];

@@ -1678,7 +1678,7 @@ extern "C" int spec_weigh_quant(const spec_quant_cache* cache, const void* q, lo
              meet(lse, n * n_heads * 4, r.p, r.bytes) || meets_strided(q, ldq, (long long)n_heads * c.head_dim, 2, n, r.p, r.bytes);
   if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
   WeighArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * LOG2E, window, sinks, lse, weight, (size_t)ldw,
-                 0, 0, 0, 0, 0, 0, 0, nullptr};
+                 0, 0, 0, 0, 0, 0, 0, 0, nullptr};
   HIPCHK(launch_weigh_quant(c, a, work, (hipStream_t)stream));
   return SPEC_OK;
 }

@@ -252,8 +252,9 @@ struct WeighArgs {
   int G, slices;              // set by the launch ...
   int tiles, ids;             // > 0: tiles of 64 rows of a slice, where sequences differ, and how many slices there can be
   int above, upto;            // sequences with more than `above` and at most `upto` rows of a KV head are taken
+  int pages;                  // that a sequence's rows can see at most
   unsigned long long by_group;
-  float* part;                // ... sums of slices [slices][n_seqs][n_kv_heads][64 max_pages], or [ids][n_kv_heads][64 max_pages]
+  float* part;                // ... sums of slices of the pages that are seen [slices][n_seqs][n_kv_heads][pages][64], or [ids][n_kv_heads][pages][64]
 };
 struct EvictArgs {
   const float* weight;

@@ -16,3 +16,12 @@ def test_scales_that_overflow_to_the_base_2_are_refused(amd, by):  # noqa: F811
     assert _attend(amd, by=by) == amd.SPEC_E_INVAL
     cache = _cache(amd)
     assert amd.load_library().spec_weigh_quant(C.byref(cache), Q, 1024, LSE, ROWS, 7, 8, by, 0, 0, W, 256, WORK, None) == amd.SPEC_E_INVAL
+
+
+@pytest.mark.parametrize("window,sinks", [(1000, 0), (64, 4), (1, 0)])
+@pytest.mark.parametrize("n_seqs,n,kv", [(1, 2047, 8), (1, 16384, 1), (3, 6000, 2), (200, 5000, 2)])
+def test_weights_under_a_window_do_not_grow_with_the_table(amd, n_seqs, n, kv, window, sinks):  # noqa: F811
+    for rows in (ROWS, None) if n % n_seqs == 0 else (ROWS,):
+        small, large = (_sizes(amd, n, 8 * kv, window, sinks, rows, n_seqs=n_seqs, n_kv_heads=kv, n_pages=100, max_pages=pages, table_ld=pages)[1]
+                        for pages in (2000, 1 << 17))
+        assert large == small <= 256 << 20
