@@ -648,6 +648,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
 #define MANY_WAVES 8
 #define MANY_ROWS (MANY_WAVES * 32)
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+__device__ __forceinline__ int many_tiles(int R, int above) { return R > above ? (R + MANY_ROWS - 1) / MANY_ROWS : 0; }
 
 template <int DH>
 __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCache c, AttendArgs a) {
@@ -656,9 +657,13 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
   constexpr bool BOTH = DH == 128;             // a thread brings 16 bytes of the keys and of the values; with 64 either
   __shared__ u32x4 ksh[2][2 * KS * KB], vsh[2][DT * 4 * VB];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r32 = lane & 31, half = lane >> 5;
-  const unsigned parts = c.n_kv_heads * a.splits, part = blockIdx.x % parts;
-  const int h = part % c.n_kv_heads, split = part / c.n_kv_heads, G = a.G;
-  Span sp = find_span(c, a.rows, a.n_rows, gridDim.x / parts - 1 - blockIdx.x / parts, [&](int M) { return M * G > a.above ? (M * G + MANY_ROWS - 1) / MANY_ROWS : 0; });
+  const int h = blockIdx.x % c.n_kv_heads, at = blockIdx.x / c.n_kv_heads, G = a.G;
+  int split = at % a.splits, splits = a.splits, tile = gridDim.x / (c.n_kv_heads * a.splits) - 1 - at / a.splits;       // the longest first
+  if (a.tiled) {                               // the others are not split
+    if (at < a.tiled * a.splits) tile = a.tiled - 1 - at / a.splits;
+    else tile = at - a.tiled * (a.splits - 1), split = 0, splits = 1;
+  }
+  Span sp = find_span(c, a.rows, a.n_rows, tile, [&](int M) { return many_tiles(M * G, a.above); });
   sp.s = __builtin_amdgcn_readfirstlane(sp.s);
   if (sp.s < 0) return;
   sp.t = __builtin_amdgcn_readfirstlane(sp.t), sp.row = __builtin_amdgcn_readfirstlane(sp.row), sp.M = __builtin_amdgcn_readfirstlane(sp.M);
@@ -667,7 +672,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
   const int len = max(given, 0), first = len - sp.M, R = sp.M * G;
   const int wg0 = sp.t * MANY_ROWS, wg_last = min(wg0 + MANY_ROWS, R) - 1, r0 = wg0 + w * 32, r_last = min(r0 + 32, R) - 1;
   const Seen seen = seen_pages(first + wg0 / G, beyond ? -1 : first + wg_last / G, a.window, a.sinks);
-  const int per = (seen.n + a.splits - 1) / a.splits, i0 = split * per, n = min(i0 + per, seen.n) - i0;
+  const int per = (seen.n + splits - 1) / splits, i0 = split * per, n = min(i0 + per, seen.n) - i0;
   const int see_all = first + r0 / G, low_all = a.window ? first + max(r_last, 0) / G - a.window + 1 : 0;
 
   const int r = r0 + r32;
@@ -828,7 +833,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
   l = __uint_as_float(other[0]) + __uint_as_float(other[1]);
   if (!valid) return;
   if (beyond) l = __uint_as_float(0x7fc00000u);
-  if (a.splits == 1) {
+  if (splits == 1) {
     const bool empty = pos < 0;
     const float inv = empty ? 0.f : 1.f / l;
 #pragma unroll
@@ -842,7 +847,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
       }
     if (a.lse && half == 0) a.lse[row_at] = empty ? -INFINITY : (m + __log2f(l)) * LN2;
   } else {
-    const size_t at = split * a.part_rows + row_at;
+    const size_t at = split * a.part_rows + (a.tiled ? ((size_t)tile * c.n_kv_heads + h) * MANY_ROWS + r - wg0 : row_at);
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -864,23 +869,22 @@ __global__ __launch_bounds__(MERGE_WAVES * 64) void attend_merge_kernel(QuantCac
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, way = w % WAVES * (64 / LANES) + lane / LANES;
   const size_t all = a.part_rows, at = (size_t)blockIdx.x * (MERGE_WAVES / WAVES) + w / WAVES;
   if (at >= all) return;                                                        // WAVES == 4: the whole workgroup
-  int row = (int)(at / a.n_heads);
-  if (a.per) {
+  int row = (int)(at / a.n_heads), head = (int)(at % a.n_heads);
+  if (a.tiled) {
+    const int h = (int)(at / MANY_ROWS) % c.n_kv_heads, tile = (int)(at / MANY_ROWS) / c.n_kv_heads;
+    const Span sp = find_span(c, a.rows, a.n_rows, tile, [&](int M) { return many_tiles(M * a.G, a.above); });
+    const int r = sp.t * MANY_ROWS + (int)(at % MANY_ROWS);
+    if (sp.s < 0 || r >= sp.M * a.G) return;
+    row = sp.row + r / a.G, head = h * a.G + r % a.G;
+  } else if (a.per) {
     const int s = row / a.per, first = min(max(a.rows[s], 0), a.n_rows), M = min(max(a.rows[s + 1], first), a.n_rows) - first;
     row -= s * a.per;
     if (row >= M || M * a.G > a.upto) return;
     row += first;
   } else if (a.rows) {
     if (row >= a.rows[c.n_seqs] || row < a.rows[0]) return;                   // rows of no sequence have no parts and stay as they are
-    if (a.above) {
-      int s = 0;                                                                // sequences that end in front of the row
-      for (int base = 0; base < c.n_seqs; base += 64)
-        s += __popcll(__ballot(base + lane < c.n_seqs && a.rows[min(base + lane, c.n_seqs - 1) + 1] <= row));
-      s = min(s, c.n_seqs - 1);
-      if ((min(a.rows[s + 1], a.n_rows) - max(a.rows[s], 0)) * a.G <= a.above) return;
-    }
   }
-  const size_t to = (size_t)row * a.n_heads + at % a.n_heads;
+  const size_t to = (size_t)row * a.n_heads + head;
   const float2 ml = lane < a.splits ? a.part_ml[lane * all + at] : make_float2(-INFINITY, 0.f);
   const float* from = a.part + at * DH + (lane % LANES) * 4;
   f32x4 ahead[AHEAD];
@@ -1510,7 +1514,7 @@ struct AttendPass {
   int row_waves;    // waves of a workgroup that have rows of their own; the others take other pages of theirs
   int splits;
   long long tiles;
-  int above, upto, per;
+  int above, upto, per, tiled;
   size_t part_rows;
 };
 struct AttendPlan {
@@ -1530,7 +1534,6 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
     x.row_tiles = many ? 0 : mixed || (rows > 16 && waves > 12ll * CUS) ? 2 : 1;
     x.row_waves = mixed ? 0 : rows > 64 ? 4 : rows > 32 ? 2 : 1;
     x.above = mixed && many ? SHORT : 0, x.upto = mixed && !many ? SHORT : INT_MAX, x.per = mixed && !many ? SHORT / G : 0;
-    x.part_rows = (size_t)(x.per ? (long long)c.n_seqs * x.per : n_rows) * n_heads;
     // rows of a workgroup, the most tiles there can be, and how many there will be about: a row of every sequence is not the long ones'
     const int tile = many ? MANY_ROWS : 16 * x.row_tiles * max(x.row_waves, 1);
     x.tiles = !mixed ? most_tiles(c, ragged, n_rows, G, tile) : many ? total / (MANY_ROWS / 2) : 2ll * c.n_seqs;
@@ -1539,6 +1542,10 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
     const long long most = many ? pages / 8 : (pages + phases - 1) / phases;
     const long long want = many ? CUS / groups : (CUS + groups - 1) / groups;
     x.splits = (int)max(1ll, min(min(want, most), (long long)MERGE_PARTS));
+    // parts of a mixed call's long sequences are for as many tiles as there will be about, so that they stay below 256 * MANY_ROWS rows whatever
+    // the call's rows are; tiles beyond, where other sequences have none, are not split
+    x.tiled = mixed && many && x.splits > 1 ? (int)min(about, x.tiles) : 0;
+    x.part_rows = x.tiled ? (size_t)x.tiled * c.n_kv_heads * MANY_ROWS : (size_t)(x.per ? (long long)c.n_seqs * x.per : n_rows) * n_heads;
   }
   return p;
 }
@@ -1551,7 +1558,7 @@ size_t attend_quant_work_bytes(const QuantCache& c, bool ragged, int n_rows, int
 }
 template <int DH>
 static hipError_t launch_attend(const QuantCache& c, const AttendArgs& a, const AttendPass& p, hipStream_t st) {
-  const unsigned groups = (unsigned)(p.tiles * c.n_kv_heads * p.splits);
+  const unsigned groups = (unsigned)((p.tiled ? p.tiled * (p.splits - 1) + p.tiles : p.tiles * p.splits) * c.n_kv_heads);
   if (p.row_tiles == 1) attend_few_kernel<DH, 1><<<groups, FEW_WAVES * 64, 0, st>>>(c, a);
   else if (p.row_tiles == 2) attend_few_kernel<DH, 2><<<groups, FEW_WAVES * 64, 0, st>>>(c, a);
   else attend_many_kernel<DH><<<groups, MANY_WAVES * 64, 0, st>>>(c, a);
@@ -1568,7 +1575,7 @@ hipError_t launch_attend_quant(const QuantCache& c, AttendArgs a, void* work, hi
   a.part = (float*)work;
   for (int i = 0; i < p.n; ++i) {
     const AttendPass& x = p.pass[i];
-    a.splits = x.splits, a.row_waves = x.row_waves, a.above = x.above, a.upto = x.upto, a.per = x.per, a.part_rows = x.part_rows;
+    a.splits = x.splits, a.row_waves = x.row_waves, a.above = x.above, a.upto = x.upto, a.per = x.per, a.tiled = x.tiled, a.part_rows = x.part_rows;
     a.part_ml = (float2*)(a.part + x.splits * x.part_rows * c.head_dim);
     const hipError_t e = c.head_dim == 128 ? launch_attend<128>(c, a, x, st) : launch_attend<64>(c, a, x, st);
     if (e != hipSuccess) return e;

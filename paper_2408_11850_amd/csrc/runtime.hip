@@ -1651,7 +1651,7 @@ extern "C" int spec_attend_quant(const spec_quant_cache* cache, const void* q, l
     if (clash) FAIL(SPEC_E_INVAL, "results and workspace must not overlap each other or what is read");
   }
   AttendArgs a = {row_start, n_rows, n_heads, (const bf16*)q, (size_t)ldq, scale * LOG2E, window, sinks, (bf16*)out, lse,
-                  0, 0, 0, 0, 0, 0, 0, nullptr, nullptr};
+                  0, 0, 0, 0, 0, 0, 0, 0, nullptr, nullptr};
   HIPCHK(launch_attend_quant(c, a, work, (hipStream_t)stream));
   return SPEC_OK;
 }

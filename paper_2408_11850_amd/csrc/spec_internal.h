@@ -235,6 +235,7 @@ struct AttendArgs {
   int row_waves;              // ... 0: by the sequence
   int above, upto;            // ... sequences with more than `above` and at most `upto` rows of a KV head are taken
   int per;                    // > 0: their parts stand `per` rows apart, else where the call's rows do
+  int tiled;                  // > 0: parts of so many tiles of 256 rows and each of their KV heads, the other tiles have none
   size_t part_rows;           // rows of heads with a part
   float* part;                // parts [splits][part_rows][head_dim] and their maxima and sums
   float2* part_ml;

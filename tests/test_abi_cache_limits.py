@@ -18,6 +18,15 @@ def test_scales_that_overflow_to_the_base_2_are_refused(amd, by):  # noqa: F811
     assert amd.load_library().spec_weigh_quant(C.byref(cache), Q, 1024, LSE, ROWS, 7, 8, by, 0, 0, W, 256, WORK, None) == amd.SPEC_E_INVAL
 
 
+@pytest.mark.parametrize("pages", [65, 513, 4097])
+@pytest.mark.parametrize("heads,kv", [(64, 8), (32, 32), (32, 4), (8, 1)])
+@pytest.mark.parametrize("tokens", [129, 256, 257, 512, 1000, 2048, 10000])
+def test_attention_of_single_tokens_needs_little(amd, tokens, heads, kv, pages):  # noqa: F811
+    """Parts are for as many tiles of 256 rows as leave compute units free: two for each of 256 of them, with 130 floats a row of 128."""
+    size = _sizes(amd, tokens, heads, n_seqs=tokens, n_kv_heads=kv, n_pages=100, max_pages=pages, table_ld=pages)[0]
+    assert size <= 2 * 256 * 256 * 130 * 4
+
+
 @pytest.mark.parametrize("window,sinks", [(1000, 0), (64, 4), (1, 0)])
 @pytest.mark.parametrize("n_seqs,n,kv", [(1, 2047, 8), (1, 16384, 1), (3, 6000, 2), (200, 5000, 2)])
 def test_weights_under_a_window_do_not_grow_with_the_table(amd, n_seqs, n, kv, window, sinks):  # noqa: F811
