@@ -1235,12 +1235,13 @@ __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs 
   int slices = a.slices, from = s;                             // the first of its slices
   if (a.tiles) {
     slices = slices_of(a, rs.M), from = 0;
+    if (slices < 2) return;                                    // written by its only slice, or by the other pass
     for (int base = 0; base < s; base += 64) {
       const int x = base + (int)(threadIdx.x & 63), first = x < s ? min(max(a.rows[x], 0), a.n_rows) : 0;
       const int mine = x < s ? slices_of(a, min(max(a.rows[x + 1], first), a.n_rows) - first) : 0;
       from += __builtin_amdgcn_readlane(lanes_upto(mine), 63);
     }
-    if (slices < 2 || from + slices > a.ids) return;           // written by its only slice; beyond: row numbers that do not rise
+    if (from + slices > a.ids) return;                         // beyond: row numbers that do not rise
   }
   const Seen seen = seen_pages(rs.first, rs.len - 1, a.window, a.sinks);
   const int i = blockIdx.x * 4 + threadIdx.x / PAGE;
@@ -1504,10 +1505,13 @@ static long long mean_tiles(const QuantCache& c, int n_rows, int G, int tile) {
 //     8 sequences, 64 rows behind 4096   27.0 | 28.6      64 rows behind 8192   18.9 | 23.9      windows of 8 requests   18.7 | 22.2
 //     against it  64 rows behind 131072   76.9 | 71.3
 // One launch (and a merge) takes all sequences, or where they may differ two of them those of more than SHORT rows of a KV head and the others.
-// The host does not know which there are, so rows of heads have to be so many that a launch with nothing to do does not count (one | two):
-//     a prompt of 2048 tokens and 31 single ones behind 8192   332 | 192      a prompt of 300 and 16 single ones behind 4000   102 | 57
-//     512 behind 3584 and the same 31   275 | 188      a prompt of 2048 and 4 windows of 8 behind 32768   889 | 172
-//     against it  256 behind 768 and 63 single ones behind 2048   62 | 78      8 times 64 behind 2048   59 | 63      64 windows of 8   127 | 131
+// The host does not know which there are: rows of heads have to be so many that a launch with nothing to do counts for little, and more than a
+// row of every sequence leaves enough for a long one (single tokens stay in one launch).  One | two:
+//     a prompt of 2048 tokens and 31 single ones behind 8192   325 | 186      a prompt of 300 and 16 single ones behind 4000   145 | 93
+//     512 behind 3584 and the same 31   275 | 193      a prompt of 2048 and 4 windows of 8 behind 32768   877 | 169
+//     a prompt of 300 behind 16384 and 1000 single ones behind 512   620 | 462
+//     against it  256 behind 768 and 63 single ones behind 2048   63 | 80      8 times 64 behind 2048   56 | 63      64 windows of 8   129 | 134
+//     2048 windows of 2 behind 512   758 | 770      512 single tokens behind 2048 (were they not left out)   395 | 407      2048 behind 512   615 | 696
 #define SHORT 160
 struct AttendPass {
   int row_tiles;    // of 16 rows in a wave; 0: many rows
@@ -1526,7 +1530,7 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
   const int G = n_heads / c.n_kv_heads;
   const long long total = (long long)n_rows * G, rows = (total + c.n_seqs - 1) / c.n_seqs;      // of a sequence, in the mean
   const long long waves = mean_tiles(c, n_rows, G, 16) * c.n_kv_heads * most_pages(c, (int)(rows / G) + 1, window, sinks);
-  const bool mixed = ragged && c.n_seqs > 1 && G <= SHORT && total > 2048 && waves > 8ll * CUS;
+  const bool mixed = ragged && c.n_seqs > 1 && G <= SHORT && total > 2048 && total - (long long)c.n_seqs * G > SHORT && waves > 8ll * CUS;
   p.n = mixed ? 2 : 1;
   for (int i = 0; i < p.n; ++i) {
     AttendPass& x = p.pass[i];
@@ -1536,7 +1540,7 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
     x.above = mixed && many ? SHORT : 0, x.upto = mixed && !many ? SHORT : INT_MAX, x.per = mixed && !many ? SHORT / G : 0;
     // rows of a workgroup, the most tiles there can be, and how many there will be about: a row of every sequence is not the long ones'
     const int tile = many ? MANY_ROWS : 16 * x.row_tiles * max(x.row_waves, 1);
-    x.tiles = !mixed ? most_tiles(c, ragged, n_rows, G, tile) : many ? total / (MANY_ROWS / 2) : 2ll * c.n_seqs;
+    x.tiles = !mixed ? most_tiles(c, ragged, n_rows, G, tile) : many ? total / (MANY_ROWS / 2) : c.n_seqs + min((long long)c.n_seqs, total / 129);
     const long long about = !mixed ? mean_tiles(c, n_rows, G, tile) : many ? max(1ll, (total - (long long)c.n_seqs * G + tile - 1) / tile) : c.n_seqs;
     const long long groups = about * c.n_kv_heads, pages = most_pages(c, (tile + G - 1) / G, window, sinks), phases = FEW_WAVES / max(x.row_waves, 1);
     const long long most = many ? pages / 8 : (pages + phases - 1) / phases;
@@ -1596,9 +1600,11 @@ struct WeighPlan {
 };
 // As for the attention two passes where sequences may differ and rows of heads are many, those of more than 64 of them and the others, and
 // slices that follow a sequence's rows (one pass, and the same number of slices for all, | two):
-//     a prompt of 2048 tokens and 31 single ones behind 8192   390 | 142      256 behind 768 and 63 single ones behind 2048   273 | 96
-//     512 behind 3584 and the same 31   138 | 114      a prompt of 2048 and 4 windows of 8 behind 32768   379 | 165
-//     against it  64 windows of 8 behind 4096   81 | 96
+//     a prompt of 2048 tokens and 31 single ones behind 8192   386 | 132      256 behind 768 and 63 single ones behind 2048   274 | 96
+//     512 behind 3584 and the same 31   137 | 109      a prompt of 2048 and 4 windows of 8 behind 32768   374 | 156
+//     a prompt of 300 behind 16384 and 1000 single ones behind 512   14680 | 1157
+//     against it  64 windows of 8 behind 4096   79 | 94      2048 windows of 2 behind 512   244 | 498: workgroups that look for long sequences
+//     512 single tokens behind 2048 (were they not left out)   236 | 278      2048 behind 512   237 | 382
 static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   WeighPlan p;
   const int G = n_heads / c.n_kv_heads, M = (n_rows + c.n_seqs - 1) / c.n_seqs;
@@ -1607,7 +1613,8 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
   const int fours = (p.pages + WEIGH_WAVES - 1) / WEIGH_WAVES;
   // of long sequences, of 64 rows in all of them, and of slices: 16 tiles or more each, and at most 64 more than there are sequences
   const long long longs = min((long long)c.n_seqs, total / 65), all = total / 64 + longs, tiles = max(16ll, (all + 63) / 64), ids = all / tiles + longs;
-  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && ids * c.n_kv_heads * p.pages <= 1 << 20;      // 256 MiB
+  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && total - (long long)c.n_seqs * G > 64 &&
+                     ids * c.n_kv_heads * p.pages <= 1 << 20;      // 256 MiB
   p.n = mixed ? 2 : 1, p.parts = 0;
   for (int i = 0; i < p.n; ++i) {
     WeighPass& x = p.pass[i];

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import cache8
-from tests.cache8 import bf16, check_attention, make, normal, starts_of, to_gpu
+from tests.cache8 import EPS, bf16, check_attention, make, normal, starts_of, to_gpu
 from tests.util import gpu_available
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs a GPU")]
@@ -48,6 +48,26 @@ def test_attention(kind, heads, kv, d, window, sinks):
     check_attention(out[:n].float().cpu().numpy(), lse[:n].cpu().numpy(), want, want_lse, mass, size, d, max(lengths))
     again, lse2 = amd.attend_fp8(g, qg, sg, window=window, sinks=sinks, want_lse=True)
     assert torch.equal(again[:n], out[:n]) and torch.equal(lse2[:n], lse[:n])
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (600, 3)])
+@pytest.mark.parametrize("heads,kv,d", [(8, 2, 64), (16, 2, 128), (20, 1, 64)])
+@pytest.mark.parametrize("kind", ["nobody long", "one long among single tokens", "one long among none", "several among none", "long ones only"])
+def test_weights(kind, heads, kv, d, window, sinks):
+    """Terms off by (d + 5) steps of their exponents' magnitudes; sums of positive terms, as deep as a sequence's rows at most."""
+    import paper_2408_11850_amd as amd
+    amd.load_library()
+    rng = np.random.default_rng(heads)
+    rows, lengths = _rows(kind)
+    c = make(rng, lengths, kv, d, junk=True)
+    start, n = starts_of(rows), sum(rows)
+    q, lse = bf16(normal(rng, n, heads, d)), (4 + normal(rng, n, heads)).astype(np.float32)
+    weight = rng.random((len(rows), kv, c.table.shape[1] * 64)).astype(np.float32)
+    up = lambda x: torch.from_numpy(x).cuda()
+    got = amd.weigh_fp8(to_gpu(amd, c), up(q).to(torch.bfloat16), up(lse), up(weight), up(start), window=window, sinks=sinks).cpu().numpy()
+    want, slack = cache8.weigh(c, start, q, lse, weight, d ** -0.5, window, sinks)
+    bound = slack * (d + 5) * EPS * 1.1 + want * (max(rows) * heads // kv + 48) * EPS
+    assert (np.abs(got - want) <= bound + 1e-37).all()
 
 
 def test_a_captured_call_whose_long_rows_outgrow_its_parts():
