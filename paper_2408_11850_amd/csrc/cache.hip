@@ -444,21 +444,22 @@ __device__ __forceinline__ void softmax_step(f32x4 (&s)[4], f32x4 (&o)[DH / 16],
   mx = groups_max(mx) * by;
   if (__any(mx > m + LAG)) {                       // maxima settle after a few pages
     asm volatile("" ::: "memory");                 // and what is to do then stays here
-    const float m_new = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - m_new);
-    m = m_new;
+    const float m_new = mx > m + LAG ? mx : m, corr = __builtin_amdgcn_exp2f(m - m_new);      // of the rows that need it: no row's bits
+    m = m_new;                                                                               // depend on its neighbours
     l *= corr;
 #pragma unroll
     for (int d = 0; d < DH / 16; ++d) o[d] *= corr;
   }
   // the product with the scale in one rounding with the difference, unless its own rounding, left in the largest score, would count
+  const bool far = fabsf(m) > FAR;
   float mul = by, less = m;
-  if (__any(fabsf(less) > FAR)) {
+  if (__any(far)) {
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) s[t][x] = difference(s[t][x], by, less);
-    mul = 1.f, less = 0.f;
+      for (int x = 0; x < 4; ++x) s[t][x] = far ? difference(s[t][x], by, m) : s[t][x];
+    mul = far ? 1.f : by, less = far ? 0.f : m;
   }
   float sum = 0.f;
 #pragma unroll
@@ -764,21 +765,22 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
     mx = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])) * a.scale_log2e;
     if (__any(mx > m + LAG)) {                 // maxima settle after a few pages
       asm volatile("" ::: "memory");           // and what is to do then stays here
-      const float m_new = fmaxf(m, mx), corr = __builtin_amdgcn_exp2f(m - m_new);
+      const float m_new = mx > m + LAG ? mx : m, corr = __builtin_amdgcn_exp2f(m - m_new);      // of the rows that need it
       m = m_new;
       l *= corr;
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] *= corr;
     }
     // the product with the scale in one rounding with the difference, unless its own rounding, left in the largest score, would count
+    const bool far = fabsf(m) > FAR;
     float by = a.scale_log2e, less = m;
-    if (__any(fabsf(m) > FAR)) {
+    if (__any(far)) {
       asm volatile("" ::: "memory");
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int x = 0; x < 16; ++x) s[t][x] = difference(s[t][x], a.scale_log2e, m);
-      by = 1.f, less = 0.f;
+        for (int x = 0; x < 16; ++x) s[t][x] = far ? difference(s[t][x], a.scale_log2e, m) : s[t][x];
+      by = far ? 1.f : by, less = far ? 0.f : m;
     }
     scores(ahead, (i + 1) & 1);                // behind the last page: of nothing, for nobody
     bf16x8 pf[4];
