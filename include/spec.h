@@ -326,7 +326,7 @@ typedef struct {
   const int32_t* table; /* [n_seqs][table_ld]: page of entries 64 i .. 64 i + 63 of a sequence */
   int32_t* len;         /* [n_seqs] */
   int n_pages, n_kv_heads, head_dim, n_seqs;
-  int max_pages;        /* columns of the table in use */
+  int max_pages;        /* columns of the table in use: no more than sequences will reach, as splits and slices go by it */
   int table_ld;         /* its row stride */
 } spec_quant_cache;
 

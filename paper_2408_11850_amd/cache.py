@@ -21,7 +21,8 @@ class Fp8Cache:
 
     k e4m3 [n_pages][heads][64][d]; v e4m3 [n_pages][heads][d][64]; scale fp32 [n_pages][heads][2] (of the keys, of the values);
     table int32 [n_seqs][max_pages] (any row stride); length int32 [n_seqs], the entries of every sequence with the rows of the
-    calls that follow.  All contiguous but the table's rows, on one GPU.  Their values may change at any time, as the calls on a stream see
+    calls that follow.  All contiguous but the table's rows, on one GPU.  How calls are split goes by the table's width, so that a table
+    for the longest text is better given as far as it is needed, table[:, :n].  Their values may change at any time, as the calls on a stream see
     them; other tensors need another Fp8Cache."""
 
     __slots__ = ("k", "v", "scale", "table", "length", "device", "heads", "d", "n_seqs", "capacity", "desc", "ref", "sizes")

@@ -25,8 +25,9 @@ typedef __attribute__((ext_vector_type(8), aligned(2))) unsigned short bf16x8a;
 #define FINITE_MAX 0x1p120f         // keys and values from here on count as infinite: their scales would leave fp32's range
 #define NONE (-3.0e38f)             // running maximum of a row that has seen nothing; scores below it cannot be told from it
 // A row's reference stays until a score is so far above it (to the base 2): weights reach 2^8.  Their rounding to bf16 is as large relative to
-// them as ever, but the largest is no longer 1 and free of it: 0.0021 instead of 0.0018 off in the 2-norm for a 4095-token prompt, whose
-// accumulators a step in two would multiply otherwise.
+// them as ever, but the largest is no longer 1 and free of it.  Distance from 64 bits in the 2-norm for normal q and codes, of which the
+// result's own rounding is 0.0017: 0.0021 to 0.0024, with the exact maximum 0.0020 to 0.0023, with weights in two bf16 parts that rounding alone.
+// us (this | exact maximum | two parts): a 4095-token prompt 283 | 299 | 395, 8 rows behind 131072 73 | 75 | 88, one token 9.6 | 9.5 | 10.1.
 #define LAG 8.f
 #define FAR 0x1p20f                 // references from here on: see where it is used
 #define LOG2E 1.4426950408889634f
@@ -178,8 +179,8 @@ struct PageList {
 // ---- append ---------------------------------------------------------------------------------------------------------------
 // A workgroup takes the entries of a call that fall into one page: keys and values of a KV head, or eight query heads.  The
 // angles' cosines and sines are made once per workgroup, in revolutions in 64 bits up to the reduction.
-// Bound by memory for many rows: 4095 tokens of 8 heads with 64 query heads (159 MB read and written) 32.4 us, 4.9 TB/s.  One token: 5.2 us,
-// the trips to its length, its page's id, the scale, and the codes that move if it grows.
+// Bound by memory for many rows: 4095 tokens of 8 heads with 64 query heads (159 MB read and written) 32.8 us, 4.8 TB/s; rows in fp32 (243 MB)
+// 41.6 us, 5.8 TB/s.  One token: 5.1 us, the trips to its length, its page's id, the scale, and the codes that move if it grows.
 template <int T>
 __device__ __forceinline__ void load8(const void* p, size_t at, float (&v)[8]) {
   if (T == SPEC_F32) {
@@ -497,8 +498,9 @@ __device__ __forceinline__ void store_rows(const AttendArgs& a, const f32x4 (&o)
 // Few rows of a KV head: the codes go to registers as operands, RT tiles of 16 rows share them in a wave.  The waves of a workgroup have
 // row_waves sets of rows and take pages in turn.  No LDS on the way, as no other wave wants these codes: pages that four waves share
 // through LDS, a tile of rows each, were slower (81 us against 69 for 64 rows of heads behind 131072), since every wave converts them.
-// One row each of 16 sequences, 32 heads: 627 MB in 115 us, 5.5 TB/s.  64 rows of 8 heads behind 131072: 268 MB in 69 us, 3.9 TB/s, what
-// registers for one page in flight and two waves a SIMD let through.  One token behind 4096: 6.7 us, four dependent trips to memory.
+// One row each of 16 sequences, 32 heads: 627 MB in 115 us, 5.4 TB/s.  64 rows of 8 heads behind 131072: 268 MB in 69 us, 3.9 TB/s, with one wave
+// a SIMD, a page of it in flight, vector instructions in 40 % of the cycles and products in 23.  One token behind 4096: 6.9 us, four dependent
+// trips to memory.
 #define FEW_WAVES 4
 template <int DH, int RT>
 __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_kernel(QuantCache c, AttendArgs a) {
@@ -641,9 +643,9 @@ __global__ __launch_bounds__(FEW_WAVES * 64, RT == 1 ? 3 : 2) void attend_few_ke
 // way to LDS.  S^T = K Q^T and O^T += V^T P^T, 32 x 32 x 16: row 8 b + 4 c + i of a key tile is entry 16 (b / 2) + 8 c + 4 (b % 2) + i, so that
 // again a lane's scores are the operand it gives, here against eight neighbouring entries of a value's row.  Scores of the next page
 // are formed while the softmax of the present one runs: keys are in LDS one page ahead of values.
-// A prompt of 4095 tokens, 64 heads over 8, d 128: 290 to 330 us, up to 0.96 PFLOP/s; 2.0 us per page, of which reading operands from LDS
-// would take 1.0 alone, the products 0.9, softmax and conversion 1.1.  It is no single one of them: without products, without LDS reads,
-// without the maxima or without the barrier the time stays, without conversion it falls by 15 %.  Slower were 64 rows a wave on half
+// A prompt of 4095 tokens, 64 heads over 8, d 128: 284 us back to back, 0.98 PFLOP/s (334 under the tracer).  Of a compute unit's busy cycles
+// the products take 44 %, vector instructions 45, LDS 28, partly one behind the other; it is no single one of them: without products, without
+// LDS reads, without the maxima or without the barrier the time stays, without conversion it falls by 15 %.  Slower were 64 rows a wave on half
 // the waves (538: accumulators and queries exceed the registers that vector instructions reach), two workgroups of 4 waves (317
 // against 303: each converts the page), values a page behind, so that all products run beside the softmax (317).
 #define MANY_WAVES 8
@@ -860,7 +862,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64, 2) void attend_many_kernel(QuantCa
 }
 
 // Parts of a row's attention together.  WAVES waves have a row and head: a lane the maximum and sum of a part (there are at most 64), then
-// 4 elements of some of the parts, the first eight of them asked for beside the sums.  64 parts of 64 rows: 4.4 to 5 us (a wave that adds
+// 4 elements of some of the parts, the first eight of them asked for beside the sums.  64 parts of 64 rows: 4.8 us (a wave that adds
 // one part after the other: 62); two trips to memory and the launch.
 #define MERGE_WAVES 4
 #define MERGE_PARTS 64
@@ -952,7 +954,7 @@ __device__ __forceinline__ int slices_of(const WeighArgs& a, int M) {
 
 // Few rows: their queries stay in registers, up to RT tiles of 16 at a time, and a wave goes over pages.  S^T = K Q^T as in the attention:
 // a lane's scores belong to one row, so that sums over the rows of a tile are sums over 16 lanes, once per page.  One row each of 8
-// sequences, 64 heads over 8, 34 MB of keys: 13 us, trips to memory before the first page and one or two pages a wave.
+// sequences, 64 heads over 8, 34 MB of keys: 13.6 us, trips to memory before the first page and one or two pages a wave.
 #define WEIGH_WAVES 4
 template <int DH, int RT>
 __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCache c, WeighArgs a) {
@@ -1046,8 +1048,9 @@ __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_few_kernel(QuantCac
 
 // Many rows: a wave keeps the 64 keys of a page as operands and the workgroup goes over tiles of 64 rows, whose queries, logarithms and
 // entries pass through LDS.  S = Q K^T, 32 x 32 x 16: a lane's scores belong to one entry.  The tiles that see a group of pages are dealt to
-// `slices` workgroups, or to as many of them as `a.tiles` asks for where sequences differ; sums of slices are added in their order.  2047 rows, 64 heads over 8, 34.9 GFLOP: 56 us and 4.8 for the slices' sums,
-// about 6 us of it before the first product and nine tiles behind; three workgroups a CU do not fit the registers (142, spilling).
+// `slices` workgroups, or to as many of them as `a.tiles` asks for where sequences differ; sums of slices are added in their order.  2047 rows,
+// 64 heads over 8, 34.9 GFLOP: 61 us traced (58 back to back, with 4.8 for the slices' sums), products in 35 % of the cycles, vector instructions in
+// 52; about 6 us of it before the first product and nine tiles behind; three workgroups a CU do not fit the registers (142, spilling).
 template <int DH>
 __global__ __launch_bounds__(WEIGH_WAVES * 64, 2) void weigh_many_kernel(QuantCache c, WeighArgs a) {
   constexpr int KS = DH / 16, QB = 66, CH = DH / 8, LOADS = 64 * CH / (WEIGH_WAVES * 64);
@@ -1263,7 +1266,7 @@ __global__ __launch_bounds__(256) void weigh_add_kernel(QuantCache c, WeighArgs 
 // One workgroup per sequence and head finds the weight of the last entry that is kept, 11 bits of an ordered key at a time (the first
 // ones are sign, exponent and two more, so that few entries of a wave meet in a counter), and lists the entries that are kept in their
 // order; then a workgroup per page of 64 of them moves their codes.  A wave has a stretch of entries, in registers where that is up to 1024.
-// Select: 4096 entries of one sequence 10 us, 16 ragged sequences of up to 16384 17 us; barriers and counters in LDS.  Gather of 2048
+// Select: 4096 entries of one sequence 11 us, 16 ragged sequences of up to 16384 17 us; barriers and counters in LDS.  Gather of 2048
 // entries of those 16, 8 heads of 128: 55 us; a value's elements are 64 bytes apart, so nearly all pages of values are read whole.
 #define SELECT_THREADS 1024
 #define SELECT_WAVES (SELECT_THREADS / 64)
@@ -1631,6 +1634,8 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
     } else {
       // many rows: tiles of 64 to so many slices that every CU has four workgroups, each at least 4 tiles (2047 rows of 64 heads over 8, us):
       //   4 slices 192, 8 100, 16 to 32 58 to 65
+      // The table's width stands for the length, which the host does not know.  The same rows behind tables of 33 pages 62, 65 95, 129 157,
+      // 513 and more 373: columns that are not needed yet are better left out of max_pages.
       x.slices = (int)max(1ll, min(min(4ll * CUS / (lines * fours), (rows + 255) / 256), 64ll));
       if (x.slices > 1) p.parts = x.slices * lines;
     }
