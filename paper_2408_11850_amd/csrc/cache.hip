@@ -1510,8 +1510,9 @@ static long long mean_tiles(const QuantCache& c, int n_rows, int G, int tile) {
 //     8 sequences, 64 rows behind 4096   27.0 | 28.6      64 rows behind 8192   18.9 | 23.9      windows of 8 requests   18.7 | 22.2
 //     against it  64 rows behind 131072   76.9 | 71.3
 // One launch (and a merge) takes all sequences, or where they may differ two of them those of more than SHORT rows of a KV head and the others.
-// The host does not know which there are: rows of heads have to be so many that a launch with nothing to do counts for little, and more than a
-// row of every sequence leaves enough for a long one (single tokens stay in one launch).  One | two:
+// The host does not know which there are: rows of heads have to be so many that a launch with nothing to do counts for little.  As many rows as
+// sequences, or so few more that none is long beside single ones, are taken for single tokens; fewer may be a prompt among sequences that rest.
+// One | two:
 //     a prompt of 2048 tokens and 31 single ones behind 8192   325 | 186      a prompt of 300 and 16 single ones behind 4000   145 | 93
 //     512 behind 3584 and the same 31   275 | 193      a prompt of 2048 and 4 windows of 8 behind 32768   877 | 169
 //     a prompt of 300 behind 16384 and 1000 single ones behind 512   620 | 462
@@ -1535,7 +1536,8 @@ static AttendPlan attend_plan(const QuantCache& c, bool ragged, int n_rows, int 
   const int G = n_heads / c.n_kv_heads;
   const long long total = (long long)n_rows * G, rows = (total + c.n_seqs - 1) / c.n_seqs;      // of a sequence, in the mean
   const long long waves = mean_tiles(c, n_rows, G, 16) * c.n_kv_heads * most_pages(c, (int)(rows / G) + 1, window, sinks);
-  const bool mixed = ragged && c.n_seqs > 1 && G <= SHORT && total > 2048 && total - (long long)c.n_seqs * G > SHORT && waves > 8ll * CUS;
+  const long long more = total - (long long)c.n_seqs * G;                                       // than a row each
+  const bool mixed = ragged && c.n_seqs > 1 && G <= SHORT && total > 2048 && (more < 0 || more > SHORT) && waves > 8ll * CUS;
   p.n = mixed ? 2 : 1;
   for (int i = 0; i < p.n; ++i) {
     AttendPass& x = p.pass[i];
@@ -1608,8 +1610,9 @@ struct WeighPlan {
 //     a prompt of 2048 tokens and 31 single ones behind 8192   386 | 132      256 behind 768 and 63 single ones behind 2048   274 | 96
 //     512 behind 3584 and the same 31   137 | 109      a prompt of 2048 and 4 windows of 8 behind 32768   374 | 156
 //     a prompt of 300 behind 16384 and 1000 single ones behind 512   14680 | 1157
+//     a prompt of 400 behind 4000 among 511 sequences that rest   4552 | 80
 //     against it  64 windows of 8 behind 4096   79 | 94      2048 windows of 2 behind 512   244 | 498: workgroups that look for long sequences
-//     512 single tokens behind 2048 (were they not left out)   236 | 278      2048 behind 512   237 | 382
+//     512 single tokens behind 2048   236 | 278      2048 behind 512   237 | 382, left here, as a prompt of as many rows as sequences would take ms
 static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_heads, int window, int sinks) {
   WeighPlan p;
   const int G = n_heads / c.n_kv_heads, M = (n_rows + c.n_seqs - 1) / c.n_seqs;
@@ -1618,8 +1621,7 @@ static WeighPlan weigh_plan(const QuantCache& c, bool ragged, int n_rows, int n_
   const int fours = (p.pages + WEIGH_WAVES - 1) / WEIGH_WAVES;
   // of long sequences, of 64 rows in all of them, and of slices: 16 tiles or more each, and at most 64 more than there are sequences
   const long long longs = min((long long)c.n_seqs, total / 65), all = total / 64 + longs, tiles = max(16ll, (all + 63) / 64), ids = all / tiles + longs;
-  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && total - (long long)c.n_seqs * G > 64 &&
-                     ids * c.n_kv_heads * p.pages <= 1 << 20;      // 256 MiB
+  const bool mixed = ragged && c.n_seqs > 1 && c.n_seqs <= 32768 && total > 2048 && ids * c.n_kv_heads * p.pages <= 1 << 20;      // 256 MiB
   p.n = mixed ? 2 : 1, p.parts = 0;
   for (int i = 0; i < p.n; ++i) {
     WeighPass& x = p.pass[i];

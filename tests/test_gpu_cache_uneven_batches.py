@@ -19,6 +19,8 @@ def _rows(kind):
         rows = [1] * 200 + [300] + [1] * 57
     elif kind == "one long among none":                      # more tiles than a row of every sequence leaves
         rows = [0] * 150 + [900] + [0] * 150
+    elif kind == "as many rows as sequences":
+        rows = [0] * 400 + [500] + [0] * 99
     elif kind == "several among none":
         rows = [0] * 70 + [257] + [0] * 80 + [333, 41, 700] + [0] * 200 + [5]
     elif kind == "long ones only":
@@ -31,7 +33,7 @@ def _rows(kind):
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (600, 3)])
 @pytest.mark.parametrize("heads,kv,d", [(8, 2, 64), (16, 2, 128), (20, 1, 64)])
-@pytest.mark.parametrize("kind", ["nobody long", "one long among single tokens", "one long among none", "several among none", "long ones only"])
+@pytest.mark.parametrize("kind", ["nobody long", "one long among single tokens", "one long among none", "as many rows as sequences", "several among none", "long ones only"])
 def test_attention(kind, heads, kv, d, window, sinks):
     import paper_2408_11850_amd as amd
     amd.load_library()
@@ -52,7 +54,7 @@ def test_attention(kind, heads, kv, d, window, sinks):
 
 @pytest.mark.parametrize("window,sinks", [(0, 0), (600, 3)])
 @pytest.mark.parametrize("heads,kv,d", [(8, 2, 64), (16, 2, 128), (20, 1, 64)])
-@pytest.mark.parametrize("kind", ["nobody long", "one long among single tokens", "one long among none", "several among none", "long ones only"])
+@pytest.mark.parametrize("kind", ["nobody long", "one long among single tokens", "one long among none", "as many rows as sequences", "several among none", "long ones only"])
 def test_weights(kind, heads, kv, d, window, sinks):
     """Terms off by (d + 5) steps of their exponents' magnitudes; sums of positive terms, as deep as a sequence's rows at most."""
     import paper_2408_11850_amd as amd
